@@ -12,9 +12,11 @@
  * ---------------------------------------
  * - Pointers are DEVICE pointers (memory the HIP runtime of this process
  *   allocated on the current device) unless the comment says HOST.
- * - Arrays are dense and row-major; no strides. Every device pointer must be
- *   16-byte aligned, except fp16 scale arrays, which need 2-byte alignment
- *   (QGEMM_EALIGN otherwise).
+ * - Arrays are dense and row-major; no strides, but for the row strides that the
+ *   serving entry points take. Every device pointer must be 16-byte aligned,
+ *   except fp16 scale arrays, which need 2-byte alignment, and the tables of
+ *   the serving entry points, which need that of their elements (QGEMM_EALIGN
+ *   otherwise).
  * - Work is enqueued on `stream` (0 = the null stream) and the call returns
  *   without synchronising; device faults surface at the caller's next sync.
  *   The caller keeps every buffer alive until the stream has passed the call.
@@ -51,6 +53,15 @@ typedef struct ihipStream_t* hipStream_t;
 #endif
 
 enum qgemm_fmt { QGEMM_Q8 = 0, QGEMM_Q4 = 1 };
+
+enum qgemm_type { QGEMM_F32 = 0, QGEMM_BF16 = 1 };
+
+enum qgemm_rope_scaling {
+  QGEMM_ROPE_PLAIN = 0,
+  QGEMM_ROPE_LINEAR = 1,
+  QGEMM_ROPE_LLAMA3 = 2,
+  QGEMM_ROPE_YARN = 3
+};
 
 enum qgemm_status {
   QGEMM_OK = 0,
@@ -242,6 +253,157 @@ const char* qgemm_last_error(void);
 int qgemm_attention_prefill(const void* q, const void* k, const void* v, void* o,
                             int B, int S, int H, int Hkv, int D,
                             float scale, int causal, hipStream_t stream);
+
+/*
+ * Serving: what stands between the QKV and the output projection of a step over
+ * a ragged batch (decode, Section 2.3, and prompts of different lengths).
+ *
+ *   qgemm_kv_plan -> QKV projection -> qgemm_rope -> qgemm_kv4_store ->
+ *   qgemm_attention_packed (prompts) / qgemm_attention_kv4 (over the cache)
+ *
+ * The step's T rows hold the new tokens of R requests end to end, request r in
+ * rows cu_q[r] .. cu_q[r+1]-1. Row strides are in elements; the heads of a row
+ * are contiguous, so query, key and value heads can be views of one projection
+ * row. Rows at or past cu_q[R] belong to no request and are left as they are.
+ * Tables live in device memory and the host does not read them: tables that
+ * contradict each other or the sizes are a caller error, every access stays in
+ * bounds, and each entry point says what it makes of them.
+ *
+ * The 4-bit cache: uint8 [pages][Hkv][page*(D + D/16)], page a power of two in
+ * [16, 1024], D 64 or 128. The record of one page and head holds the key codes
+ * [page][D/2], the value codes [page][D/2], the key scales [page][D/32] and the
+ * value scales [page][D/32] (microscaled 4-bit floating point): a code is an
+ * e2m1 number (bit 3 the sign; 0, 0.5, 1, 1.5, 2, 3, 4, 6), element 2j in the
+ * low nibble of byte j; a scale byte E stands for 2^(E-127), 255 for NaN.
+ * Token p of a request is at slot block_table[r][p / page] * page + p % page.
+ */
+
+/*
+ * Block tables, slots and positions of a step, from the requests' lengths, in one
+ * launch. For request r with kv_len[r] tokens in the cache and q_len[r] new
+ * ones (negative lengths count as 0; sums below 2^31):
+ *   have = ceil(kv_len / page), need = ceil((kv_len + q_len) / page)
+ *   block_table[r][j] = free_pages[f + j - have] for have <= j < need,
+ *     f the sum of (need - have) over the requests before r; entries below
+ *     have are read, those from need on left as they are
+ *   cu_q[r] = sum of q_len before r; total_len[r] = kv_len[r] + q_len[r]
+ *   the row t = cu_q[r] + i of new token i: positions[t] = kv_len[r] + i,
+ *     slots[t] = its slot
+ *   used[0] = sum of (need - have); rows at or past cu_q[R]: position 0, slot -1
+ * kv_len, q_len, total_len: int32 [R]; block_table: int32 [R][W]; free_pages:
+ * int32 [F]; cu_q: int32 [R+1]; positions, slots: int32 [T]; used: int32 [1].
+ * Outputs alias no input but block_table. Where the free list ends (used[0] > F)
+ * table entries become -1; such a token, one past W pages, one of a negative
+ * table entry and one whose slot is 2^31 or more have slot -1. Tokens past T are
+ * not planned (nor the pages that begin with them). R <= 4096.
+ */
+int qgemm_kv_plan(const int32_t* kv_len, const int32_t* q_len, int32_t* block_table,
+                  const int32_t* free_pages, int32_t* cu_q, int32_t* positions, int32_t* slots,
+                  int32_t* total_len, int32_t* used, int R, int W, int F, int page, int T,
+                  hipStream_t stream);
+
+/*
+ * Frequencies of qgemm_rope for rot dimensions (host only, no launch):
+ *   f_i = base^(-2i / rot), 0 <= i < rot/2, then by `scaling`
+ *   PLAIN: f_i.   LINEAR: f_i / factor.
+ *   LLAMA3, YARN: w f_i + (1 - w) f_i / factor, clamped to 0 <= w <= 1, with
+ *     LLAMA3: w = (length f_i / 2 pi - low) / (high - low): turns over the
+ *       original context, from `low` (divided) to `high` (kept);
+ *     YARN: w = 1 - (i - from) / (to - from), from = max(floor d(high), 0),
+ *       to = min(ceil d(low), rot - 1), d(t) = rot ln(length / 2 pi t) / 2 ln base
+ *       (to - from taken as 0.001 if not positive).
+ * inv_freq: HOST double [rot/2]; gain: HOST, the factor of the sine and cosine,
+ * 0.1 ln(factor) + 1 for YARN and 1 otherwise. rot even, at most 512; base > 1;
+ * factor >= 1; LLAMA3 and YARN: 0 < low < high and length > 0 (what a scaling
+ * does not use is ignored).
+ */
+int qgemm_rope_frequencies(double* inv_freq, float* gain, int rot, double base, int scaling,
+                           double factor, double low, double high, double length);
+
+/*
+ * Rotary positions on rows of heads, and their conversion to bf16:
+ *   for the first rot_heads heads and the pairs (a, b) of a head's first rot
+ *   elements, pair i at (i, i + rot/2) or, interleaved = 1, at (2i, 2i + 1), with
+ *   the angle positions[t] * inv_freq[i]:
+ *     a' = gain (a cos - b sin),  b' = gain (a sin + b cos)
+ *   every other element is only rounded.
+ * So one call takes whole QKV rows, with rot_heads = query and key heads.
+ * x: fp32 (as qgemm_dense writes it) or bf16 [T][heads][D] at x_stride elements
+ * between rows, x_type QGEMM_F32 or QGEMM_BF16; y: bf16 at y_stride; bf16 x may
+ * be y itself at the same stride, and may not overlap it otherwise. positions:
+ * int32 [T]; inv_freq: double [rot/2] in device memory. The angle's turns are
+ * taken in fp64 and its sine, cosine and the rotation in fp32; bf16 rounding to
+ * nearest even. D and rot even, rot <= min(D, 512); any stride >= heads*D and
+ * addresses aligned to the elements (16 elements are moved at once where D, rot,
+ * strides and addresses are multiples of 16 elements or bytes, else two).
+ */
+int qgemm_rope(const void* x, int x_type, const int32_t* positions, const double* inv_freq, void* y,
+               int T, int heads, int rot_heads, int D, int rot, int64_t x_stride, int64_t y_stride,
+               int interleaved, float gain, hipStream_t stream);
+
+/*
+ * Keys and values of T tokens into the 4-bit cache. k, v: bf16 [T][Hkv][D] at
+ * k_stride / v_stride elements between rows (multiples of 8); slots: int32 [T],
+ * tokens whose slot is outside [0, pages*page) are skipped; two tokens of one
+ * slot leave it unspecified. For each block of 32 elements of a head:
+ *   E = floor(log2(largest magnitude, rounded to two significant bits, ties up)) - 2,
+ *     at least -126; codes = x / 2^E to the nearest level, ties to the even code
+ * (so a block's largest magnitudes are at most half a level step off, 7 going to
+ * 8 and not to 6). A block with an infinity or NaN is held as NaN.
+ */
+int qgemm_kv4_store(const void* k, const void* v, const int32_t* slots, void* cache, int T, int Hkv,
+                    int D, int64_t k_stride, int64_t v_stride, int pages, int page,
+                    hipStream_t stream);
+
+/*
+ * The cache's keys and values of T slots, as the bf16 numbers they stand for
+ * (exact but below bf16's range): k, v: bf16 [T][Hkv][D], dense. Rows whose slot is outside
+ * [0, pages*page) are left as they are.
+ */
+int qgemm_kv4_load(const void* cache, const int32_t* slots, void* k, void* v, int T, int Hkv, int D,
+                   int pages, int page, hipStream_t stream);
+
+/*
+ * Prefill attention over prompts of different lengths packed end to end, each
+ * causal in itself: as qgemm_attention_prefill for every prompt, row t of
+ * prompt r (rows cu[r] .. cu[r+1]-1) over the keys cu[r] .. t.
+ * q, o: bf16 [T][H][D]; k, v: bf16 [T][Hkv][D], at their strides (elements,
+ * multiples of 8); cu: int32 [R+1], ascending, cu[0] == 0, cu[R] <= T; prompts
+ * of no rows may stand among them. Rows at or past cu[R] are neither read nor
+ * written. A prompt's rows depend on no other prompt, whatever that holds
+ * (infinities and NaN included), nor on later rows. D is 64 or 128; T*H*D < 2^31;
+ * q, k and v each span less than 4 GiB. Precision as qgemm_attention_prefill.
+ * A cu that does not ascend gives unspecified rows.
+ */
+int qgemm_attention_packed(const void* q, const void* k, const void* v, const int32_t* cu, void* o,
+                           int T, int R, int H, int Hkv, int D, int64_t q_stride, int64_t k_stride,
+                           int64_t v_stride, int64_t o_stride, float scale, hipStream_t stream);
+
+/*
+ * Attention of new tokens over the 4-bit cache (their own keys and values stored
+ * there before): single tokens, drafted tokens, the chunk of a long prompt. With
+ * n = cu_q[r+1] - cu_q[r] new tokens (1 for every request if cu_q is null; then
+ * T == R) and kv_len[r] keys in all, new token i is at position
+ * p = kv_len[r] - n + i and sees the keys 0 .. p:
+ *   o[cu_q[r] + i][h] = sum_j softmax_j(scale q . k_j[g]) v_j[g],  g = h / (H / Hkv)
+ * A row that sees no key (p < 0) gives 0.
+ * q: bf16 [T][H][D] at q_stride elements between rows (a multiple of 8); o: bf16
+ * [T][H][D], dense; cache, block_table as above, kv_len: int32 [R]; cu_q: int32
+ * [R+1], ascending, or null. fp32 scores, sums and accumulation; the softmax
+ * weights enter the output product as bf16. Keys of a page outside [0, pages) or
+ * past the table's W entries make the rows that see them NaN; nothing else that
+ * the pages hold behind a row's position reaches it. Results do not depend on how the
+ * work was split beyond fp32 summation order, and are the same on every call.
+ * workspace: caller-owned device memory, 16-byte aligned, of the bytes that
+ * qgemm_attention_kv4_workspace gives for the same sizes; it needs no
+ * initialisation, and calls that can overlap need one each. W*page <= 2^30,
+ * T*H*D < 2^31, R <= 2^20. R == 0 or T == 0 is a no-op.
+ */
+int qgemm_attention_kv4(const void* q, const void* cache, const int32_t* block_table,
+                        const int32_t* kv_len, const int32_t* cu_q, void* o, void* workspace,
+                        int64_t workspace_bytes, int T, int R, int H, int Hkv, int D, int W, int pages,
+                        int page, int64_t q_stride, float scale, hipStream_t stream);
+int qgemm_attention_kv4_workspace(int T, int R, int H, int Hkv, int D, int W, int page, int64_t* bytes);
 
 /*
  * Measurement utility, not part of the GEMM path: runs `iters` rounds of four

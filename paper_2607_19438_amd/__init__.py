@@ -16,7 +16,8 @@ import os
 import torch  # imported before the library so that both share one HIP runtime
 
 __all__ = ["Q8", "Q4", "QGemmError", "lib", "lib_path", "dense", "moe", "moe_noalloc", "moe_bucket", "moe_grouped",
-           "moe_gate_up_swiglu", "moe_down_combine", "swiglu", "moe_combine", "attention_prefill", "probe_mfma_clock", "last_error", "release", "version", "EXPORTS", "ExpertTable"]
+           "moe_gate_up_swiglu", "moe_down_combine", "swiglu", "moe_combine", "attention_prefill", "probe_mfma_clock", "last_error", "release", "version", "EXPORTS", "ExpertTable",
+           "KvPlan", "kv_plan", "rope_frequencies", "rope", "kv4_cache_shape", "kv4_store", "kv4_load", "attention_packed", "attention_kv4"]
 
 Q8 = 0
 Q4 = 1
@@ -25,6 +26,9 @@ _LIB_PATH = os.path.join(_HERE, "libqgemm.so")
 
 _vp = ctypes.c_void_p
 _i = ctypes.c_int
+_l = ctypes.c_int64
+_d = ctypes.c_double
+_f = ctypes.c_float
 # name -> (restype, argtypes); mirrors include/qgemm.h
 EXPORTS = {
     "qgemm_dense": (_i, [_vp, _vp, _vp, _vp, _i, _i, _i, _i, _vp]),
@@ -37,6 +41,14 @@ EXPORTS = {
     "qgemm_swiglu": (_i, [_vp, _vp, _i, _i, _vp]),
     "qgemm_moe_combine": (_i, [_vp, _vp, _vp, _i, _i, _i, _vp]),
     "qgemm_attention_prefill": (_i, [_vp, _vp, _vp, _vp, _i, _i, _i, _i, _i, ctypes.c_float, _i, _vp]),
+    "qgemm_kv_plan": (_i, [_vp] * 9 + [_i] * 5 + [_vp]),
+    "qgemm_rope_frequencies": (_i, [ctypes.POINTER(_d), ctypes.POINTER(_f), _i, _d, _i, _d, _d, _d, _d]),
+    "qgemm_rope": (_i, [_vp, _i, _vp, _vp, _vp, _i, _i, _i, _i, _i, _l, _l, _i, _f, _vp]),
+    "qgemm_kv4_store": (_i, [_vp, _vp, _vp, _vp, _i, _i, _i, _l, _l, _i, _i, _vp]),
+    "qgemm_kv4_load": (_i, [_vp, _vp, _vp, _vp, _i, _i, _i, _i, _i, _vp]),
+    "qgemm_attention_packed": (_i, [_vp] * 5 + [_i] * 5 + [_l] * 4 + [_f, _vp]),
+    "qgemm_attention_kv4": (_i, [_vp] * 7 + [_l] + [_i] * 8 + [_l, _f, _vp]),
+    "qgemm_attention_kv4_workspace": (_i, [_i] * 7 + [ctypes.POINTER(_l)]),
     "qgemm_probe_mfma_clock": (_i, [_i, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_double), _vp]),
     "qgemm_last_error": (ctypes.c_char_p, []),
     "qgemm_release": (_i, []),
@@ -367,6 +379,233 @@ def attention_prefill(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal:
         raise ValueError("out must have the shape of q")
     _check(lib().qgemm_attention_prefill(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), B, S, H, Hkv, D,
                                          float(scale), int(bool(causal)), _stream(q)))
+    return out
+
+
+# ---------------------------------------------------------------------------
+# serving: a step over a ragged batch
+# ---------------------------------------------------------------------------
+
+_I32 = (torch.int32,)
+_BF16 = (torch.bfloat16,)
+
+
+def _need_rows(t: torch.Tensor, name: str, dtypes):
+    """A tensor [T][heads][D] whose heads lie end to end; returns the elements between rows."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a GPU tensor")
+    if t.dtype not in dtypes:
+        raise TypeError(f"{name} has dtype {t.dtype}, expected one of {dtypes}")
+    if t.dim() != 3:
+        raise ValueError(f"{name} must have 3 dimensions")
+    T, h, D = t.shape
+    s = t.stride()
+    if (D > 1 and s[2] != 1) or (h > 1 and s[1] != D):
+        raise ValueError(f"the heads of a row of {name} must be contiguous")
+    return s[0] if T > 1 else h * D
+
+
+def _enqueue(fn, tensors, *args):
+    """``fn(*args, stream)`` on the current stream of the tensors' device, which they must share."""
+    dev = tensors[0].get_device()
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            raise ValueError("the tensors must be on one device")
+    if torch.cuda.current_device() == dev:
+        _check(fn(*args, _stream(tensors[0])))
+    else:
+        with torch.cuda.device(dev):
+            _check(fn(*args, _stream(tensors[0])))
+
+
+class KvPlan:
+    """What ``kv_plan`` gives: ``cu_q`` [R+1], ``positions`` [T], ``slots`` [T], ``kv_len`` [R] (with the new
+    tokens) and ``used`` [1] (pages taken from the free list), all int32 on the GPU."""
+
+    __slots__ = ("cu_q", "positions", "slots", "kv_len", "used")
+
+    def __init__(self, R: int, T: int, device):
+        # one allocation, as the plan of a small step is all latency
+        n = torch.empty(2 * R + 2 + 2 * T, dtype=torch.int32, device=device)
+        self.cu_q, self.kv_len, self.used, self.positions, self.slots = n.split((R + 1, R, 1, T, T))
+
+
+def kv_plan(kv_len, q_len, block_table, free_pages, page: int, tokens: int, out: KvPlan | None = None) -> KvPlan:
+    """Slots, positions and first rows of a step's tokens, and the pages it adds to ``block_table`` (``qgemm_kv_plan``).
+
+    ``kv_len`` / ``q_len`` [R]: tokens in the cache / new ones; ``block_table`` [R][W] is updated in place from
+    ``free_pages``; ``tokens``: rows of the step, those behind the last token have slot -1. ``out``: an earlier
+    plan of the same sizes to write into."""
+    _need(kv_len, "kv_len", _I32, 1)
+    _need(q_len, "q_len", _I32, 1)
+    _need(block_table, "block_table", _I32, 2)
+    _need(free_pages, "free_pages", _I32, 1)
+    R = kv_len.shape[0]
+    if q_len.shape[0] != R or block_table.shape[0] != R:
+        raise ValueError("kv_len, q_len and block_table disagree on the number of requests")
+    if tokens < 0:
+        raise ValueError("tokens must be >= 0")
+    if out is None:
+        out = KvPlan(R, tokens, kv_len.device)
+    for name, n in (("cu_q", R + 1), ("positions", tokens), ("slots", tokens), ("kv_len", R), ("used", 1)):
+        t = getattr(out, name)
+        _need(t, "out." + name, _I32, 1)
+        if t.shape[0] != n:
+            raise ValueError(f"out.{name} must have {n} entries")
+    _enqueue(lib().qgemm_kv_plan, (kv_len, q_len, block_table, free_pages, out.cu_q, out.positions, out.slots, out.kv_len, out.used),
+             kv_len.data_ptr(), q_len.data_ptr(), block_table.data_ptr(), free_pages.data_ptr(), out.cu_q.data_ptr(),
+             out.positions.data_ptr(), out.slots.data_ptr(), out.kv_len.data_ptr(), out.used.data_ptr(), R,
+             block_table.shape[1], free_pages.shape[0], page, tokens)
+    return out
+
+
+_SCALINGS = {"none": 0, "linear": 1, "llama3": 2, "yarn": 3}
+
+
+def rope_frequencies(rot: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0, low: float = 1.0,
+                     high: float = 0.0, length: float = 0.0, device=None):
+    """``(inv_freq, gain)`` for ``rope`` (``qgemm_rope_frequencies``): float64 [rot/2] on ``device`` (the current GPU
+    by default) and the factor of the sine and cosine.
+
+    ``scaling``: "none"; "linear" (``factor``); "llama3" and "yarn" (``factor``, the original context's ``length``, and
+    the turns over it up to ``low`` of which a pair is divided by ``factor`` and from ``high`` on kept)."""
+    if scaling not in _SCALINGS:
+        raise ValueError(f"scaling must be one of {tuple(_SCALINGS)}")
+    f = torch.empty(max(rot // 2, 1), dtype=torch.float64)
+    gain = _f(1.0)
+    _check(lib().qgemm_rope_frequencies(ctypes.cast(f.data_ptr(), ctypes.POINTER(_d)), ctypes.byref(gain), rot, base,
+                                        _SCALINGS[scaling], factor, low, high, length))
+    return f.to("cuda" if device is None else device), gain.value
+
+
+def rope(x: torch.Tensor, positions: torch.Tensor, inv_freq: torch.Tensor, rot_heads: int, interleaved: bool = False,
+         gain: float = 1.0, out: torch.Tensor | None = None):
+    """Rotary positions on the first ``rot_heads`` heads of rows ``x`` [T][heads][D], fp32 or bf16, and their conversion
+    to bf16 (``qgemm_rope``). The first ``2 * len(inv_freq)`` elements of a head are rotated, as pairs half of them
+    apart or (``interleaved``) neighbouring. ``out``: bf16, may be a bf16 ``x`` itself."""
+    xs = _need_rows(x, "x", (torch.float32, torch.bfloat16))
+    _need(positions, "positions", _I32, 1)
+    _need(inv_freq, "inv_freq", (torch.float64,), 1)
+    T, heads, D = x.shape
+    if positions.shape[0] != T:
+        raise ValueError("x and positions disagree on T")
+    if out is None:
+        out = torch.empty((T, heads, D), dtype=torch.bfloat16, device=x.device)
+    ys = _need_rows(out, "out", _BF16)
+    if out.shape != x.shape:
+        raise ValueError("out must have the shape of x")
+    _enqueue(lib().qgemm_rope, (x, positions, inv_freq, out), x.data_ptr(), int(x.dtype == torch.bfloat16), positions.data_ptr(),
+             inv_freq.data_ptr(), out.data_ptr(), T, heads, rot_heads, D, 2 * inv_freq.shape[0], xs, ys, int(bool(interleaved)),
+             float(gain))
+    return out
+
+
+def kv4_cache_shape(pages: int, Hkv: int, D: int, page: int):
+    """Shape of the uint8 tensor of a paged 4-bit cache: ``(pages, Hkv, page * (D + D/16))``."""
+    return pages, Hkv, page * (D + D // 16)
+
+
+def _cache_sizes(cache: torch.Tensor, D: int):
+    _need(cache, "cache", (torch.uint8,), 3)
+    pages, Hkv, record = cache.shape
+    if D < 16 or record * 16 % (17 * D):
+        raise ValueError(f"the cache's records of {record} bytes hold no whole number of slots of head dimension {D}")
+    return pages, Hkv, record * 16 // (17 * D)
+
+
+def kv4_store(k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, cache: torch.Tensor):
+    """Quantises ``k``, ``v`` [T][Hkv][D] bf16 into the cache's ``slots`` [T] (``qgemm_kv4_store``); negative slots are
+    skipped. ``cache``: uint8 of ``kv4_cache_shape``."""
+    ks = _need_rows(k, "k", _BF16)
+    vs = _need_rows(v, "v", _BF16)
+    _need(slots, "slots", _I32, 1)
+    T, Hkv, D = k.shape
+    pages, heads, page = _cache_sizes(cache, D)
+    if v.shape != k.shape or heads != Hkv or slots.shape[0] != T:
+        raise ValueError("k, v, slots and cache disagree on T, Hkv or D")
+    _enqueue(lib().qgemm_kv4_store, (k, v, slots, cache), k.data_ptr(), v.data_ptr(), slots.data_ptr(), cache.data_ptr(), T, Hkv, D, ks, vs,
+             pages, page)
+
+
+def kv4_load(cache: torch.Tensor, slots: torch.Tensor, D: int, k: torch.Tensor | None = None, v: torch.Tensor | None = None):
+    """The keys and values of the cache's ``slots`` [T] as bf16 [T][Hkv][D] each (``qgemm_kv4_load``); rows of negative
+    slots are left as they are in ``k`` and ``v``."""
+    _need(slots, "slots", _I32, 1)
+    pages, Hkv, page = _cache_sizes(cache, D)
+    shape = (slots.shape[0], Hkv, D)
+    if k is None:
+        k = torch.empty(shape, dtype=torch.bfloat16, device=cache.device)
+    if v is None:
+        v = torch.empty(shape, dtype=torch.bfloat16, device=cache.device)
+    _need(k, "k", _BF16, 3)
+    _need(v, "v", _BF16, 3)
+    if k.shape != shape or v.shape != shape:
+        raise ValueError("k and v must be [T][Hkv][D]")
+    _enqueue(lib().qgemm_kv4_load, (cache, slots, k, v), cache.data_ptr(), slots.data_ptr(), k.data_ptr(), v.data_ptr(), shape[0], Hkv, D,
+             pages, page)
+    return k, v
+
+
+def attention_packed(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu: torch.Tensor, scale: float | None = None,
+                     out: torch.Tensor | None = None):
+    """Causal attention over prompts packed end to end, prompt r in rows ``cu[r] .. cu[r+1]-1``
+    (``qgemm_attention_packed``): q ``[T][H][D]``, k / v ``[T][Hkv][D]`` bf16, views of one projection row among
+    them -> o ``[T][H][D]`` bf16. Rows behind the last prompt are not written."""
+    qs = _need_rows(q, "q", _BF16)
+    ks = _need_rows(k, "k", _BF16)
+    vs = _need_rows(v, "v", _BF16)
+    _need(cu, "cu", _I32, 1)
+    T, H, D = q.shape
+    if k.shape != v.shape or k.shape[0] != T or k.shape[2] != D:
+        raise ValueError("q, k and v disagree on T or D")
+    if cu.shape[0] < 1:
+        raise ValueError("cu must have one entry more than there are prompts")
+    if scale is None:
+        scale = 1.0 / float(D) ** 0.5
+    if out is None:
+        out = torch.empty((T, H, D), dtype=torch.bfloat16, device=q.device)
+    ys = _need_rows(out, "out", _BF16)
+    if out.shape != q.shape:
+        raise ValueError("out must have the shape of q")
+    _enqueue(lib().qgemm_attention_packed, (q, k, v, cu, out), q.data_ptr(), k.data_ptr(), v.data_ptr(), cu.data_ptr(), out.data_ptr(), T,
+             cu.shape[0] - 1, H, k.shape[1], D, qs, ks, vs, ys, float(scale))
+    return out
+
+
+def attention_kv4(q: torch.Tensor, cache: torch.Tensor, block_table: torch.Tensor, kv_len: torch.Tensor,
+                  cu_q: torch.Tensor | None = None, scale: float | None = None, out: torch.Tensor | None = None):
+    """Attention of new tokens over the paged 4-bit cache (``qgemm_attention_kv4``): q ``[T][H][D]`` bf16 -> o
+    ``[T][H][D]`` bf16. ``kv_len`` [R]: each request's keys, the new tokens' own (stored before) among them;
+    ``cu_q`` [R+1]: first rows of the requests, or None where each has one token. Rows behind the last request
+    are not written."""
+    qs = _need_rows(q, "q", _BF16)
+    _need(block_table, "block_table", _I32, 2)
+    _need(kv_len, "kv_len", _I32, 1)
+    T, H, D = q.shape
+    pages, Hkv, page = _cache_sizes(cache, D)
+    R, W = block_table.shape
+    if kv_len.shape[0] != R or (cu_q is None and T != R):
+        raise ValueError("q, block_table and kv_len disagree on the number of requests")
+    if cu_q is not None:
+        _need(cu_q, "cu_q", _I32, 1)
+        if cu_q.shape[0] != R + 1:
+            raise ValueError("cu_q must have one entry more than there are requests")
+    if scale is None:
+        scale = 1.0 / float(D) ** 0.5
+    if out is None:
+        out = torch.empty((T, H, D), dtype=torch.bfloat16, device=q.device)
+    _need(out, "out", _BF16, 3)
+    if out.shape != q.shape:
+        raise ValueError("out must have the shape of q")
+    n = _l(0)
+    _check(lib().qgemm_attention_kv4_workspace(T, R, H, Hkv, D, W, page, ctypes.byref(n)))
+    # of the call's own: torch's allocator keeps it from other streams, and inside a capture it is the graph's
+    ws = torch.empty(n.value, dtype=torch.uint8, device=q.device)
+    _enqueue(lib().qgemm_attention_kv4, (q, cache, block_table, kv_len, cu_q, out), q.data_ptr(), cache.data_ptr(),
+             block_table.data_ptr(), kv_len.data_ptr(), None if cu_q is None else cu_q.data_ptr(), out.data_ptr(),
+             ws.data_ptr(), n.value, T, R, H, Hkv, D, W, pages, page, qs, float(scale))
     return out
 
 

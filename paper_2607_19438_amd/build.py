@@ -12,9 +12,10 @@ import tempfile
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libqgemm.so")
-SOURCES = [os.path.join(CSRC, f) for f in ("qgemm_api.hip", "moe_direct.hip")]
+SOURCES = [os.path.join(CSRC, f) for f in ("qgemm_api.hip", "moe_direct.hip", "serve_api.hip")]
 DEPS = SOURCES + [os.path.join(CSRC, f) for f in ("qgemm_kernels.hpp", "qgemm_aux.hpp", "qgemm_smallm.hpp", "moe_direct.hpp",
-                                                  "moe_direct_api.hpp", "tile_rules.hpp", "attn_kernels.hpp")] + [
+                                                  "moe_direct_api.hpp", "tile_rules.hpp", "attn_kernels.hpp", "api_util.hpp",
+                                                  "serve_kernels.hpp", "attn_kv4.hpp")] + [
     os.path.join(os.path.dirname(HERE), "include", "qgemm.h")]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

@@ -25,6 +25,13 @@
 // and barrier work per MFMA. Measured (unsplit -> split, us): causal 512 x 32/8 heads D=128 14.6 -> 11.1,
 // 4 x 300 x 8/8 10.4 -> 8.5, 3 x 700 x 32/8 D=64 18.3 -> 15.3, 2048 x 32/4 D=128 48.1 -> 46.8, 4096 x 32/4
 // 142 -> 155; not causal 2 x 1000 x 16/4 D=64 15.8 -> 14.8, 2048 x 32/4 D=128 66.8 -> 77.0.
+//
+// PACKED: prompts of different lengths end to end, causal within each. The workgroups own query rows of the
+// packed sequence as if it were one prompt, across borders: row i sees the keys from its own prompt's first
+// row to i, so a workgroup walks the key blocks from the first row of its first row's prompt, and blocks on a
+// border are masked key by key as blocks on the diagonal are. ceil(T / rows) workgroups per head for any mix
+// of lengths (a tile per prompt would leave most of a tile empty for short ones), the number is known without
+// the lengths, and a border costs masked blocks in one tile only.
 #pragma once
 
 #include "qgemm_kernels.hpp"
@@ -46,6 +53,10 @@ struct AttnArgs {
   int H;
   int Hkv;
   float sl2;           // softmax scale * log2(e)
+  // PACKED: S rows in all (B = 1), R prompts, prompt r in rows cu[r] .. cu[r + 1] - 1; elements between rows
+  const int32_t* cu;
+  int R;
+  long qs, ks, vs, os;
 };
 
 // The kernel body lives in a device function (the kernel below only forwards to it): its
@@ -59,9 +70,87 @@ __device__ __forceinline__ float other_half(float x) {
   return __builtin_bit_cast(float, (unsigned)(lane < 32 ? r[1] : r[0]));
 }
 
-template <int D, bool CAUSAL, bool SPLIT>
+// First rows of the prompts that the BQ packed rows from q0 on belong to, written to starts[BQ] (LDS). The last
+// prompt that starts at or before q0 is found with a step per factor of kAttnThreads in R; those that start
+// inside the tile mark their row, and a running maximum spreads the marks. Rows before cu[0] or behind cu[R],
+// and tables that do not ascend, give some row in [0, i] for row i.
+template <int BQ>
+__device__ __forceinline__ void packed_starts(const AttnArgs& a, int q0, int* starts) {
+  const int tid = threadIdx.x;
+  int lo = 0, n = a.R + 1;             // entries lo .. lo + n - 1; entry lo is at or before q0 (taken as row 0 at lo = 0)
+  while (n > 1) {
+    const int step = (n + kAttnThreads - 1) / kAttnThreads;
+    const int at = tid * step;
+    const int c = __syncthreads_count(at < n && a.cu[lo + at] <= q0);
+    const int to = max(c - 1, 0) * step;
+    lo += to;
+    n = step > 1 ? min(step, n - to) : 1;
+  }
+  if (tid < BQ) starts[tid] = tid == 0 ? min(max(a.cu[lo], 0), q0) : 0;
+  __syncthreads();
+  for (int e = lo + 1;; e += kAttnThreads) {
+    const int v = e + tid <= a.R ? a.cu[e + tid] : 0x7fffffff;
+    if (v > q0 && v < q0 + BQ) starts[v - q0] = v;
+    if (!__syncthreads_and(v < q0 + BQ)) break;
+  }
+  if (tid < 64) {
+    constexpr int PER = BQ / 64;
+    int v[PER], top = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) v[i] = top = max(top, starts[tid * PER + i]);
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int up = __shfl_up(top, d);
+      if (tid >= d) top = max(top, up);
+    }
+    const int before = __shfl_up(top, 1);
+#pragma unroll
+    for (int i = 0; i < PER; ++i) starts[tid * PER + i] = tid > 0 ? max(v[i], before) : v[i];
+  }
+  __syncthreads();
+}
+
+// One packed row by itself, by a whole wave: o = sum_j softmax(scale q.k)_j v_j over the keys j0 .. row. For rows
+// whose result is not finite: in the tiles a weight of 0 times another prompt's infinite or NaN value is NaN.
+template <int D>
+__device__ __noinline__ void packed_row(const AttnArgs& a, int row, int j0, int h, int g) {
+  const int lane = threadIdx.x & 63;
+  const uint16_t* q = a.q + (size_t)row * a.qs + (size_t)h * D;
+  auto f = [](uint16_t b) { return __builtin_bit_cast(float, (uint32_t)b << 16); };
+  auto score = [&](int j) {
+    const uint16_t* k = a.k + (size_t)j * a.ks + (size_t)g * D;
+    float s = 0.0f;
+    for (int d = 0; d < D; ++d) s = __builtin_fmaf(f(q[d]), f(k[d]), s);
+    return s;
+  };
+  float m = -__builtin_inff();
+  for (int j = j0 + lane; j <= row; j += 64) m = fmaxf(m, score(j));
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
+  float l = 0.0f, o[D / 64] = {};
+  for (int jb = j0; jb <= row; jb += 64) {
+    const int j = jb + lane;
+    const float p = j <= row ? __builtin_amdgcn_exp2f((score(j) - m) * a.sl2) : 0.0f;
+    l += p;
+    const int n = min(64, row + 1 - jb);
+    for (int i = 0; i < n; ++i) {
+      const float pi = __shfl(p, i);
+      const uint16_t* v = a.v + (size_t)(jb + i) * a.vs + (size_t)g * D;
+#pragma unroll
+      for (int c = 0; c < D / 64; ++c) o[c] = __builtin_fmaf(pi, f(v[64 * c + lane]), o[c]);
+    }
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) l += __shfl_xor(l, d);
+#pragma unroll
+  for (int c = 0; c < D / 64; ++c)
+    a.o[(size_t)row * a.os + (size_t)h * D + 64 * c + lane] = (uint16_t)pack_bf16x2(o[c] / l, 0.0f);
+}
+
+template <int D, bool CAUSAL, bool SPLIT, bool PACKED = false>
 __device__ __forceinline__ void attn_body(const AttnArgs& a) {
   static_assert(D == 64 || D == 128, "head dimension 64 or 128");
+  static_assert(CAUSAL || !PACKED, "packed prompts are causal");
   constexpr int BQ = kAttnBQ<SPLIT>;
   constexpr int NT = SPLIT ? 1 : 2;           // 32-key tiles of a block per wave
   constexpr int KCH = D / 8;                  // 16-byte chunks per key row
@@ -81,10 +170,11 @@ __device__ __forceinline__ void attn_body(const AttnArgs& a) {
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 31;     // this lane's query within the wave (MFMA column)
   const int hh = lane >> 5;      // MFMA lane half
-  const int S = a.S, H = a.H;
-  const int nqb = (S + BQ - 1) / BQ;
+  const int S = PACKED ? min(max(a.cu[a.R], 0), a.S) : a.S;
+  const int H = a.H;
+  const int nqb = ((PACKED ? a.S : S) + BQ - 1) / BQ;
   int bh, qb;
-  if (CAUSAL && SPLIT) {
+  if (CAUSAL && (SPLIT || PACKED)) {
     // the heaviest query blocks of all heads first, so that light ones fill in. Workgroups reach the 8
     // XCDs round-robin: with a multiple of 8 heads each XCD takes consecutive ones, which share keys and
     // values in its L2
@@ -121,14 +211,27 @@ __device__ __forceinline__ void attn_body(const AttnArgs& a) {
   const int qs = q0 + (SPLIT ? wave & 1 : wave) * 32;   // the wave's first query position
   const int qrow = qs + col;                  // this lane's query position
 
-  const size_t qstride = (size_t)H * D;       // elements between consecutive tokens of q / o
-  const size_t kstride = (size_t)a.Hkv * D;
+  const size_t qstride = PACKED ? (size_t)a.qs : (size_t)H * D;       // elements between consecutive tokens of q / o
+  const size_t kstride = PACKED ? (size_t)a.ks : (size_t)a.Hkv * D;
+  const size_t vstride = PACKED ? (size_t)a.vs : kstride;
+  int first_row = 0;             // PACKED: first key that this lane's query sees,
+  int wave_lo = 0, wave_hi = 0;  // and those of the wave's first and last query
+  int kb0 = 0;                   // first key block
+  if constexpr (PACKED) {
+    __shared__ int starts[BQ];
+    if (q0 >= S) return;
+    packed_starts<BQ>(a, q0, starts);
+    first_row = starts[qrow - q0];
+    wave_lo = __builtin_amdgcn_readfirstlane(starts[qs - q0]);
+    wave_hi = __builtin_amdgcn_readfirstlane(starts[qs + 31 - q0]);
+    kb0 = __builtin_amdgcn_readfirstlane(starts[0]) / kAttnBK;
+  }
   const __amdgpu_buffer_rsrc_t qr = make_rsrc(a.q + (size_t)b * S * qstride + (size_t)h * D,
                                               (uint32_t)(((size_t)(S - 1) * qstride + D) * 2));
   const __amdgpu_buffer_rsrc_t kr = make_rsrc(a.k + (size_t)b * S * kstride + (size_t)g * D,
                                               (uint32_t)(((size_t)(S - 1) * kstride + D) * 2));
-  const __amdgpu_buffer_rsrc_t vr = make_rsrc(a.v + (size_t)b * S * kstride + (size_t)g * D,
-                                              (uint32_t)(((size_t)(S - 1) * kstride + D) * 2));
+  const __amdgpu_buffer_rsrc_t vr = make_rsrc(a.v + (size_t)b * S * vstride + (size_t)g * D,
+                                              (uint32_t)(((size_t)(S - 1) * vstride + D) * 2));
 
   // query fragments (B operand of K Q^T): step t needs q[qrow][16t + 8hh .. +8]
   bf16x8 qf[KSTEPS];
@@ -173,10 +276,11 @@ __device__ __forceinline__ void attn_body(const AttnArgs& a) {
 #pragma unroll
   for (int i = 0; i < KDMA; ++i) {
     const int krow = (wave * KDMA + i) * KROWS_DMA;
-    vdma_off[i] = ((uint32_t)(krow + dkey) * (uint32_t)kstride + 8u * (uint32_t)((lane % KCH) ^ vswz(krow + dkey))) * 2u;
+    vdma_off[i] = ((uint32_t)(krow + dkey) * (uint32_t)vstride + 8u * (uint32_t)((lane % KCH) ^ vswz(krow + dkey))) * 2u;
   }
+  const uint32_t vblock_bytes = PACKED ? (uint32_t)kAttnBK * (uint32_t)vstride * 2u : kblock_bytes;
   auto dma_values = [&](uint16_t* vs, int jb) {
-    const uint32_t base = (uint32_t)jb * kblock_bytes;
+    const uint32_t base = (uint32_t)jb * vblock_bytes;
 #pragma unroll
     for (int i = 0; i < KDMA; ++i) {
       const int krow = (wave * KDMA + i) * KROWS_DMA;
@@ -195,8 +299,8 @@ __device__ __forceinline__ void attn_body(const AttnArgs& a) {
   float l_run = 0.0f;
   const float sl2 = a.sl2;
 
-  dma_keys(ks0, 0);
-  dma_values(vt0, 0);
+  dma_keys(ks0, kb0);
+  dma_values(vt0, kb0);
   wait_vmcnt_lgkm0<0>();
   __syncthreads();
 
@@ -241,7 +345,7 @@ __device__ __forceinline__ void attn_body(const AttnArgs& a) {
     const int t0 = j0 + 32 * kh;            // the wave's first key of the block
     // (tiles and waves' queries both start at multiples of 32, so every query of a wave sees at least the
     // first key of a block that is not skipped)
-    if ((!SPLIT || t0 < S) && (!CAUSAL || t0 <= qs + 31)) {
+    if ((!SPLIT || t0 < S) && (!CAUSAL || t0 <= qs + 31) && (!PACKED || t0 + 32 * NT > wave_lo)) {
       // scores S^T[key][query] for the wave's keys of the block: two accumulators, one per 32-key tile
       // (SPLIT: even and odd K16 steps), so that no MFMA waits for the one before; the key fragments of
       // step t+2 are read from LDS while the MFMAs of step t run
@@ -271,14 +375,14 @@ __device__ __forceinline__ void attn_body(const AttnArgs& a) {
       __builtin_amdgcn_s_setprio(0);
       if (SPLIT) sc[0] += sc[1];
       // key of register r in tile kt: t0 + kt*32 + (r/4)*8 + 4hh + r%4
-      const bool need_mask = (CAUSAL && t0 + 32 * NT - 1 > qs) || t0 + 32 * NT > S;
+      const bool need_mask = (CAUSAL && t0 + 32 * NT - 1 > qs) || t0 + 32 * NT > S || (PACKED && t0 < wave_hi);
       if (need_mask) {
 #pragma unroll
         for (int kt = 0; kt < NT; ++kt)
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
             const int kp = t0 + kt * 32 + (r >> 2) * 8 + 4 * hh + (r & 3);
-            if (kp >= S || (CAUSAL && kp > qrow)) sc[kt][r] = -__builtin_inff();
+            if (kp >= S || (CAUSAL && kp > qrow) || (PACKED && kp < first_row)) sc[kt][r] = -__builtin_inff();
           }
       }
       float mloc = -__builtin_inff();
@@ -304,8 +408,9 @@ __device__ __forceinline__ void attn_body(const AttnArgs& a) {
       // p = exp2((s - m) * scale * log2 e), one fused multiply-add per score; P^T as packed bf16,
       // per key tile: registers (2i, 2i+1). The second half's exponentials (SPLIT: of the tile's
       // registers, else tile 1's) are written between the first output-product MFMAs so the two overlap.
-      // SPLIT: a half whose keys so far all score -inf (keys with infinities) keeps maximum -inf, weights 0
-      const float ms = (SPLIT && m_run == -__builtin_inff()) ? 0.0f : m_run * sl2;
+      // SPLIT: a half whose keys so far all score -inf (keys with infinities) keeps maximum -inf, weights 0;
+      // PACKED: so does a row whose prompt begins behind the keys so far
+      const float ms = ((SPLIT || PACKED) && m_run == -__builtin_inff()) ? 0.0f : m_run * sl2;
       float lsum = 0.0f;
       uint32_t pf[NT][8];
       auto exp_half = [&](int second) {
@@ -349,7 +454,7 @@ __device__ __forceinline__ void attn_body(const AttnArgs& a) {
     __syncthreads();
   };
 
-  for (int jb = 0; jb < nkb; jb += 2) {
+  for (int jb = kb0; jb < nkb; jb += 2) {
     step(jb, ks0, vt0, ks1, vt1);
     if (jb + 1 < nkb) step(jb + 1, ks1, vt1, ks0, vt0);
   }
@@ -391,8 +496,18 @@ __device__ __forceinline__ void attn_body(const AttnArgs& a) {
   // normalise and store: lane (col, hh) holds o[qrow][dt*32 + 8a + 4hh + {0..3}] in acc_o[dt][4a..4a+3]
   const float l_tot = l_run + other_half(l_run);
   const float inv = 1.0f / l_tot;
-  if (qrow < S) {
-    uint16_t* orow = a.o + ((size_t)b * S + qrow) * qstride + (size_t)h * D;
+  uint32_t odd = 0;                // PACKED: the wave's queries whose result is infinite or NaN
+  if constexpr (PACKED) {
+    float z = inv;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) z = __builtin_fmaf(acc_o[dt][r], 0.0f, z);
+    const unsigned long long lanes = __ballot(qrow < S && !__builtin_isfinite(z));
+    odd = (uint32_t)lanes | (uint32_t)(lanes >> 32);
+  }
+  if (qrow < S && !(PACKED && ((odd >> col) & 1))) {
+    uint16_t* orow = a.o + ((size_t)b * S + qrow) * (PACKED ? (size_t)a.os : qstride) + (size_t)h * D;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
 #pragma unroll
@@ -403,11 +518,22 @@ __device__ __forceinline__ void attn_body(const AttnArgs& a) {
       }
     }
   }
+  if constexpr (PACKED) {
+    for (; odd; odd &= odd - 1) {
+      const int i = __builtin_ctz(odd);
+      packed_row<D>(a, qs + i, __builtin_amdgcn_readlane(first_row, i), h, g);
+    }
+  }
 }
 
 template <int D, bool CAUSAL, bool SPLIT>
 __global__ __launch_bounds__(kAttnThreads, 2) void attn_fwd_kernel(AttnArgs a) {
   attn_body<D, CAUSAL, SPLIT>(a);
+}
+
+template <int D, bool SPLIT>
+__global__ __launch_bounds__(kAttnThreads, 2) void attn_packed_kernel(AttnArgs a) {
+  attn_body<D, true, SPLIT, true>(a);
 }
 
 }  // namespace qg

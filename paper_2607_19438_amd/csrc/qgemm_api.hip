@@ -13,6 +13,7 @@
 #include <vector>
 
 #include "../../include/qgemm.h"
+#include "api_util.hpp"
 #include "qgemm_kernels.hpp"
 #include "qgemm_aux.hpp"
 #include "qgemm_smallm.hpp"
@@ -26,9 +27,9 @@
 // hipGetSymbolAddress.
 static __device__ __align__(256) int32_t scratch[(1 << 18) + (1 << 18) + 64];
 
-namespace {
+namespace qg {
 
-thread_local std::string g_last_error;
+static thread_local std::string g_last_error;
 
 int fail(int code, const char* fmt, ...) {
   char buf[512];
@@ -45,13 +46,20 @@ int ok() {
   return QGEMM_OK;
 }
 
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
 int check_launch(const char* what) {
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return fail(QGEMM_EHIP, "%s: kernel launch failed: %s", what, hipGetErrorString(e));
   return QGEMM_OK;
 }
+
+}  // namespace qg
+
+namespace {
+
+using qg::aligned16;
+using qg::check_launch;
+using qg::fail;
+using qg::ok;
 
 int check_common(int N, int K, int fmt) {
   if (fmt != QGEMM_Q8 && fmt != QGEMM_Q4) return fail(QGEMM_EINVAL, "unknown weight format %d", fmt);
@@ -398,7 +406,7 @@ extern "C" {
 
 int qgemm_version(void) { return (1 << 16) | 0; }
 
-const char* qgemm_last_error(void) { return g_last_error.c_str(); }
+const char* qgemm_last_error(void) { return qg::g_last_error.c_str(); }
 
 int qgemm_dense(const void* x, const void* wq, const void* scales, float* y, int M, int N, int K, int fmt,
                 hipStream_t stream) {

@@ -1,0 +1,208 @@
+"""GPU: ``attention_kv4`` against the fp64 oracle on the values that the cache's bytes stand for. Bar: the oracle's
+``attn_tolerance`` (2^-7 sum_j p_j |v_j| for the weights' rounding to bf16, 2^-8 |o| for the output's); the
+unpacked keys and values are exact in bf16."""
+import numpy as np
+import pytest
+
+import oracle
+from gpu_util import torch_or_skip
+from serve_util import bf16, dev_bf16, dev_i32, host_bf16, random_cache, starts, tables
+
+pytestmark = pytest.mark.gpu
+
+
+def q():
+    import paper_2607_19438_amd as m
+    return m
+
+
+def make(kv, new, H, Hkv, D, page, seed=0, pad=0, std=1.0, width=None):
+    rng = np.random.default_rng(seed)
+    table, pages = tables(rng, kv, page, width=width)
+    cache, k, v = random_cache(rng, pages, Hkv, D, page)
+    qn, bits = bf16(rng.standard_normal((int(sum(new)) + pad, H, D)) * std)
+    return table, cache, k, v, qn, bits, starts(new)
+
+
+def run(torch, case, kv, cu, scale=None, out=None):
+    table, cache, _, _, _, bits, _ = case
+    return q().attention_kv4(dev_bf16(torch, bits), torch.from_numpy(cache).cuda(), dev_i32(torch, table), dev_i32(torch, kv),
+                             None if cu is None else dev_i32(torch, cu), scale, out=out)
+
+
+def check(torch, kv, new, H, Hkv, D, page, seed=0, pad=0, std=1.0, rows=None, width=None):
+    case = make(kv, new, H, Hkv, D, page, seed, pad, std, width)
+    table, cache, k, v, qn, bits, cu = case
+    out = torch.full(qn.shape, 9.0, dtype=torch.bfloat16, device="cuda")
+    run(torch, case, kv, None if list(new) == [1] * len(new) and not pad else cu, out=out)
+    got = host_bf16(torch, out)
+    assert np.all(got[cu[-1]:] == 9.0)                       # rows of no request
+    scale = D ** -0.5
+    if rows is None:
+        ref, absv = oracle.cached_attention(qn, k, v, table, kv, cu, page, scale)
+        sel = np.arange(cu[-1])
+    else:
+        ref, absv, sel = np.zeros(qn.shape), np.zeros(qn.shape), np.array(rows)
+        for t in rows:
+            r = int(np.searchsorted(cu, t, side="right") - 1)
+            seen = int(kv[r]) - int(cu[r + 1] - 1 - t)
+            kk, vv = oracle.gather_cache(k, v, table[r], seen, page)
+            for h in range(H):
+                g = h // (H // Hkv)
+                s = kk[:, g] @ qn[t, h] * scale
+                p = np.exp(s - s.max())
+                p /= p.sum()
+                ref[t, h], absv[t, h] = p @ vv[:, g], p @ np.abs(vv[:, g])
+    worst = oracle.attn_ratio(got[sel], ref[sel], absv[sel])
+    print(f"[parity] kv4 {list(kv)[:6]} x {list(new)[:6]} {H}/{Hkv}x{D} page {page}: max |err| / bar = {worst:.3f}", flush=True)
+    assert worst <= 1.0
+    return out
+
+
+DECODE = [  # kv lengths, H, Hkv, D, page
+    ([1], 1, 1, 64, 16), ([1], 8, 2, 128, 16), ([2, 15, 16, 17], 4, 1, 128, 16), ([31, 32, 33, 127, 128, 129], 4, 4, 64, 32),
+    ([300], 6, 2, 128, 64), ([1000, 1, 40], 16, 1, 128, 16), ([129, 513, 257], 32, 4, 64, 128), ([5] * 70, 2, 1, 64, 16),
+    ([700], 40, 2, 128, 16), ([90, 1, 260], 66, 1, 64, 256), ([1025], 3, 1, 128, 1024),
+]
+
+
+@pytest.mark.parametrize("kv,H,Hkv,D,page", DECODE)
+def test_single_tokens(kv, H, Hkv, D, page):
+    check(torch_or_skip(), kv, [1] * len(kv), H, Hkv, D, page, seed=len(kv) + D)
+
+
+SEVERAL = [  # kv lengths, new tokens, H, Hkv, D, page, rows behind
+    ([5], [5], 2, 1, 64, 16, 0), ([40, 9], [3, 9], 4, 2, 128, 16, 2), ([100, 200, 33], [4, 0, 33], 8, 2, 64, 32, 0),
+    ([260, 130], [17, 130], 2, 1, 128, 64, 0), ([129, 1, 64], [6, 1, 2], 12, 4, 128, 16, 5), ([300], [70], 4, 1, 64, 16, 0),
+    ([0, 7, 0], [0, 1, 0], 2, 2, 128, 16, 3), ([600, 20], [9, 20], 16, 2, 64, 128, 0),
+]
+
+
+@pytest.mark.parametrize("kv,new,H,Hkv,D,page,pad", SEVERAL)
+def test_several_tokens(kv, new, H, Hkv, D, page, pad):
+    check(torch_or_skip(), kv, new, H, Hkv, D, page, seed=sum(new), pad=pad)
+
+
+def test_rows_that_see_nothing_are_zero():
+    """No key at all, and more new tokens than keys (the first ones are before the cache's start)."""
+    torch = torch_or_skip()
+    out = check(torch, [0, 3, 0, 40], [1, 5, 2, 1], 4, 2, 128, 16, seed=2)
+    assert torch.all(out[0] == 0) and torch.all(out[1:3] == 0) and torch.all(out[6:8] == 0)
+    out = check(torch, [0, 0], [1, 1], 2, 1, 64, 16, seed=3)
+    assert torch.all(out == 0)
+
+
+@pytest.mark.parametrize("D,page", [(128, 16), (64, 64)])
+def test_long_and_short_together(D, page):
+    """A cache long enough to be split over most workgroups, beside short ones: sampled rows."""
+    torch = torch_or_skip()
+    kv = [20000, 3, 700, 1, 5000, 64]
+    check(torch, kv, [1] * 6, 16, 2, D, page, seed=7, rows=range(6))
+    check(torch, kv, [4, 2, 5, 1, 3, 6], 16, 2, D, page, seed=8, rows=[0, 3, 4, 5, 6, 10, 11, 12, 14, 20])
+
+
+@pytest.mark.parametrize("std", [4.0, 16.0])
+def test_sharp(std):
+    check(torch_or_skip(), [500, 77], [1, 1], 8, 2, 128, 16, seed=5, std=std)
+
+
+def test_many_requests():
+    """More requests than a workgroup has threads."""
+    torch = torch_or_skip()
+    rng = np.random.default_rng(10)
+    kv = rng.integers(0, 60, 700)
+    new = np.minimum(kv, rng.integers(0, 3, 700))
+    check(torch, kv, [int(n) for n in new], 2, 1, 64, 16, seed=10)
+
+
+def test_what_pages_hold_behind_a_row_reaches_nothing():
+    """Slots behind a request's last key and spare pages full of NaN, table entries behind its pages of any value:
+    the bits of a clean cache. And a NaN key or value of a later token leaves the rows before it alone."""
+    torch = torch_or_skip()
+    kv, new, H, Hkv, D, page = [37, 5, 130], [4, 5, 1], 4, 2, 128, 16
+    case = make(kv, new, H, Hkv, D, page, seed=12)
+    table, cache, k, v, qn, bits, cu = case
+    clean = run(torch, case, kv, cu)
+    used = np.zeros(len(cache) * page, bool)
+    for r, n in enumerate(kv):
+        for p in range(n):
+            used[table[r, p // page] * page + p % page] = True
+    dirty = cache.copy()
+    n0 = page * D
+    for s in np.nonzero(~used)[0]:
+        p, o = divmod(int(s), page)
+        for which in range(2):
+            dirty[p, :, n0 + (which * page + o) * 4:n0 + (which * page + o) * 4 + 4] = 255
+    wild = table.copy()
+    wild[table < 0] = [-2 ** 31, 2 ** 31 - 1, 10 ** 6, -1][: 1] * int((table < 0).sum())
+    o = run(torch, (wild, dirty, k, v, qn, bits, cu), kv, cu)
+    assert torch.equal(o, clean)
+    # request 0, its last token (position 36): NaN key; request 1, position 3: NaN values in one block of 32
+    s0 = int(table[0, 36 // page] * page + 36 % page)
+    s1 = int(table[1, 0] * page + 3)
+    dirty[s0 // page, :, n0 + (s0 % page) * 4 + 1] = 255
+    dirty[s1 // page, :, n0 + (page + s1 % page) * 4 + 2] = 255
+    o = run(torch, (wild, dirty, k, v, qn, bits, cu), kv, cu).float()
+    c = clean.float()
+    assert torch.equal(o[:3], c[:3]) and torch.isnan(o[3]).all()
+    assert torch.equal(o[4:7], c[4:7])
+    assert torch.isnan(o[7:9, :, 64:96]).all()
+    keep = [i for i in range(128) if not 64 <= i < 96]
+    assert torch.equal(o[7:9][..., keep], c[7:9][..., keep]) and torch.equal(o[9], c[9])
+
+
+def test_missing_pages_are_nan():
+    torch = torch_or_skip()
+    kv, H, Hkv, D, page = [40, 40, 200, 20], 4, 1, 64, 16
+    case = make(kv, [1] * 4, H, Hkv, D, page, seed=13, width=13)
+    table, cache, *_ = case
+    table[1, 1] = len(cache)                       # one past the pool
+    table[2, 7] = -1
+    o = run(torch, case, kv, None).float()
+    assert torch.isfinite(o[0]).all() and torch.isnan(o[1]).all() and torch.isnan(o[2]).all() and torch.isfinite(o[3]).all()
+    o = run(torch, case, [40, 16, 112, 209], None).float()        # not needed; the table of 13 pages holds 208 keys
+    assert torch.isfinite(o[:3]).all() and torch.isnan(o[3]).all()
+    o = run(torch, case, [40, -5, 2 ** 31 - 1, 1], None).float()
+    assert torch.isfinite(o[0]).all() and torch.all(o[1] == 0) and torch.isnan(o[2]).all() and torch.isfinite(o[3]).all()
+
+
+def test_inconsistent_first_rows_stay_in_bounds():
+    torch = torch_or_skip()
+    case = make([40, 9, 33], [3, 4, 2], 4, 2, 64, 16, seed=14)
+    buf = torch.full((9 + 64, 4, 64), 9.0, dtype=torch.bfloat16, device="cuda")
+    for cu in ([0, 100, 50, 9], [-5, 3, 2 ** 31 - 1, 9], [9, 9, 0, 4], [-1, -1, -1, -1]):
+        run(torch, case, [40, 9, 33], cu, out=buf[32:41])
+        torch.cuda.synchronize()
+        assert torch.all(buf[:32] == 9) and torch.all(buf[41:] == 9)
+
+
+def test_strided_queries_same_bits_every_time():
+    torch = torch_or_skip()
+    m = q()
+    kv = [3000, 40, 1, 777]
+    case = make(kv, [2, 1, 1, 3], 8, 2, 128, 16, seed=15)
+    table, cache, _, _, _, bits, cu = case
+    o = run(torch, case, kv, cu)
+    wide = torch.zeros((7, 12, 128), dtype=torch.bfloat16, device="cuda")
+    wide[:, :8] = dev_bf16(torch, bits)
+    args = (torch.from_numpy(cache).cuda(), dev_i32(torch, table), dev_i32(torch, kv), dev_i32(torch, cu))
+    for _ in range(3):
+        assert torch.equal(m.attention_kv4(wide[:, :8], *args), o)
+
+
+def test_cache_past_32_bits():
+    """Pages whose byte offsets pass 2^32."""
+    torch = torch_or_skip()
+    m = q()
+    pages = (5 << 30) // (2 * 16 * 136)
+    big = torch.empty(m.kv4_cache_shape(pages, 2, 128, 16), dtype=torch.uint8, device="cuda")
+    rng = np.random.default_rng(16)
+    small, k, v = random_cache(rng, 5, 2, 128, 16)
+    at = [pages - 1, 3, pages - 2, pages // 2, pages - 7]
+    for i, p in enumerate(at):
+        big[p] = torch.from_numpy(small[i]).cuda()
+    qn, bits = bf16(rng.standard_normal((1, 4, 128)))
+    o = m.attention_kv4(dev_bf16(torch, bits), big, dev_i32(torch, [at]), dev_i32(torch, [77]))
+    ref, absv = oracle.cached_attention(qn, k, v, [[0, 1, 2, 3, 4]], [77], [0, 1], 16, 128 ** -0.5)
+    assert oracle.attn_ratio(host_bf16(torch, o), ref, absv) <= 1.0
+    del big
