@@ -35,6 +35,7 @@ int check_cache(int Hkv, int D, int pages, int page) {
   if (D != 64 && D != 128) return fail(QGEMM_EUNSUPPORTED, "head dimension must be 64 or 128 (got %d)", D);
   if (!good_page(page)) return fail(QGEMM_EINVAL, "page must be a power of two in [16, 1024] (got %d)", page);
   if (pages < 1) return fail(QGEMM_EINVAL, "pages must be >= 1 (got %d)", pages);
+  if ((long)Hkv * page * (D + D / 16) > 0x7fffffffL) return fail(QGEMM_EUNSUPPORTED, "a page of all heads spans 2 GiB or more");
   if ((long)pages * page > 0x7fffffffL) return fail(QGEMM_EUNSUPPORTED, "the cache has 2^31 or more slots");
   return QGEMM_OK;
 }
@@ -63,7 +64,7 @@ int check_rows(const char* name, const void* p, int64_t stride, int64_t row, int
 // attention over the cache: how many workgroups, and how many rows in a tile
 // ---------------------------------------------------------------------------
 
-constexpr long kKv4MaxGroups = 1024;      // four workgroups on each of 256 CUs
+constexpr long kCUs = 256;
 
 struct Kv4Plan {
   int nt;             // 16-row tiles that share a pass over the keys
@@ -78,13 +79,16 @@ Kv4Plan kv4_plan(int T, int R, int H, int Hkv, int D, int W, int page) {
   p.nt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
   const long tiles = ((long)T * G) / (16 * p.nt) + R;   // at least their number, requests of no tokens aside
   const long grans = std::max<long>(1, qg::ceil_div((long)W * page, qg::kKv4Granule));
-  const long most = std::min<long>(tiles, kKv4MaxGroups) * std::min<long>(Hkv, kKv4MaxGroups) * std::min<long>(grans, kKv4MaxGroups);
-  p.groups = (int)std::min<long>(kKv4MaxGroups, most);
+  // as many workgroups as the CUs hold at once, or fewer if there are not so many granules
+  const long fill = kCUs * (p.nt == 1 ? (D == 128 ? qg::kKv4PerCU<128, 1> : qg::kKv4PerCU<64, 1>)
+                                      : p.nt == 2 ? qg::kKv4PerCU<128, 2> : qg::kKv4PerCU<128, 4>);
+  const long most = std::min(tiles, fill) * std::min<long>(Hkv, fill) * std::min(grans, fill);
+  p.groups = (int)std::min(fill, most);
   p.part_floats = 16L * p.nt * (D + 2);
   return p;
 }
 
-long kv4_workspace_bytes(const Kv4Plan& p) { return p.groups * ((long)sizeof(int4) + 2 * p.part_floats * (long)sizeof(float)); }
+long kv4_workspace_bytes(const Kv4Plan& p) { return p.groups * ((long)sizeof(qg::Kv4Head) + 2 * p.part_floats * (long)sizeof(float)); }
 
 int check_kv4(int T, int R, int H, int Hkv, int D, int W, int page) {
   int rc = check_heads(H, Hkv);
@@ -95,6 +99,10 @@ int check_kv4(int T, int R, int H, int Hkv, int D, int W, int page) {
   if ((long)T * H * D > 0x7fffffffL) return fail(QGEMM_EUNSUPPORTED, "T*H*D must be below 2^31");
   if ((long)W * page > (1 << 30)) return fail(QGEMM_EUNSUPPORTED, "W*page must be at most 2^30");
   if (R > (1 << 20)) return fail(QGEMM_EUNSUPPORTED, "more than 2^20 requests");
+  // the kernel counts (16-row tile, key/value head, 128 keys) of all requests in 32 bits
+  const double grans = (double)std::max<long>(1, qg::ceil_div((long)W * page, qg::kKv4Granule)) + qg::kKv4Start;
+  if ((double)((long)T * (H / Hkv) / 16 + R) * Hkv * grans >= 2147483648.0)
+    return fail(QGEMM_EUNSUPPORTED, "T, R, Hkv and W*page are too large together");
   return QGEMM_OK;
 }
 
@@ -103,7 +111,8 @@ int launch_kv4(const qg::Kv4Args& a, bool join, hipStream_t s) {
   hipLaunchKernelGGL((qg::kv4_attn_kernel<D, NT>), dim3((unsigned)a.nwg), dim3(qg::kKv4Threads), 0, s, a);
   int rc = check_launch("qgemm_attention_kv4");
   if (rc != QGEMM_OK || !join) return rc;
-  hipLaunchKernelGGL((qg::kv4_join_kernel<D, NT>), dim3((unsigned)a.nwg), dim3(qg::kKv4Threads), 0, s, a);
+  hipLaunchKernelGGL((qg::kv4_join_kernel<D, NT>), dim3((unsigned)a.nwg, 16 * NT / qg::kKv4JoinRows),
+                     dim3(64 * qg::kKv4JoinRows), 0, s, a);
   return check_launch("qgemm_attention_kv4 (join)");
 }
 
@@ -359,7 +368,7 @@ int qgemm_attention_kv4(const void* q, const void* cache, const int32_t* block_t
   a.kv_len = kv_len;
   a.cu = cu_q;
   a.o = static_cast<uint16_t*>(o);
-  a.head = static_cast<int4*>(workspace);
+  a.head = static_cast<qg::Kv4Head*>(workspace);
   a.part = reinterpret_cast<float*>(a.head + plan.groups);
   a.T = T;
   a.R = R;

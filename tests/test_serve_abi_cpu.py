@@ -110,7 +110,8 @@ def test_attention_kv4_refusals(m):
     assert g(8, 2, 4, 3, 64, 4, 16, ctypes.byref(n)) == -1 and g(8, 2, 4, 2, 80, 4, 16, ctypes.byref(n)) == -3
     assert g(0, 2, 4, 2, 64, 4, 16, ctypes.byref(n)) == 0 and n.value == 0
     assert g(8, 2, 4, 2, 64, 4, 16, ctypes.byref(n)) == 0 and 0 < n.value < 1 << 20
-    assert g(1 << 16, 1 << 20, 16, 2, 128, 1 << 16, 16, ctypes.byref(n)) == 0 and 0 < n.value < 1 << 27
+    assert g(1 << 16, 1 << 12, 16, 2, 128, 1 << 16, 16, ctypes.byref(n)) == 0 and 0 < n.value < 1 << 27
+    assert g(1 << 16, 1 << 20, 16, 2, 128, 1 << 16, 16, ctypes.byref(n)) == -3 and "together" in m.last_error()
 
 
 SCALED = [("none", {}), ("linear", {"factor": 4.0}), ("llama3", {"factor": 8.0, "low": 1.0, "high": 4.0, "length": 8192.0}),
