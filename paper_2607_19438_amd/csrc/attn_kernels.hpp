@@ -70,50 +70,70 @@ __device__ __forceinline__ float other_half(float x) {
   return __builtin_bit_cast(float, (unsigned)(lane < 32 ? r[1] : r[0]));
 }
 
-// First rows of the prompts that the BQ packed rows from q0 on belong to, written to starts[BQ] (LDS). The last
-// prompt that starts at or before q0 is found with a step per factor of kAttnThreads in R; those that start
-// inside the tile mark their row, and a running maximum spreads the marks. Rows before cu[0] or behind cu[R],
-// and tables that do not ascend, give some row in [0, i] for row i.
+// First rows of the prompts that the packed rows from q0 on belong to. Two steps, so that what has to be done
+// between them can overlap the loads: find() searches cu with a factor of kAttnThreads per round for the last
+// prompt that starts at or before q0, and the prompts that start inside the tile mark their row in LDS; after a
+// barrier, scan() spreads the marks with a running maximum, in every wave by itself. Rows before cu[0] or behind
+// cu[R], and tables that do not ascend, give some row in [0, i] for row i.
 template <int BQ>
-__device__ __forceinline__ void packed_starts(const AttnArgs& a, int q0, int* starts) {
-  const int tid = threadIdx.x;
-  int lo = 0, n = a.R + 1;             // entries lo .. lo + n - 1; entry lo is at or before q0 (taken as row 0 at lo = 0)
-  while (n > 1) {
-    const int step = (n + kAttnThreads - 1) / kAttnThreads;
-    const int at = tid * step;
-    const int c = __syncthreads_count(at < n && a.cu[lo + at] <= q0);
-    const int to = max(c - 1, 0) * step;
-    lo += to;
-    n = step > 1 ? min(step, n - to) : 1;
+struct PackedStarts {
+  static constexpr int PER = BQ / 64;
+  int v[PER];                          // of rows PER lane .. PER lane + PER - 1 of the tile
+
+  static __device__ __forceinline__ void find(const AttnArgs& a, int q0, int* marks) {
+    const int tid = threadIdx.x;
+    if (tid < BQ) marks[tid] = 0;
+    int lo = 0, n = a.R + 1;           // entries lo .. lo + n - 1; lo is at or before q0, or the first of all
+    while (n > kAttnThreads) {
+      const int step = (n + kAttnThreads - 1) / kAttnThreads;
+      const int at = tid * step;
+      const int c = __syncthreads_count(at < n && a.cu[lo + at] <= q0);
+      const int to = max(c - 1, 0) * step;
+      lo += to;
+      n = min(step, n - to);
+    }
+    int v = tid < n ? a.cu[lo + tid] : 0x7fffffff;
+    const int c = __syncthreads_count(v <= q0);
+    if (tid == max(c - 1, 0)) marks[0] = min(max(v, 0), q0);
+    for (int e = lo + n;; e += kAttnThreads) {
+      if (v > q0 && v < q0 + BQ) marks[v - q0] = v;
+      if (e > a.R || !__syncthreads_and(v < q0 + BQ || v == 0x7fffffff)) break;
+      v = e + tid <= a.R ? a.cu[e + tid] : 0x7fffffff;
+    }
   }
-  if (tid < BQ) starts[tid] = tid == 0 ? min(max(a.cu[lo], 0), q0) : 0;
-  __syncthreads();
-  for (int e = lo + 1;; e += kAttnThreads) {
-    const int v = e + tid <= a.R ? a.cu[e + tid] : 0x7fffffff;
-    if (v > q0 && v < q0 + BQ) starts[v - q0] = v;
-    if (!__syncthreads_and(v < q0 + BQ)) break;
-  }
-  if (tid < 64) {
-    constexpr int PER = BQ / 64;
-    int v[PER], top = 0;
+
+  __device__ __forceinline__ void scan(const int* marks) {
+    const int lane = threadIdx.x & 63;
+    int top = 0;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) v[i] = top = max(top, starts[tid * PER + i]);
+    for (int i = 0; i < PER; ++i) v[i] = top = max(top, marks[lane * PER + i]);
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
       const int up = __shfl_up(top, d);
-      if (tid >= d) top = max(top, up);
+      if (lane >= d) top = max(top, up);
     }
     const int before = __shfl_up(top, 1);
 #pragma unroll
-    for (int i = 0; i < PER; ++i) starts[tid * PER + i] = tid > 0 ? max(v[i], before) : v[i];
+    for (int i = 0; i < PER; ++i) v[i] = lane > 0 ? max(v[i], before) : v[i];
   }
-  __syncthreads();
-}
+
+  // of row `at` of the tile
+  __device__ __forceinline__ int of(int at) const {
+    int r = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int x = __shfl(v[i], at / PER);
+      if (at % PER == i) r = x;
+    }
+    return r;
+  }
+};
 
 // One packed row by itself, by a whole wave: o = sum_j softmax(scale q.k)_j v_j over the keys j0 .. row. For rows
 // whose result is not finite: in the tiles a weight of 0 times another prompt's infinite or NaN value is NaN.
+// (Inlined: a call gives the kernel a stack, which costs each launch 4 us.)
 template <int D>
-__device__ __noinline__ void packed_row(const AttnArgs& a, int row, int j0, int h, int g) {
+__device__ __forceinline__ void packed_row(const AttnArgs& a, int row, int j0, int h, int g) {
   const int lane = threadIdx.x & 63;
   const uint16_t* q = a.q + (size_t)row * a.qs + (size_t)h * D;
   auto f = [](uint16_t b) { return __builtin_bit_cast(float, (uint32_t)b << 16); };
@@ -170,9 +190,9 @@ __device__ __forceinline__ void attn_body(const AttnArgs& a) {
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 31;     // this lane's query within the wave (MFMA column)
   const int hh = lane >> 5;      // MFMA lane half
-  const int S = PACKED ? min(max(a.cu[a.R], 0), a.S) : a.S;
+  int S = a.S;                   // PACKED: up to the last prompt's end, below
   const int H = a.H;
-  const int nqb = ((PACKED ? a.S : S) + BQ - 1) / BQ;
+  const int nqb = (S + BQ - 1) / BQ;
   int bh, qb;
   if (CAUSAL && (SPLIT || PACKED)) {
     // the heaviest query blocks of all heads first, so that light ones fill in. Workgroups reach the 8
@@ -217,29 +237,33 @@ __device__ __forceinline__ void attn_body(const AttnArgs& a) {
   int first_row = 0;             // PACKED: first key that this lane's query sees,
   int wave_lo = 0, wave_hi = 0;  // and those of the wave's first and last query
   int kb0 = 0;                   // first key block
-  if constexpr (PACKED) {
-    __shared__ int starts[BQ];
-    if (q0 >= S) return;
-    packed_starts<BQ>(a, q0, starts);
-    first_row = starts[qrow - q0];
-    wave_lo = __builtin_amdgcn_readfirstlane(starts[qs - q0]);
-    wave_hi = __builtin_amdgcn_readfirstlane(starts[qs + 31 - q0]);
-    kb0 = __builtin_amdgcn_readfirstlane(starts[0]) / kAttnBK;
-  }
-  const __amdgpu_buffer_rsrc_t qr = make_rsrc(a.q + (size_t)b * S * qstride + (size_t)h * D,
-                                              (uint32_t)(((size_t)(S - 1) * qstride + D) * 2));
-  const __amdgpu_buffer_rsrc_t kr = make_rsrc(a.k + (size_t)b * S * kstride + (size_t)g * D,
-                                              (uint32_t)(((size_t)(S - 1) * kstride + D) * 2));
-  const __amdgpu_buffer_rsrc_t vr = make_rsrc(a.v + (size_t)b * S * vstride + (size_t)g * D,
-                                              (uint32_t)(((size_t)(S - 1) * vstride + D) * 2));
-
+  const __amdgpu_buffer_rsrc_t qr = make_rsrc(a.q + (size_t)b * a.S * qstride + (size_t)h * D,
+                                              (uint32_t)(((size_t)(a.S - 1) * qstride + D) * 2));
   // query fragments (B operand of K Q^T): step t needs q[qrow][16t + 8hh .. +8]
   bf16x8 qf[KSTEPS];
 #pragma unroll
   for (int t = 0; t < KSTEPS; ++t) {
-    const uint32_t off = qrow < S ? ((uint32_t)qrow * (uint32_t)qstride + 16u * t + 8u * hh) * 2u : kOOB;
+    const uint32_t off = qrow < a.S ? ((uint32_t)qrow * (uint32_t)qstride + 16u * t + 8u * hh) * 2u : kOOB;
     qf[t] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(qr, off, 0, 0));
   }
+
+  if constexpr (PACKED) {        // (the queries above are in flight meanwhile)
+    __shared__ int marks[BQ];
+    PackedStarts<BQ> starts;
+    starts.find(a, q0, marks);
+    S = min(max(a.cu[a.R], 0), a.S);
+    __syncthreads();
+    if (q0 >= S) return;
+    starts.scan(marks);
+    first_row = starts.of(qrow - q0);
+    wave_lo = __builtin_amdgcn_readfirstlane(starts.of(qs - q0));
+    wave_hi = __builtin_amdgcn_readfirstlane(starts.of(qs + 31 - q0));
+    kb0 = __builtin_amdgcn_readfirstlane(starts.v[0]) / kAttnBK;
+  }
+  const __amdgpu_buffer_rsrc_t kr = make_rsrc(a.k + (size_t)b * S * kstride + (size_t)g * D,
+                                              (uint32_t)(((size_t)(S - 1) * kstride + D) * 2));
+  const __amdgpu_buffer_rsrc_t vr = make_rsrc(a.v + (size_t)b * S * vstride + (size_t)g * D,
+                                              (uint32_t)(((size_t)(S - 1) * vstride + D) * 2));
 
   // 16-byte chunk swizzle of a key row in LDS: any 16 consecutive keys read at one logical chunk
   // hit 16 distinct bank groups, and any 8 hit 8 distinct 16-byte groups of a 128-byte bank

@@ -219,4 +219,23 @@ inline bool attn_split(bool d64, bool causal, long S, long heads) {
   return (S > 128 && S <= 160) || (S > 192 && (even || S > 600 || narrow <= 400));
 }
 
+// The same choice for R packed prompts of T rows in all (their lengths are not known here): 64-row workgroups while
+// the 128-row ones are few for the CUs, 2 of which a CU holds at D = 128 and 3 at D = 64. How few depends on how
+// uneven the chains are: with one or two prompts the longest is as long as T, or half of it, and decides; with
+// many of them all are short and the total does. Time of the 64-row form over that of the 128-row one, prompts of
+// one length, by the number of 128-row workgroups:
+//   D=128  R = 1    192 0.70  384 0.73  576 0.72-0.80  768 0.88-1.16  1024 1.20
+//          R = 3    256 0.86  384 0.97 (16 heads 0.72)  512 0.94  576 1.02  1024 0.98  1504 0.97-1.10
+//          R = 8    192 0.95 (8 heads 0.87)  256 0.93  288 0.94-1.09  384 1.05  576 1.03  1024 1.13
+//          R = 200  128 0.77  192 0.87  256 0.89  264 1.06  384 1.13  768 1.08
+//   D=64   R = 1    384 0.73  576 0.72  768 0.72 (24 heads 1.07)  1024 1.12  1504 0.98-1.11
+//          R = 3    384 0.80  576 0.83  768 0.83-0.89  1024 0.95  1504 0.90-1.08
+//          R = 8    288 0.83  384 0.89  432 0.86  512 1.08  576 1.03  768 1.14
+//          R = 200  256 0.87  352 0.88  384 0.89  432 1.12  576 1.12  1024 1.03
+inline bool attn_packed_split(bool d64, long T, long R, long heads) {
+  const long wide = heads * ceil_div(T, 128);
+  if (d64) return wide <= (R <= 5 ? 768 : 400);
+  return wide <= (R <= 2 ? 640 : R <= 5 ? 512 : 256);
+}
+
 }  // namespace qg
