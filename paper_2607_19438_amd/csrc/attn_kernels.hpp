@@ -247,18 +247,9 @@ __device__ __forceinline__ void attn_body(const AttnArgs& a) {
     qf[t] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(qr, off, 0, 0));
   }
 
-  if constexpr (PACKED) {        // (the queries above are in flight meanwhile)
-    __shared__ int marks[BQ];
-    PackedStarts<BQ> starts;
-    starts.find(a, q0, marks);
-    S = min(max(a.cu[a.R], 0), a.S);
-    __syncthreads();
+  if constexpr (PACKED) {
+    S = min(max(__builtin_amdgcn_readfirstlane(a.cu[a.R]), 0), a.S);
     if (q0 >= S) return;
-    starts.scan(marks);
-    first_row = starts.of(qrow - q0);
-    wave_lo = __builtin_amdgcn_readfirstlane(starts.of(qs - q0));
-    wave_hi = __builtin_amdgcn_readfirstlane(starts.of(qs + 31 - q0));
-    kb0 = __builtin_amdgcn_readfirstlane(starts.v[0]) / kAttnBK;
   }
   const __amdgpu_buffer_rsrc_t kr = make_rsrc(a.k + (size_t)b * S * kstride + (size_t)g * D,
                                               (uint32_t)(((size_t)(S - 1) * kstride + D) * 2));
@@ -323,8 +314,21 @@ __device__ __forceinline__ void attn_body(const AttnArgs& a) {
   float l_run = 0.0f;
   const float sl2 = a.sl2;
 
-  dma_keys(ks0, kb0);
-  dma_values(vt0, kb0);
+  // PACKED: the blocks are walked from the last to the first, as the last does not wait for the prompts' starts
+  const int jb0 = PACKED ? nkb - 1 : 0;
+  dma_keys(ks0, jb0);
+  dma_values(vt0, jb0);
+  if constexpr (PACKED) {
+    __shared__ int marks[BQ];
+    PackedStarts<BQ> starts;
+    starts.find(a, q0, marks);
+    __syncthreads();
+    starts.scan(marks);
+    first_row = starts.of(qrow - q0);
+    wave_lo = __builtin_amdgcn_readfirstlane(starts.of(qs - q0));
+    wave_hi = __builtin_amdgcn_readfirstlane(starts.of(qs + 31 - q0));
+    kb0 = __builtin_amdgcn_readfirstlane(starts.v[0]) / kAttnBK;
+  }
   wait_vmcnt_lgkm0<0>();
   __syncthreads();
 
@@ -361,10 +365,10 @@ __device__ __forceinline__ void attn_body(const AttnArgs& a) {
   // one key block: math on buffer (ksc, vtc) while the next block's keys stream into (ksn, vtn)
   auto step = [&](int jb, const uint16_t* ksc, const uint16_t* vtc, uint16_t* ksn, uint16_t* vtn) {
     const int j0 = jb * kAttnBK;
-    const bool more = jb + 1 < nkb;
-    if (more) {
-      dma_keys(ksn, jb + 1);
-      dma_values(vtn, jb + 1);
+    const int jn = PACKED ? jb - 1 : jb + 1;
+    if (PACKED ? jn >= kb0 : jn < nkb) {
+      dma_keys(ksn, jn);
+      dma_values(vtn, jn);
     }
     const int t0 = j0 + 32 * kh;            // the wave's first key of the block
     // (tiles and waves' queries both start at multiples of 32, so every query of a wave sees at least the
@@ -406,7 +410,9 @@ __device__ __forceinline__ void attn_body(const AttnArgs& a) {
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
             const int kp = t0 + kt * 32 + (r >> 2) * 8 + 4 * hh + (r & 3);
-            if (kp >= S || (CAUSAL && kp > qrow) || (PACKED && kp < first_row)) sc[kt][r] = -__builtin_inff();
+            // (PACKED: from first_row to qrow, which lies below S where it counts)
+            if (PACKED ? (unsigned)(kp - first_row) > (unsigned)(qrow - first_row) : kp >= S || (CAUSAL && kp > qrow))
+              sc[kt][r] = -__builtin_inff();
           }
       }
       float mloc = -__builtin_inff();
@@ -433,7 +439,7 @@ __device__ __forceinline__ void attn_body(const AttnArgs& a) {
       // per key tile: registers (2i, 2i+1). The second half's exponentials (SPLIT: of the tile's
       // registers, else tile 1's) are written between the first output-product MFMAs so the two overlap.
       // SPLIT: a half whose keys so far all score -inf (keys with infinities) keeps maximum -inf, weights 0;
-      // PACKED: so does a row whose prompt begins behind the keys so far
+      // PACKED: so does a row that has met keys behind it or of other prompts only
       const float ms = ((SPLIT || PACKED) && m_run == -__builtin_inff()) ? 0.0f : m_run * sl2;
       float lsum = 0.0f;
       uint32_t pf[NT][8];
@@ -478,9 +484,16 @@ __device__ __forceinline__ void attn_body(const AttnArgs& a) {
     __syncthreads();
   };
 
-  for (int jb = kb0; jb < nkb; jb += 2) {
-    step(jb, ks0, vt0, ks1, vt1);
-    if (jb + 1 < nkb) step(jb + 1, ks1, vt1, ks0, vt0);
+  if constexpr (PACKED) {
+    for (int jb = jb0; jb >= kb0; jb -= 2) {
+      step(jb, ks0, vt0, ks1, vt1);
+      if (jb > kb0) step(jb - 1, ks1, vt1, ks0, vt0);
+    }
+  } else {
+    for (int jb = 0; jb < nkb; jb += 2) {
+      step(jb, ks0, vt0, ks1, vt1);
+      if (jb + 1 < nkb) step(jb + 1, ks1, vt1, ks0, vt0);
+    }
   }
 
   if constexpr (SPLIT) {

@@ -106,7 +106,7 @@ def test_one_prompt_equals_attention_prefill():
         assert np.all(np.abs(o - p) <= 2 * oracle.attn_tolerance(ref, absv))
 
 
-@pytest.mark.parametrize("H", [1, 32])
+@pytest.mark.parametrize("H", [1, 32, 128])
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
 def test_prompts_do_not_touch_each_other(bad, H):
     """Infinite and NaN queries, keys and values of one prompt (and of rows of none) reach no other prompt's rows,
