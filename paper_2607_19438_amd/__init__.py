@@ -388,36 +388,48 @@ def attention_prefill(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal:
 
 _I32 = (torch.int32,)
 _BF16 = (torch.bfloat16,)
+_F64 = (torch.float64,)
+_ROWS = (torch.float32, torch.bfloat16)
 
 
 def _need_rows(t: torch.Tensor, name: str, dtypes):
-    """A tensor [T][heads][D] whose heads lie end to end; returns the elements between rows."""
+    """A tensor [T][heads][D] whose heads lie end to end; returns its shape and the elements between rows."""
+    if isinstance(t, torch.Tensor) and t.is_cuda and t.dtype in dtypes and t.dim() == 3:
+        T, h, D = n = t.shape
+        s0, s1, s2 = t.stride()
+        if (s2 == 1 or D <= 1) and (s1 == D or h <= 1):
+            return n, s0 if T > 1 else h * D
+        raise ValueError(f"the heads of a row of {name} must be contiguous")
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
     if not t.is_cuda:
         raise ValueError(f"{name} must be a GPU tensor")
     if t.dtype not in dtypes:
         raise TypeError(f"{name} has dtype {t.dtype}, expected one of {dtypes}")
-    if t.dim() != 3:
-        raise ValueError(f"{name} must have 3 dimensions")
-    T, h, D = t.shape
-    s = t.stride()
-    if (D > 1 and s[2] != 1) or (h > 1 and s[1] != D):
-        raise ValueError(f"the heads of a row of {name} must be contiguous")
-    return s[0] if T > 1 else h * D
+    raise ValueError(f"{name} must have 3 dimensions")
 
 
-def _enqueue(fn, tensors, *args):
-    """``fn(*args, stream)`` on the current stream of the tensors' device, which they must share."""
-    dev = tensors[0].get_device()
-    for t in tensors:
-        if t is not None and t.get_device() != dev:
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
+def _device(first: torch.Tensor, *others) -> int:
+    """The device that the tensors share."""
+    dev = first.get_device()
+    for t in others:
+        if t.get_device() != dev:
             raise ValueError("the tensors must be on one device")
-    if torch.cuda.current_device() == dev:
-        _check(fn(*args, _stream(tensors[0])))
+    return dev
+
+
+def _enqueue(fn, dev: int, first: torch.Tensor, *args):
+    """``fn(*args, stream)`` on the current stream of device ``dev``, that of ``first``."""
+    if _current_device() == dev:
+        rc = fn(*args, _stream(first))
     else:
         with torch.cuda.device(dev):
-            _check(fn(*args, _stream(tensors[0])))
+            rc = fn(*args, _stream(first))
+    if rc:
+        _check(rc)
 
 
 class KvPlan:
@@ -429,7 +441,7 @@ class KvPlan:
     def __init__(self, R: int, T: int, device):
         # one allocation, as the plan of a small step is all latency
         n = torch.empty(2 * R + 2 + 2 * T, dtype=torch.int32, device=device)
-        self.cu_q, self.kv_len, self.used, self.positions, self.slots = n.split((R + 1, R, 1, T, T))
+        self.cu_q, self.kv_len, self.used, self.positions, self.slots = n.split_with_sizes((R + 1, R, 1, T, T))
 
 
 def kv_plan(kv_len, q_len, block_table, free_pages, page: int, tokens: int, out: KvPlan | None = None) -> KvPlan:
@@ -447,16 +459,18 @@ def kv_plan(kv_len, q_len, block_table, free_pages, page: int, tokens: int, out:
         raise ValueError("kv_len, q_len and block_table disagree on the number of requests")
     if tokens < 0:
         raise ValueError("tokens must be >= 0")
+    dev = _device(kv_len, q_len, block_table, free_pages)
     if out is None:
         out = KvPlan(R, tokens, kv_len.device)
-    for name, n in (("cu_q", R + 1), ("positions", tokens), ("slots", tokens), ("kv_len", R), ("used", 1)):
-        t = getattr(out, name)
-        _need(t, "out." + name, _I32, 1)
-        if t.shape[0] != n:
-            raise ValueError(f"out.{name} must have {n} entries")
-    _enqueue(lib().qgemm_kv_plan, (kv_len, q_len, block_table, free_pages, out.cu_q, out.positions, out.slots, out.kv_len, out.used),
-             kv_len.data_ptr(), q_len.data_ptr(), block_table.data_ptr(), free_pages.data_ptr(), out.cu_q.data_ptr(),
-             out.positions.data_ptr(), out.slots.data_ptr(), out.kv_len.data_ptr(), out.used.data_ptr(), R,
+    else:
+        for name, n in (("cu_q", R + 1), ("positions", tokens), ("slots", tokens), ("kv_len", R), ("used", 1)):
+            t = getattr(out, name)
+            _need(t, "out." + name, _I32, 1)
+            if t.shape[0] != n:
+                raise ValueError(f"out.{name} must have {n} entries")
+        _device(kv_len, out.cu_q, out.positions, out.slots, out.kv_len, out.used)
+    _enqueue(lib().qgemm_kv_plan, dev, kv_len, kv_len.data_ptr(), q_len.data_ptr(), block_table.data_ptr(), free_pages.data_ptr(),
+             out.cu_q.data_ptr(), out.positions.data_ptr(), out.slots.data_ptr(), out.kv_len.data_ptr(), out.used.data_ptr(), R,
              block_table.shape[1], free_pages.shape[0], page, tokens)
     return out
 
@@ -485,20 +499,21 @@ def rope(x: torch.Tensor, positions: torch.Tensor, inv_freq: torch.Tensor, rot_h
     """Rotary positions on the first ``rot_heads`` heads of rows ``x`` [T][heads][D], fp32 or bf16, and their conversion
     to bf16 (``qgemm_rope``). The first ``2 * len(inv_freq)`` elements of a head are rotated, as pairs half of them
     apart or (``interleaved``) neighbouring. ``out``: bf16, may be a bf16 ``x`` itself."""
-    xs = _need_rows(x, "x", (torch.float32, torch.bfloat16))
+    (T, heads, D), xs = _need_rows(x, "x", _ROWS)
     _need(positions, "positions", _I32, 1)
-    _need(inv_freq, "inv_freq", (torch.float64,), 1)
-    T, heads, D = x.shape
+    _need(inv_freq, "inv_freq", _F64, 1)
     if positions.shape[0] != T:
         raise ValueError("x and positions disagree on T")
     if out is None:
         out = torch.empty((T, heads, D), dtype=torch.bfloat16, device=x.device)
-    ys = _need_rows(out, "out", _BF16)
-    if out.shape != x.shape:
-        raise ValueError("out must have the shape of x")
-    _enqueue(lib().qgemm_rope, (x, positions, inv_freq, out), x.data_ptr(), int(x.dtype == torch.bfloat16), positions.data_ptr(),
-             inv_freq.data_ptr(), out.data_ptr(), T, heads, rot_heads, D, 2 * inv_freq.shape[0], xs, ys, int(bool(interleaved)),
-             float(gain))
+        ys = heads * D
+    else:
+        shape, ys = _need_rows(out, "out", _BF16)
+        if shape != (T, heads, D):
+            raise ValueError("out must have the shape of x")
+    _enqueue(lib().qgemm_rope, _device(x, positions, inv_freq, out), x, x.data_ptr(), 1 if x.dtype is torch.bfloat16 else 0,
+             positions.data_ptr(), inv_freq.data_ptr(), out.data_ptr(), T, heads, rot_heads, D, 2 * inv_freq.shape[0], xs, ys,
+             1 if interleaved else 0, gain)
     return out
 
 
@@ -518,15 +533,15 @@ def _cache_sizes(cache: torch.Tensor, D: int):
 def kv4_store(k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, cache: torch.Tensor):
     """Quantises ``k``, ``v`` [T][Hkv][D] bf16 into the cache's ``slots`` [T] (``qgemm_kv4_store``); negative slots are
     skipped. ``cache``: uint8 of ``kv4_cache_shape``."""
-    ks = _need_rows(k, "k", _BF16)
-    vs = _need_rows(v, "v", _BF16)
+    shape, ks = _need_rows(k, "k", _BF16)
+    vshape, vs = _need_rows(v, "v", _BF16)
     _need(slots, "slots", _I32, 1)
-    T, Hkv, D = k.shape
+    T, Hkv, D = shape
     pages, heads, page = _cache_sizes(cache, D)
-    if v.shape != k.shape or heads != Hkv or slots.shape[0] != T:
+    if vshape != shape or heads != Hkv or slots.shape[0] != T:
         raise ValueError("k, v, slots and cache disagree on T, Hkv or D")
-    _enqueue(lib().qgemm_kv4_store, (k, v, slots, cache), k.data_ptr(), v.data_ptr(), slots.data_ptr(), cache.data_ptr(), T, Hkv, D, ks, vs,
-             pages, page)
+    _enqueue(lib().qgemm_kv4_store, _device(k, v, slots, cache), k, k.data_ptr(), v.data_ptr(), slots.data_ptr(), cache.data_ptr(), T, Hkv,
+             D, ks, vs, pages, page)
 
 
 def kv4_load(cache: torch.Tensor, slots: torch.Tensor, D: int, k: torch.Tensor | None = None, v: torch.Tensor | None = None):
@@ -537,14 +552,16 @@ def kv4_load(cache: torch.Tensor, slots: torch.Tensor, D: int, k: torch.Tensor |
     shape = (slots.shape[0], Hkv, D)
     if k is None:
         k = torch.empty(shape, dtype=torch.bfloat16, device=cache.device)
+    else:
+        _need(k, "k", _BF16, 3)
     if v is None:
         v = torch.empty(shape, dtype=torch.bfloat16, device=cache.device)
-    _need(k, "k", _BF16, 3)
-    _need(v, "v", _BF16, 3)
+    else:
+        _need(v, "v", _BF16, 3)
     if k.shape != shape or v.shape != shape:
         raise ValueError("k and v must be [T][Hkv][D]")
-    _enqueue(lib().qgemm_kv4_load, (cache, slots, k, v), cache.data_ptr(), slots.data_ptr(), k.data_ptr(), v.data_ptr(), shape[0], Hkv, D,
-             pages, page)
+    _enqueue(lib().qgemm_kv4_load, _device(cache, slots, k, v), cache, cache.data_ptr(), slots.data_ptr(), k.data_ptr(), v.data_ptr(),
+             shape[0], Hkv, D, pages, page)
     return k, v
 
 
@@ -553,24 +570,25 @@ def attention_packed(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu: torc
     """Causal attention over prompts packed end to end, prompt r in rows ``cu[r] .. cu[r+1]-1``
     (``qgemm_attention_packed``): q ``[T][H][D]``, k / v ``[T][Hkv][D]`` bf16, views of one projection row among
     them -> o ``[T][H][D]`` bf16. Rows behind the last prompt are not written."""
-    qs = _need_rows(q, "q", _BF16)
-    ks = _need_rows(k, "k", _BF16)
-    vs = _need_rows(v, "v", _BF16)
+    shape, qs = _need_rows(q, "q", _BF16)
+    kshape, ks = _need_rows(k, "k", _BF16)
+    vshape, vs = _need_rows(v, "v", _BF16)
     _need(cu, "cu", _I32, 1)
-    T, H, D = q.shape
-    if k.shape != v.shape or k.shape[0] != T or k.shape[2] != D:
+    T, H, D = shape
+    if kshape != vshape or kshape[0] != T or kshape[2] != D:
         raise ValueError("q, k and v disagree on T or D")
-    if cu.shape[0] < 1:
+    R = cu.shape[0] - 1
+    if R < 0:
         raise ValueError("cu must have one entry more than there are prompts")
-    if scale is None:
-        scale = 1.0 / float(D) ** 0.5
     if out is None:
         out = torch.empty((T, H, D), dtype=torch.bfloat16, device=q.device)
-    ys = _need_rows(out, "out", _BF16)
-    if out.shape != q.shape:
-        raise ValueError("out must have the shape of q")
-    _enqueue(lib().qgemm_attention_packed, (q, k, v, cu, out), q.data_ptr(), k.data_ptr(), v.data_ptr(), cu.data_ptr(), out.data_ptr(), T,
-             cu.shape[0] - 1, H, k.shape[1], D, qs, ks, vs, ys, float(scale))
+        ys = H * D
+    else:
+        oshape, ys = _need_rows(out, "out", _BF16)
+        if oshape != shape:
+            raise ValueError("out must have the shape of q")
+    _enqueue(lib().qgemm_attention_packed, _device(q, k, v, cu, out), q, q.data_ptr(), k.data_ptr(), v.data_ptr(), cu.data_ptr(),
+             out.data_ptr(), T, R, H, kshape[1], D, qs, ks, vs, ys, D ** -0.5 if scale is None else scale)
     return out
 
 
@@ -580,10 +598,9 @@ def attention_kv4(q: torch.Tensor, cache: torch.Tensor, block_table: torch.Tenso
     ``[T][H][D]`` bf16. ``kv_len`` [R]: each request's keys, the new tokens' own (stored before) among them;
     ``cu_q`` [R+1]: first rows of the requests, or None where each has one token. Rows behind the last request
     are not written."""
-    qs = _need_rows(q, "q", _BF16)
+    (T, H, D), qs = _need_rows(q, "q", _BF16)
     _need(block_table, "block_table", _I32, 2)
     _need(kv_len, "kv_len", _I32, 1)
-    T, H, D = q.shape
     pages, Hkv, page = _cache_sizes(cache, D)
     R, W = block_table.shape
     if kv_len.shape[0] != R or (cu_q is None and T != R):
@@ -592,20 +609,20 @@ def attention_kv4(q: torch.Tensor, cache: torch.Tensor, block_table: torch.Tenso
         _need(cu_q, "cu_q", _I32, 1)
         if cu_q.shape[0] != R + 1:
             raise ValueError("cu_q must have one entry more than there are requests")
-    if scale is None:
-        scale = 1.0 / float(D) ** 0.5
+        _device(q, cu_q)
     if out is None:
         out = torch.empty((T, H, D), dtype=torch.bfloat16, device=q.device)
-    _need(out, "out", _BF16, 3)
-    if out.shape != q.shape:
-        raise ValueError("out must have the shape of q")
+    else:
+        _need(out, "out", _BF16, 3)
+        if out.shape != q.shape:
+            raise ValueError("out must have the shape of q")
     n = _l(0)
     _check(lib().qgemm_attention_kv4_workspace(T, R, H, Hkv, D, W, page, ctypes.byref(n)))
     # of the call's own: torch's allocator keeps it from other streams, and inside a capture it is the graph's
     ws = torch.empty(n.value, dtype=torch.uint8, device=q.device)
-    _enqueue(lib().qgemm_attention_kv4, (q, cache, block_table, kv_len, cu_q, out), q.data_ptr(), cache.data_ptr(),
+    _enqueue(lib().qgemm_attention_kv4, _device(q, cache, block_table, kv_len, out), q, q.data_ptr(), cache.data_ptr(),
              block_table.data_ptr(), kv_len.data_ptr(), None if cu_q is None else cu_q.data_ptr(), out.data_ptr(),
-             ws.data_ptr(), n.value, T, R, H, Hkv, D, W, pages, page, qs, float(scale))
+             ws.data_ptr(), n.value, T, R, H, Hkv, D, W, pages, page, qs, D ** -0.5 if scale is None else scale)
     return out
 
 

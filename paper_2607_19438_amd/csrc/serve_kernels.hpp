@@ -15,7 +15,7 @@ namespace {
 // ---------------------------------------------------------------------------
 
 constexpr int kPlanThreads = 256;
-constexpr int kPlanTokens = 1024;      // tokens of a workgroup
+constexpr int kPlanTokens = 256;       // tokens of a workgroup
 constexpr int kPlanMaxR = 4096;        // requests: three int32 per request in LDS (48 KiB)
 
 struct PlanArgs {
@@ -171,15 +171,49 @@ __device__ __forceinline__ void store8(uint16_t* p, const float (&v)[8]) {
 // LDS. The angle is taken in turns in fp64 (position x frequency / 2 pi, less its whole turns): at position
 // 10^6 an fp32 product is off by 0.06 radians. What is left is below half a turn, so fp32 keeps 2^-25 of one.
 // WIDE: 16 elements per thread and step, with 16-byte accesses, where sizes, strides and addresses allow it;
-// else two elements.
+// else two elements. (The first step's loads before the sines, and each next step's before the last one's work:
+// 3000 rows of 24 x 64 5.2 -> 5.5 us, 8000 rows 10.0 -> 11.8, 16 rows of 40 x 128 3.1 -> 3.3. The waves are
+// enough to cover them.)
 template <typename TX, bool INTER, bool WIDE>
 __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeArgs a) {
+  constexpr int N = WIDE ? 8 : 1;      // elements of a thread's two pieces
   __shared__ float2 cs[4 * kRopeMaxPairs];
   const int tid = threadIdx.x;
   const int group = blockIdx.x / a.parts, part = blockIdx.x - group * a.parts;
   const int t0 = group * a.tokens;
   const int nt = min(a.tokens, a.T - t0);
   const int pairs = a.rot >> 1;
+  const int units = a.D / (2 * N);                    // of a head
+  const int turned = a.rot / (2 * N);                 // of them rotated, in the heads that are
+  const int per = (a.heads + a.parts - 1) / a.parts;
+  const int h0 = part * per, nh = min(per, a.heads - h0);
+  const int n = nt * nh * units;
+  struct Item {
+    int t, u, o1, o2;      // token, unit, offsets of its two pieces in the head
+    bool rot;
+    size_t head;           // head x D
+    float p[N], q[N];
+  };
+  auto fetch = [&](int i) {
+    Item m;
+    m.u = i % units;
+    const int hu = i / units;
+    const int h = h0 + hu % nh;
+    m.t = hu / nh;
+    m.rot = h < a.rot_heads && m.u < turned;
+    m.o1 = m.rot && !INTER ? N * m.u : 2 * N * m.u;
+    m.o2 = m.rot && !INTER ? N * m.u + pairs : 2 * N * m.u + N;
+    m.head = (size_t)h * a.D;
+    const TX* x = static_cast<const TX*>(a.x) + (size_t)(t0 + m.t) * a.xs + m.head;
+    if constexpr (WIDE) {
+      load8(x + m.o1, m.p);
+      load8(x + m.o2, m.q);
+    } else {
+      m.p[0] = load_one(x + m.o1);
+      m.q[0] = load_one(x + m.o2);
+    }
+    return m;
+  };
   for (int i = tid; i < nt * pairs; i += kRopeThreads) {
     const int t = i / pairs;
     double turn = (double)a.positions[t0 + t] * (a.inv_freq[i - t * pairs] * 0.15915494309189535);
@@ -189,60 +223,38 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeArgs a) {
     cs[i] = make_float2(c * a.gain, s * a.gain);
   }
   __syncthreads();
-  const int units = WIDE ? a.D >> 4 : a.D >> 1;       // of a head
-  const int turned = WIDE ? a.rot >> 4 : pairs;       // of them rotated, in the heads that are
-  const int per = (a.heads + a.parts - 1) / a.parts;
-  const int h0 = part * per, nh = min(per, a.heads - h0);
-  const int n = nt * nh * units;
   for (int i = tid; i < n; i += kRopeThreads) {
-    const int u = i % units, hu = i / units;
-    const int h = h0 + hu % nh, t = hu / nh;
-    const TX* x = static_cast<const TX*>(a.x) + (size_t)(t0 + t) * a.xs + (size_t)h * a.D;
-    uint16_t* y = a.y + (size_t)(t0 + t) * a.ys + (size_t)h * a.D;
-    const bool rot = h < a.rot_heads && u < turned;
-    if constexpr (WIDE) {
-      const int o1 = rot && !INTER ? 8 * u : 16 * u;
-      const int o2 = rot && !INTER ? 8 * u + pairs : 16 * u + 8;
-      float p[8], q[8];
-      load8(x + o1, p);
-      load8(x + o2, q);
-      if (rot) {
-        const float2* w = cs + t * pairs + 8 * u;
-        if constexpr (INTER) {
+    Item item = fetch(i);
+    if (item.rot) {
+      const float2* w = cs + item.t * pairs + N * item.u;
+      if constexpr (WIDE && INTER) {
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const float2 w0 = w[k], w1 = w[4 + k];
-            const float a0 = p[2 * k], b0 = p[2 * k + 1], a1 = q[2 * k], b1 = q[2 * k + 1];
-            p[2 * k] = a0 * w0.x - b0 * w0.y;
-            p[2 * k + 1] = a0 * w0.y + b0 * w0.x;
-            q[2 * k] = a1 * w1.x - b1 * w1.y;
-            q[2 * k + 1] = a1 * w1.y + b1 * w1.x;
-          }
-        } else {
+        for (int k = 0; k < 4; ++k) {
+          const float2 w0 = w[k], w1 = w[4 + k];
+          const float a0 = item.p[2 * k], b0 = item.p[2 * k + 1], a1 = item.q[2 * k], b1 = item.q[2 * k + 1];
+          item.p[2 * k] = a0 * w0.x - b0 * w0.y;
+          item.p[2 * k + 1] = a0 * w0.y + b0 * w0.x;
+          item.q[2 * k] = a1 * w1.x - b1 * w1.y;
+          item.q[2 * k + 1] = a1 * w1.y + b1 * w1.x;
+        }
+      } else {
 #pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            const float2 wk = w[k];
-            const float a0 = p[k], b0 = q[k];
-            p[k] = a0 * wk.x - b0 * wk.y;
-            q[k] = a0 * wk.y + b0 * wk.x;
-          }
+        for (int k = 0; k < N; ++k) {
+          const float2 wk = w[k];
+          const float a0 = item.p[k], b0 = item.q[k];
+          item.p[k] = a0 * wk.x - b0 * wk.y;
+          item.q[k] = a0 * wk.y + b0 * wk.x;
         }
       }
-      store8(y + o1, p);
-      store8(y + o2, q);
+    }
+    uint16_t* y = a.y + (size_t)(t0 + item.t) * a.ys + item.head;
+    if constexpr (WIDE) {
+      store8(y + item.o1, item.p);
+      store8(y + item.o2, item.q);
     } else {
-      const int o1 = rot && !INTER ? u : 2 * u;
-      const int o2 = rot && !INTER ? u + pairs : 2 * u + 1;
-      float p = load_one(x + o1), q = load_one(x + o2);
-      if (rot) {
-        const float2 w = cs[t * pairs + u];
-        const float a0 = p, b0 = q;
-        p = a0 * w.x - b0 * w.y;
-        q = a0 * w.y + b0 * w.x;
-      }
-      const uint32_t w = pack_bf16x2(p, q);
-      y[o1] = (uint16_t)w;
-      y[o2] = (uint16_t)(w >> 16);
+      const uint32_t w = pack_bf16x2(item.p[0], item.q[0]);
+      y[item.o1] = (uint16_t)w;
+      y[item.o2] = (uint16_t)(w >> 16);
     }
   }
 }
@@ -256,8 +268,8 @@ constexpr int kCacheThreads = 256;
 // Byte offsets within the record of one (page, head): key codes, value codes, key scales, value scales.
 struct Kv4Layout {
   int D, page_log2;
-  __device__ __forceinline__ int codes(int which, int off, int block) const {
-    return ((which << page_log2) + off) * (D >> 1) + 16 * block;
+  __device__ __forceinline__ int codes(int which, int off, int unit) const {       // of 8 elements
+    return ((which << page_log2) + off) * (D >> 1) + 4 * unit;
   }
   __device__ __forceinline__ int scale(int which, int off, int block) const {
     return (D << page_log2) + ((which << page_log2) + off) * (D >> 5) + block;
@@ -272,12 +284,27 @@ struct CacheArgs {
   uint16_t* vo;
   uint8_t* cache;
   const int32_t* slots;
-  long n;                  // threads: tokens x 2 x heads x blocks
   long ks, vs;             // elements between tokens
+  unsigned n;              // threads: tokens x 2 x heads x (D / 8)
   int Hkv, nslots;
-  int blocks_log2;         // blocks of 32 of a head
+  int units_log2;          // of D / 8
   Kv4Layout lay;
 };
+
+// A thread moves 8 elements: 16 bytes of bf16 and 4 of codes, so that a wave's accesses on either side are contiguous
+// within a token; four neighbouring threads share a block of 32 and its scale.
+struct CacheItem {
+  long t;
+  int which, h, unit;      // keys or values, head, 8 elements of it
+};
+__device__ __forceinline__ CacheItem cache_item(const CacheArgs& a, unsigned i) {
+  const unsigned row = i >> a.units_log2, per = 2u * (unsigned)a.Hkv;
+  const unsigned t = row / per;
+  unsigned h = row - t * per;
+  const bool second = h >= (unsigned)a.Hkv;
+  if (second) h -= (unsigned)a.Hkv;
+  return {(long)t, second ? 1 : 0, (int)h, (int)(i & ((1u << a.units_log2) - 1u))};
+}
 
 // A block's exponent: that of its largest magnitude rounded to two significant bits (so 1.75 and up counts as
 // the next power of two, whose half is the level 4; the plain exponent would cut those to 6 of 8), less 2 for
@@ -289,45 +316,32 @@ __device__ __forceinline__ uint32_t block_exponent(uint32_t top) {   // bits of 
   return e < 3u ? 1u : e - 2u;
 }
 
-// One thread quantises one block of 32 values: 64 bytes read, 16 + 1 written.
 __global__ __launch_bounds__(kCacheThreads) void kv4_store_kernel(CacheArgs a) {
-  const long i = (long)blockIdx.x * kCacheThreads + threadIdx.x;
-  if (i >= a.n) return;
-  const int block = (int)(i & ((1 << a.blocks_log2) - 1));
-  const long hi = i >> a.blocks_log2;
-  const long tw = hi / a.Hkv;
-  const int h = (int)(hi - tw * a.Hkv);
-  const int which = (int)(tw & 1);
-  const long t = tw >> 1;
-  const int slot = a.slots[t];
+  const unsigned i = blockIdx.x * kCacheThreads + threadIdx.x;
+  if (i >= a.n) return;          // (n is a multiple of 4: the threads of a block are all here or all gone)
+  const CacheItem it = cache_item(a, i);
+  const int slot = a.slots[it.t];
+  const u32x4 w = *reinterpret_cast<const u32x4*>((it.which ? a.v + it.t * a.vs : a.k + it.t * a.ks) + (size_t)it.h * a.lay.D + 8 * it.unit);
+  uint32_t top = 0;              // bf16 magnitudes order as integers, NaN above infinity
+#pragma unroll
+  for (int c = 0; c < 4; ++c) top = max(top, max((w[c] << 16) & 0x7fff0000u, w[c] & 0x7fff0000u));
+  top = max(top, (uint32_t)__shfl_xor((int)top, 1));
+  top = max(top, (uint32_t)__shfl_xor((int)top, 2));
   if ((unsigned)slot >= (unsigned)a.nslots) return;
-  const u32x4* src = reinterpret_cast<const u32x4*>((which ? a.v + t * a.vs : a.k + t * a.ks) + (size_t)h * a.lay.D + 32 * block);
-  u32x4 w[4];
-#pragma unroll
-  for (int j = 0; j < 4; ++j) w[j] = src[j];
-  uint32_t top = 0;        // bf16 magnitudes order as integers, NaN above infinity
-#pragma unroll
-  for (int j = 0; j < 4; ++j)
-#pragma unroll
-    for (int c = 0; c < 4; ++c) top = max(top, max((w[j][c] << 16) & 0x7fff0000u, w[j][c] & 0x7fff0000u));
   const uint32_t e = block_exponent(top);
-  u32x4 codes = {};
+  uint32_t codes = 0;
   if (e != 255u) {
     const float unit = __builtin_bit_cast(float, e << 23);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      uint32_t c = 0;      // v_cvt_scalef32_pk_fp4_bf16: x / unit to the next level, ties to the even code
-      c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, (uint32_t)w[j][0]), unit, 0);
-      c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, (uint32_t)w[j][1]), unit, 1);
-      c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, (uint32_t)w[j][2]), unit, 2);
-      c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, (uint32_t)w[j][3]), unit, 3);
-      codes[j] = c;
-    }
+    // v_cvt_scalef32_pk_fp4_bf16: x / unit to the next level, ties to the even code
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(codes, __builtin_bit_cast(bf16x2, (uint32_t)w[0]), unit, 0);
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(codes, __builtin_bit_cast(bf16x2, (uint32_t)w[1]), unit, 1);
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(codes, __builtin_bit_cast(bf16x2, (uint32_t)w[2]), unit, 2);
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(codes, __builtin_bit_cast(bf16x2, (uint32_t)w[3]), unit, 3);
   }
   const int page = slot >> a.lay.page_log2, off = slot & ((1 << a.lay.page_log2) - 1);
-  uint8_t* rec = a.cache + ((size_t)page * a.Hkv + h) * a.lay.record();
-  *reinterpret_cast<u32x4*>(rec + a.lay.codes(which, off, block)) = codes;
-  rec[a.lay.scale(which, off, block)] = (uint8_t)e;
+  uint8_t* rec = a.cache + ((size_t)page * a.Hkv + it.h) * a.lay.record();
+  *reinterpret_cast<uint32_t*>(rec + a.lay.codes(it.which, off, it.unit)) = codes;
+  if ((it.unit & 3) == 0) rec[a.lay.scale(it.which, off, it.unit >> 2)] = (uint8_t)e;
 }
 
 // Two levels of a packed byte (0..3 of w) times 2^(e-127); exact in bf16, NaN for e = 255.
@@ -342,23 +356,17 @@ __device__ __forceinline__ u32x4 fp4_unit(uint32_t w, float unit) {
 }
 
 __global__ __launch_bounds__(kCacheThreads) void kv4_load_kernel(CacheArgs a) {
-  const long i = (long)blockIdx.x * kCacheThreads + threadIdx.x;
+  const unsigned i = blockIdx.x * kCacheThreads + threadIdx.x;
   if (i >= a.n) return;
-  const int block = (int)(i & ((1 << a.blocks_log2) - 1));
-  const long hi = i >> a.blocks_log2;
-  const long tw = hi / a.Hkv;
-  const int h = (int)(hi - tw * a.Hkv);
-  const int which = (int)(tw & 1);
-  const long t = tw >> 1;
-  const int slot = a.slots[t];
+  const CacheItem it = cache_item(a, i);
+  const int slot = a.slots[it.t];
   if ((unsigned)slot >= (unsigned)a.nslots) return;
   const int page = slot >> a.lay.page_log2, off = slot & ((1 << a.lay.page_log2) - 1);
-  const uint8_t* rec = a.cache + ((size_t)page * a.Hkv + h) * a.lay.record();
-  const u32x4 codes = *reinterpret_cast<const u32x4*>(rec + a.lay.codes(which, off, block));
-  const float unit = __builtin_bit_cast(float, (uint32_t)rec[a.lay.scale(which, off, block)] << 23);
-  u32x4* dst = reinterpret_cast<u32x4*>((which ? a.vo : a.ko) + ((size_t)t * a.Hkv + h) * a.lay.D + 32 * block);
-#pragma unroll
-  for (int j = 0; j < 4; ++j) dst[j] = fp4_unit(codes[j], unit);
+  const uint8_t* rec = a.cache + ((size_t)page * a.Hkv + it.h) * a.lay.record();
+  const uint32_t codes = *reinterpret_cast<const uint32_t*>(rec + a.lay.codes(it.which, off, it.unit));
+  const uint32_t e = rec[a.lay.scale(it.which, off, it.unit >> 2)];
+  *reinterpret_cast<u32x4*>((it.which ? a.vo : a.ko) + ((size_t)it.t * a.Hkv + it.h) * a.lay.D + 8 * it.unit) =
+      fp4_unit(codes, __builtin_bit_cast(float, e << 23));
 }
 
 }  // namespace
