@@ -347,9 +347,9 @@ int qgemm_rope(const void* x, int x_type, const int32_t* positions, const double
  * tokens whose slot is outside [0, pages*page) are skipped; two tokens of one
  * slot leave it unspecified. For each block of 32 elements of a head:
  *   E = floor(log2(largest magnitude, rounded to two significant bits, ties up)) - 2,
- *     at least -126; codes = x / 2^E to the nearest level, ties to the even code
+ *     between -126 and 125; codes = x / 2^E to the nearest level, ties to the even code
  * (so a block's largest magnitudes are at most half a level step off, 7 going to
- * 8 and not to 6). A block with an infinity or NaN is held as NaN.
+ * 8 and not to 6; from 1.75 * 2^127 on all are held as 6 * 2^125). A block with an infinity or NaN is held as NaN.
  */
 int qgemm_kv4_store(const void* k, const void* v, const int32_t* slots, void* cache, int T, int Hkv,
                     int D, int64_t k_stride, int64_t v_stride, int pages, int page,
@@ -391,7 +391,8 @@ int qgemm_attention_packed(const void* q, const void* k, const void* v, const in
  * [T][H][D], dense; cache, block_table as above, kv_len: int32 [R]; cu_q: int32
  * [R+1], ascending, or null. fp32 scores, sums and accumulation; the softmax
  * weights enter the output product as bf16. Keys of a page outside [0, pages) or
- * past the table's W entries make the rows that see them NaN; nothing else that
+ * past the table's W entries make the rows that see them NaN, and a value block of scale
+ * byte 253 or 254, which passes bf16's range, counts as one of NaN; nothing else that
  * the pages hold behind a row's position reaches it. Results do not depend on how the
  * work was split beyond fp32 summation order, and are the same on every call.
  * workspace: caller-owned device memory, 16-byte aligned, of the bytes that

@@ -117,7 +117,7 @@ def quantise(x):
             while 2.0 ** (p + 1) <= top:
                 p += 1
             m = top / 2.0 ** p                       # 1 <= m < 2; to two significant bits: 1, 1.5 or 2
-            e = max((p + 1 if m >= 1.75 else p) - 2, -126)
+            e = min(max((p + 1 if m >= 1.75 else p) - 2, -126), 125)
         E[i] = e + 127
         a = np.abs(b) / 2.0 ** e
         d = np.abs(a[:, None] - LEVELS[None, :])

@@ -513,7 +513,7 @@ def rope(x: torch.Tensor, positions: torch.Tensor, inv_freq: torch.Tensor, rot_h
             raise ValueError("out must have the shape of x")
     _enqueue(lib().qgemm_rope, _device(x, positions, inv_freq, out), x, x.data_ptr(), 1 if x.dtype is torch.bfloat16 else 0,
              positions.data_ptr(), inv_freq.data_ptr(), out.data_ptr(), T, heads, rot_heads, D, 2 * inv_freq.shape[0], xs, ys,
-             1 if interleaved else 0, gain)
+             1 if interleaved else 0, float(gain))
     return out
 
 
@@ -588,7 +588,7 @@ def attention_packed(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu: torc
         if oshape != shape:
             raise ValueError("out must have the shape of q")
     _enqueue(lib().qgemm_attention_packed, _device(q, k, v, cu, out), q, q.data_ptr(), k.data_ptr(), v.data_ptr(), cu.data_ptr(),
-             out.data_ptr(), T, R, H, kshape[1], D, qs, ks, vs, ys, D ** -0.5 if scale is None else scale)
+             out.data_ptr(), T, R, H, kshape[1], D, qs, ks, vs, ys, D ** -0.5 if scale is None else float(scale))
     return out
 
 
@@ -622,7 +622,7 @@ def attention_kv4(q: torch.Tensor, cache: torch.Tensor, block_table: torch.Tenso
     ws = torch.empty(n.value, dtype=torch.uint8, device=q.device)
     _enqueue(lib().qgemm_attention_kv4, _device(q, cache, block_table, kv_len, out), q, q.data_ptr(), cache.data_ptr(),
              block_table.data_ptr(), kv_len.data_ptr(), None if cu_q is None else cu_q.data_ptr(), out.data_ptr(),
-             ws.data_ptr(), n.value, T, R, H, Hkv, D, W, pages, page, qs, D ** -0.5 if scale is None else scale)
+             ws.data_ptr(), n.value, T, R, H, Hkv, D, W, pages, page, qs, D ** -0.5 if scale is None else float(scale))
     return out
 
 

@@ -129,18 +129,23 @@ struct PackedStarts {
   }
 };
 
-// One packed row by itself, by a whole wave: o = sum_j softmax(scale q.k)_j v_j over the keys j0 .. row. For rows
-// whose result is not finite: in the tiles a weight of 0 times another prompt's infinite or NaN value is NaN.
-// (Inlined: a call gives the kernel a stack, which costs each launch 4 us.)
+// One packed row by itself, by a whole wave: o = sum_j softmax(scale q.k)_j v_j over the keys j0 .. row. For rows of
+// finite weights whose result is not: in the tiles a weight of 0 times another prompt's, or a later row's, infinite or
+// NaN value is NaN. (Inlined: a call gives the kernel a stack, which costs each launch 4 us.)
 template <int D>
 __device__ __forceinline__ void packed_row(const AttnArgs& a, int row, int j0, int h, int g) {
   const int lane = threadIdx.x & 63;
-  const uint16_t* q = a.q + (size_t)row * a.qs + (size_t)h * D;
-  auto f = [](uint16_t b) { return __builtin_bit_cast(float, (uint32_t)b << 16); };
+  const u32x4* q = reinterpret_cast<const u32x4*>(a.q + (size_t)row * a.qs + (size_t)h * D);
+  auto lo = [](uint32_t w) { return __builtin_bit_cast(float, w << 16); };
+  auto hi = [](uint32_t w) { return __builtin_bit_cast(float, w & 0xffff0000u); };
   auto score = [&](int j) {
-    const uint16_t* k = a.k + (size_t)j * a.ks + (size_t)g * D;
+    const u32x4* k = reinterpret_cast<const u32x4*>(a.k + (size_t)j * a.ks + (size_t)g * D);
     float s = 0.0f;
-    for (int d = 0; d < D; ++d) s = __builtin_fmaf(f(q[d]), f(k[d]), s);
+    for (int c = 0; c < D / 8; ++c) {
+      const u32x4 x = q[c], y = k[c];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s = __builtin_fmaf(hi(x[e]), hi(y[e]), __builtin_fmaf(lo(x[e]), lo(y[e]), s));
+    }
     return s;
   };
   float m = -__builtin_inff();
@@ -157,7 +162,7 @@ __device__ __forceinline__ void packed_row(const AttnArgs& a, int row, int j0, i
       const float pi = __shfl(p, i);
       const uint16_t* v = a.v + (size_t)(jb + i) * a.vs + (size_t)g * D;
 #pragma unroll
-      for (int c = 0; c < D / 64; ++c) o[c] = __builtin_fmaf(pi, f(v[64 * c + lane]), o[c]);
+      for (int c = 0; c < D / 64; ++c) o[c] = __builtin_fmaf(pi, lo(v[64 * c + lane]), o[c]);
     }
   }
 #pragma unroll
@@ -533,14 +538,16 @@ __device__ __forceinline__ void attn_body(const AttnArgs& a) {
   // normalise and store: lane (col, hh) holds o[qrow][dt*32 + 8a + 4hh + {0..3}] in acc_o[dt][4a..4a+3]
   const float l_tot = l_run + other_half(l_run);
   const float inv = 1.0f / l_tot;
-  uint32_t odd = 0;                // PACKED: the wave's queries whose result is infinite or NaN
+  // PACKED: the wave's queries of finite weights whose result is infinite or NaN. (Weights that are not finite come
+  // from a key that the query sees, and every element is NaN as it stands.)
+  uint32_t odd = 0;
   if constexpr (PACKED) {
-    float z = inv;
+    float z = 0.0f;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
       for (int r = 0; r < 16; ++r) z = __builtin_fmaf(acc_o[dt][r], 0.0f, z);
-    const unsigned long long lanes = __ballot(qrow < S && !__builtin_isfinite(z));
+    const unsigned long long lanes = __ballot(qrow < S && __builtin_isfinite(inv) && !__builtin_isfinite(z));
     odd = (uint32_t)lanes | (uint32_t)(lanes >> 32);
   }
   if (qrow < S && !(PACKED && ((odd >> col) & 1))) {

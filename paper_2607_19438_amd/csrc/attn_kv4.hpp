@@ -38,6 +38,10 @@ constexpr int kKv4Bufs = 2;                           // steps of keys and value
 // 11.3, 11.2.
 constexpr int kKv4Start = 2;
 
+// Value blocks from this scale on count as NaN: 4 and 6 times 2^126 are infinite in bf16, and a weight of 0 would not
+// keep an infinity out of the product either. (The store gives at most 252, or 255.)
+constexpr uint32_t kKv4NaN = 253;
+
 // The unit that a workgroup's last segment begins and does not end: where its other parts are, and its rows.
 struct Kv4Head {
   int r;              // request, -1: there is no such unit
@@ -326,11 +330,11 @@ __device__ __forceinline__ void kv4_body(const Kv4Args& a) {
             for (int t = 0; t < DW; ++t) b.v[i][t] = hidden ? 0u : b.v[i][t];
           }
         }
-        const unsigned long long nan_at[2] = {__ballot(b.vs[0] == 255u), __ballot(b.vs[1] == 255u)};
+        const unsigned long long nan_at[2] = {__ballot(b.vs[0] >= kKv4NaN), __ballot(b.vs[1] >= kKv4NaN)};
         if (nan_at[0] | nan_at[1]) {
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
-            const bool nan = b.vs[i] == 255u;
+            const bool nan = b.vs[i] >= kKv4NaN;
             b.vs[i] = nan ? 0u : b.vs[i];
 #pragma unroll
             for (int t = 0; t < DW; ++t) b.v[i][t] = nan ? 0u : b.v[i][t];
@@ -524,7 +528,7 @@ __device__ __forceinline__ void kv4_body(const Kv4Args& a) {
 }
 
 template <int D, int NT>
-constexpr int kKv4PerCU = NT == 1 ? (D == 128 ? 3 : 4) : NT == 2 ? 2 : 1;
+constexpr int kKv4PerCU = NT == 2 ? 2 : D == 128 ? 3 : 4;      // workgroups that a CU holds, by the registers
 
 template <int D, int NT>
 __global__ __launch_bounds__(kKv4Threads, (kKv4PerCU<D, NT>)) void kv4_attn_kernel(Kv4Args a) {

@@ -76,12 +76,15 @@ Kv4Plan kv4_plan(int T, int R, int H, int Hkv, int D, int W, int page) {
   const long G = H / Hkv;
   const long rows = ((long)T * G + R - 1) / R;          // of a request and head, on average
   Kv4Plan p{};
-  p.nt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+  // Two tiles share the unpacking of the keys and values where a request's rows need more than one; a wave of four
+  // has the registers of a whole SIMD. (us, one tile, two, four: 2 chunks of 550 rows, 5000 keys, 32/8 heads of 128
+  // 190, 159, 199; 6 requests of 8 to 32 rows and 32/4 heads 43.2, 41.5, 49.3; 16 of 6 rows and 32/8 heads 38.3,
+  // 33.7; 9 of 3 to 9 rows, 32/8 heads of 64 17.5, 17.2.)
+  p.nt = rows <= 16 ? 1 : 2;
   const long tiles = ((long)T * G) / (16 * p.nt) + R;   // at least their number, requests of no tokens aside
   const long grans = std::max<long>(1, qg::ceil_div((long)W * page, qg::kKv4Granule));
   // as many workgroups as the CUs hold at once, or fewer if there are not so many granules
-  const long fill = kCUs * (p.nt == 1 ? (D == 128 ? qg::kKv4PerCU<128, 1> : qg::kKv4PerCU<64, 1>)
-                                      : p.nt == 2 ? qg::kKv4PerCU<128, 2> : qg::kKv4PerCU<128, 4>);
+  const long fill = kCUs * (p.nt == 2 ? qg::kKv4PerCU<128, 2> : D == 128 ? qg::kKv4PerCU<128, 1> : qg::kKv4PerCU<64, 1>);
   const long most = std::min(tiles, fill) * std::min<long>(Hkv, fill) * std::min(grans, fill);
   p.groups = (int)std::min(fill, most);
   p.part_floats = 16L * p.nt * (D + 2);
@@ -118,9 +121,7 @@ int launch_kv4(const qg::Kv4Args& a, bool join, hipStream_t s) {
 
 template <int D>
 int launch_kv4_nt(const qg::Kv4Args& a, int nt, bool join, hipStream_t s) {
-  if (nt == 1) return launch_kv4<D, 1>(a, join, s);
-  if (nt == 2) return launch_kv4<D, 2>(a, join, s);
-  return launch_kv4<D, 4>(a, join, s);
+  return nt == 1 ? launch_kv4<D, 1>(a, join, s) : launch_kv4<D, 2>(a, join, s);
 }
 
 }  // namespace

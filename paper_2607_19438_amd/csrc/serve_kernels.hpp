@@ -308,12 +308,12 @@ __device__ __forceinline__ CacheItem cache_item(const CacheArgs& a, unsigned i) 
 
 // A block's exponent: that of its largest magnitude rounded to two significant bits (so 1.75 and up counts as
 // the next power of two, whose half is the level 4; the plain exponent would cut those to 6 of 8), less 2 for
-// the largest level's 4 <= 6 < 8. Zero and the smallest blocks take 2^-126; a block with an infinity or NaN
-// 255, which reads as NaN.
+// the largest level's 4 <= 6 < 8. Zero and the smallest blocks take 2^-126, the largest 2^125 (6 of it are the most
+// below bf16's end); a block with an infinity or NaN 255, which reads as NaN.
 __device__ __forceinline__ uint32_t block_exponent(uint32_t top) {   // bits of the largest |x|
   if (top >= 0x7f800000u) return 255u;
   const uint32_t e = (top + 0x200000u) >> 23;
-  return e < 3u ? 1u : e - 2u;
+  return min(max(e, 3u) - 2u, 252u);
 }
 
 __global__ __launch_bounds__(kCacheThreads) void kv4_store_kernel(CacheArgs a) {

@@ -147,6 +147,8 @@ def test_what_pages_hold_behind_a_row_reaches_nothing():
     assert torch.equal(o[:3], c[:3]) and torch.isnan(o[3]).all()
     assert torch.equal(o[4:7], c[4:7])
     assert torch.isnan(o[7:9, :, 64:96]).all()
+    dirty[s1 // page, :, n0 + (page + s1 % page) * 4 + 2] = 254           # past bf16's range: the same
+    assert torch.isnan(run(torch, (wild, dirty, k, v, qn, bits, cu), kv, cu).float()[7:9, :, 64:96]).all()
     keep = [i for i in range(128) if not 64 <= i < 96]
     assert torch.equal(o[7:9][..., keep], c[7:9][..., keep]) and torch.equal(o[9], c[9])
 
@@ -164,6 +166,23 @@ def test_missing_pages_are_nan():
     assert torch.isfinite(o[:3]).all() and torch.isnan(o[3]).all()
     o = run(torch, case, [40, -5, 2 ** 31 - 1, 1], None).float()
     assert torch.isfinite(o[0]).all() and torch.all(o[1] == 0) and torch.isnan(o[2]).all() and torch.isfinite(o[3]).all()
+
+
+def test_tables_of_no_pages():
+    torch = torch_or_skip()
+    m = q()
+    x = torch.randn((3, 4, 64), device="cuda").to(torch.bfloat16)
+    cache = torch.zeros(m.kv4_cache_shape(1, 2, 64, 16), dtype=torch.uint8, device="cuda")
+    table = torch.empty((3, 0), dtype=torch.int32, device="cuda")
+    o = m.attention_kv4(x, cache, table, dev_i32(torch, [0, 0, 0]))
+    assert torch.all(o == 0)
+    o = m.attention_kv4(x, cache, table, dev_i32(torch, [0, 1, 0])).float()
+    assert torch.all(o[0] == 0) and torch.isnan(o[1]).all() and torch.all(o[2] == 0)
+    none = torch.empty((0, 4, 64), dtype=torch.bfloat16, device="cuda")
+    assert m.attention_kv4(none, cache, table[:0], dev_i32(torch, [])).shape == (0, 4, 64)
+    out = torch.full((3, 4, 64), 9.0, dtype=torch.bfloat16, device="cuda")
+    m.attention_kv4(x, cache, table[:0], dev_i32(torch, []), dev_i32(torch, [0]), out=out)       # rows of no request
+    assert torch.all(out == 9)
 
 
 def test_inconsistent_first_rows_stay_in_bounds():

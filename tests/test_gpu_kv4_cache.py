@@ -60,7 +60,7 @@ def test_store_and_load(T, Hkv, D, page, pages):
     m.kv4_load(dc, dev_i32(torch, every), D, kk, vv)
     for got, ref in zip((kk, vv), oracle.decode_cache(want, D)):
         got = host_bf16(torch, got)
-        fits = ~(np.abs(ref) > 3.3895e38)                        # (random exponents: beyond bf16)
+        fits = ~(np.abs(ref) > 3.3895e38)                        # (random exponents: beyond bf16's range)
         tiny = np.abs(ref) < 2.0 ** -126
         assert np.array_equal(got[:-4][fits & ~tiny], ref[fits & ~tiny], equal_nan=True)
         assert np.all(np.abs(got[:-4][tiny] - ref[tiny]) <= 2.0 ** -133)
@@ -141,6 +141,19 @@ def test_strided_rows_and_large_offsets():
     for x, y in zip(m.kv4_load(big, at, 128), m.kv4_load(a, slots, 128)):
         assert torch.equal(x, y)
     del big
+
+
+def test_the_largest_numbers_stay_finite():
+    torch = torch_or_skip()
+    m = q()
+    x = torch.full((3, 1, 64), 3.3895e38, device="cuda").to(torch.bfloat16)
+    x[1], x[2] = -x[1], 2.9e38
+    cache = torch.zeros(m.kv4_cache_shape(1, 1, 64, 16), dtype=torch.uint8, device="cuda")
+    slots = torch.arange(3, dtype=torch.int32, device="cuda")
+    m.kv4_store(x, x, slots, cache)
+    for y in m.kv4_load(cache, slots, 64):
+        y = host_bf16(torch, y)
+        assert np.all(y[0] == 6 * 2.0 ** 125) and np.all(y[1] == -6 * 2.0 ** 125) and np.all(y[2] == 6 * 2.0 ** 125)
 
 
 def test_values_of_one_step():

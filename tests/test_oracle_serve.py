@@ -74,6 +74,8 @@ def test_quantise_by_hand():
     b[0] = 6.99
     assert oracle.quantise(b)[1] == 127
     assert oracle.quantise(np.zeros(32))[1] == 1
+    codes, E = oracle.quantise(np.full(32, 3.3895e38))          # no further than 6 * 2^125, the last below bf16's end
+    assert E == 252 and np.all(codes == 7)
     for bad in (np.inf, -np.inf, np.nan):
         b[5] = bad
         assert oracle.quantise(b)[1] == 255

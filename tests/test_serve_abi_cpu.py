@@ -138,6 +138,41 @@ def test_frequency_refusals(m):
         m.rope_frequencies(64, scaling="ntk", device="cpu")
 
 
+def test_calls_go_to_the_device_of_their_tensors(m, monkeypatch):
+    """Tensors of another device than the current one: that device is made current around the call and its stream taken;
+    tensors of two devices are refused."""
+    import torch
+
+    class Fake:
+        def __init__(self, dev):
+            self.dev = dev
+
+        def get_device(self):
+            return self.dev
+
+    seen, current = [], [0]
+
+    class Guard:
+        def __init__(self, dev):
+            self.dev = dev
+
+        def __enter__(self):
+            self.was, current[0] = current[0], self.dev
+
+        def __exit__(self, *a):
+            current[0] = self.was
+
+    monkeypatch.setattr(torch.cuda, "device", Guard)
+    monkeypatch.setattr(m, "_current_device", lambda: current[0])
+    monkeypatch.setattr(m, "_stream", lambda t: 100 + t.get_device())
+    for dev in (0, 3):
+        a = Fake(dev)
+        m._enqueue(lambda *x: seen.append((current[0], *x)) or 0, m._device(a, Fake(dev)), a, 7)
+    assert seen == [(0, 7, 100), (3, 7, 103)] and current == [0]
+    with pytest.raises(ValueError, match="one device"):
+        m._device(Fake(0), Fake(1))
+
+
 def test_binding_refuses_host_tensors_and_shapes(m):
     import torch
     i = torch.zeros(4, dtype=torch.int32)
