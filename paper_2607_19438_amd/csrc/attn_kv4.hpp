@@ -252,11 +252,12 @@ __device__ __forceinline__ void kv4_body(const Kv4Args& a) {
       const int kall = clamp_i(rq.kv - rq.n + row0 / G + 1, 0, rq.len);       // keys that every row sees
 
       f32x4 acc[NT][DT];
-      float m_run[NT], l_run[NT];
+      float m_run[NT];
+      f32x4 l_run[NT];                              // sum of the weights as they enter the product, four times
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         m_run[nt] = -__builtin_inff();
-        l_run[nt] = rq.kv > rq.len ? __builtin_nanf("") : 0.0f;   // keys without a page to look in
+        l_run[nt] = f32x4{} + (rq.kv > rq.len ? __builtin_nanf("") : 0.0f);   // keys without a page to look in
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) acc[nt][dt] = f32x4{};
       }
@@ -373,13 +374,14 @@ __device__ __forceinline__ void kv4_body(const Kv4Args& a) {
           const float ms = m_run[nt] == -__builtin_inff() ? 0.0f : m_run[nt] * a.sl2;
           float p[8];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[nt][e >> 2][e & 3], a.sl2, -ms));
-            l_run[nt] += p[e];
-          }
+          for (int e = 0; e < 8; ++e) p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[nt][e >> 2][e & 3], a.sl2, -ms));
           pb[nt] = __builtin_bit_cast(bf16x8, u32x4{pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]),
                                                     pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7])});
         }
+        // the weights' sum as a product with ones: rounded as they are, so that their rounding cancels where few weigh
+        const bf16x8 ones = __builtin_bit_cast(bf16x8, u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u});
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) l_run[nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pb[nt], l_run[nt], 0, 0, 0);
         asm volatile("" ::: "memory");       // the tile's writes stay before its reads; a wave's LDS accesses run in order
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) {
@@ -455,10 +457,9 @@ __device__ __forceinline__ void kv4_body(const Kv4Args& a) {
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
           *reinterpret_cast<f32x4*>(&ow[col * D + (((4 * dt + grp) ^ (col & 7)) << 2)]) = acc[nt][dt];
-        const float l = sum_over_groups(l_run[nt]);
         if (grp == 0) {
           ml[wave][16 * nt + col][0] = m_run[nt];
-          ml[wave][16 * nt + col][1] = l;
+          ml[wave][16 * nt + col][1] = l_run[nt][0];
         }
         __syncthreads();
         const int row = tid >> 4, ch = tid & 15;
