@@ -167,6 +167,14 @@ __device__ __forceinline__ void store8(uint16_t* p, const float (&v)[8]) {
       u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
 }
 
+// (a, b) turned by w = (cosine, sine), each with one product rounded and one fused; written out, so that every form of
+// the kernel gives the same bits.
+__device__ __forceinline__ void rotate(float& a, float& b, float2 w) {
+  const float a0 = a;
+  a = __builtin_fmaf(a0, w.x, -(b * w.y));
+  b = __builtin_fmaf(a0, w.y, b * w.x);
+}
+
 // The sine and cosine of every (token, pair) are evaluated once per workgroup and shared by all heads through
 // LDS. The angle is taken in turns in fp64 (position x frequency / 2 pi, less its whole turns): at position
 // 10^6 an fp32 product is off by 0.06 radians. What is left is below half a turn, so fp32 keeps 2^-25 of one.
@@ -230,21 +238,12 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeArgs a) {
       if constexpr (WIDE && INTER) {
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          const float2 w0 = w[k], w1 = w[4 + k];
-          const float a0 = item.p[2 * k], b0 = item.p[2 * k + 1], a1 = item.q[2 * k], b1 = item.q[2 * k + 1];
-          item.p[2 * k] = a0 * w0.x - b0 * w0.y;
-          item.p[2 * k + 1] = a0 * w0.y + b0 * w0.x;
-          item.q[2 * k] = a1 * w1.x - b1 * w1.y;
-          item.q[2 * k + 1] = a1 * w1.y + b1 * w1.x;
+          rotate(item.p[2 * k], item.p[2 * k + 1], w[k]);
+          rotate(item.q[2 * k], item.q[2 * k + 1], w[4 + k]);
         }
       } else {
 #pragma unroll
-        for (int k = 0; k < N; ++k) {
-          const float2 wk = w[k];
-          const float a0 = item.p[k], b0 = item.q[k];
-          item.p[k] = a0 * wk.x - b0 * wk.y;
-          item.q[k] = a0 * wk.y + b0 * wk.x;
-        }
+        for (int k = 0; k < N; ++k) rotate(item.p[k], item.q[k], w[k]);
       }
     }
     uint16_t* y = a.y + (size_t)(t0 + item.t) * a.ys + item.head;
