@@ -11,6 +11,7 @@ no fallback path, and a missing library raises ``QGemmError``.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 import torch  # imported before the library so that both share one HIP runtime
@@ -421,13 +422,17 @@ def _device(first: torch.Tensor, *others) -> int:
     return dev
 
 
-def _enqueue(fn, dev: int, first: torch.Tensor, *args):
-    """``fn(*args, stream)`` on the current stream of device ``dev``, that of ``first``."""
+def _stream_of(dev: int):
+    return torch.cuda.current_stream(dev).cuda_stream if _raw_stream is None else _raw_stream(dev)
+
+
+def _enqueue(fn, dev: int, *args):
+    """``fn(*args, stream)`` on the current stream of device ``dev``, which is made current for the call if it is not."""
     if _current_device() == dev:
-        rc = fn(*args, _stream(first))
+        rc = fn(*args, _stream_of(dev))
     else:
         with torch.cuda.device(dev):
-            rc = fn(*args, _stream(first))
+            rc = fn(*args, _stream_of(dev))
     if rc:
         _check(rc)
 
@@ -469,7 +474,7 @@ def kv_plan(kv_len, q_len, block_table, free_pages, page: int, tokens: int, out:
             if t.shape[0] != n:
                 raise ValueError(f"out.{name} must have {n} entries")
         _device(kv_len, out.cu_q, out.positions, out.slots, out.kv_len, out.used)
-    _enqueue(lib().qgemm_kv_plan, dev, kv_len, kv_len.data_ptr(), q_len.data_ptr(), block_table.data_ptr(), free_pages.data_ptr(),
+    _enqueue(lib().qgemm_kv_plan, dev, kv_len.data_ptr(), q_len.data_ptr(), block_table.data_ptr(), free_pages.data_ptr(),
              out.cu_q.data_ptr(), out.positions.data_ptr(), out.slots.data_ptr(), out.kv_len.data_ptr(), out.used.data_ptr(), R,
              block_table.shape[1], free_pages.shape[0], page, tokens)
     return out
@@ -511,7 +516,7 @@ def rope(x: torch.Tensor, positions: torch.Tensor, inv_freq: torch.Tensor, rot_h
         shape, ys = _need_rows(out, "out", _BF16)
         if shape != (T, heads, D):
             raise ValueError("out must have the shape of x")
-    _enqueue(lib().qgemm_rope, _device(x, positions, inv_freq, out), x, x.data_ptr(), 1 if x.dtype is torch.bfloat16 else 0,
+    _enqueue(lib().qgemm_rope, _device(x, positions, inv_freq, out), x.data_ptr(), 1 if x.dtype is torch.bfloat16 else 0,
              positions.data_ptr(), inv_freq.data_ptr(), out.data_ptr(), T, heads, rot_heads, D, 2 * inv_freq.shape[0], xs, ys,
              1 if interleaved else 0, float(gain))
     return out
@@ -540,7 +545,7 @@ def kv4_store(k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, cache: torc
     pages, heads, page = _cache_sizes(cache, D)
     if vshape != shape or heads != Hkv or slots.shape[0] != T:
         raise ValueError("k, v, slots and cache disagree on T, Hkv or D")
-    _enqueue(lib().qgemm_kv4_store, _device(k, v, slots, cache), k, k.data_ptr(), v.data_ptr(), slots.data_ptr(), cache.data_ptr(), T, Hkv,
+    _enqueue(lib().qgemm_kv4_store, _device(k, v, slots, cache), k.data_ptr(), v.data_ptr(), slots.data_ptr(), cache.data_ptr(), T, Hkv,
              D, ks, vs, pages, page)
 
 
@@ -560,7 +565,7 @@ def kv4_load(cache: torch.Tensor, slots: torch.Tensor, D: int, k: torch.Tensor |
         _need(v, "v", _BF16, 3)
     if k.shape != shape or v.shape != shape:
         raise ValueError("k and v must be [T][Hkv][D]")
-    _enqueue(lib().qgemm_kv4_load, _device(cache, slots, k, v), cache, cache.data_ptr(), slots.data_ptr(), k.data_ptr(), v.data_ptr(),
+    _enqueue(lib().qgemm_kv4_load, _device(cache, slots, k, v), cache.data_ptr(), slots.data_ptr(), k.data_ptr(), v.data_ptr(),
              shape[0], Hkv, D, pages, page)
     return k, v
 
@@ -587,9 +592,17 @@ def attention_packed(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu: torc
         oshape, ys = _need_rows(out, "out", _BF16)
         if oshape != shape:
             raise ValueError("out must have the shape of q")
-    _enqueue(lib().qgemm_attention_packed, _device(q, k, v, cu, out), q, q.data_ptr(), k.data_ptr(), v.data_ptr(), cu.data_ptr(),
+    _enqueue(lib().qgemm_attention_packed, _device(q, k, v, cu, out), q.data_ptr(), k.data_ptr(), v.data_ptr(), cu.data_ptr(),
              out.data_ptr(), T, R, H, kshape[1], D, qs, ks, vs, ys, D ** -0.5 if scale is None else float(scale))
     return out
+
+
+@functools.lru_cache(maxsize=256)
+def _kv4_workspace(*sizes) -> int:
+    """Bytes of ``attention_kv4``'s workspace, which follow from the sizes alone."""
+    n = _l(0)
+    _check(lib().qgemm_attention_kv4_workspace(*sizes, ctypes.byref(n)))
+    return n.value
 
 
 def attention_kv4(q: torch.Tensor, cache: torch.Tensor, block_table: torch.Tensor, kv_len: torch.Tensor,
@@ -616,13 +629,12 @@ def attention_kv4(q: torch.Tensor, cache: torch.Tensor, block_table: torch.Tenso
         _need(out, "out", _BF16, 3)
         if out.shape != q.shape:
             raise ValueError("out must have the shape of q")
-    n = _l(0)
-    _check(lib().qgemm_attention_kv4_workspace(T, R, H, Hkv, D, W, page, ctypes.byref(n)))
+    need = _kv4_workspace(T, R, H, Hkv, D, W, page)
     # of the call's own: torch's allocator keeps it from other streams, and inside a capture it is the graph's
-    ws = torch.empty(n.value, dtype=torch.uint8, device=q.device)
-    _enqueue(lib().qgemm_attention_kv4, _device(q, cache, block_table, kv_len, out), q, q.data_ptr(), cache.data_ptr(),
+    ws = torch.empty(need, dtype=torch.uint8, device=q.device)
+    _enqueue(lib().qgemm_attention_kv4, _device(q, cache, block_table, kv_len, out), q.data_ptr(), cache.data_ptr(),
              block_table.data_ptr(), kv_len.data_ptr(), None if cu_q is None else cu_q.data_ptr(), out.data_ptr(),
-             ws.data_ptr(), n.value, T, R, H, Hkv, D, W, pages, page, qs, D ** -0.5 if scale is None else float(scale))
+             ws.data_ptr(), need, T, R, H, Hkv, D, W, pages, page, qs, D ** -0.5 if scale is None else float(scale))
     return out
 
 

@@ -164,10 +164,9 @@ def test_calls_go_to_the_device_of_their_tensors(m, monkeypatch):
 
     monkeypatch.setattr(torch.cuda, "device", Guard)
     monkeypatch.setattr(m, "_current_device", lambda: current[0])
-    monkeypatch.setattr(m, "_stream", lambda t: 100 + t.get_device())
+    monkeypatch.setattr(m, "_stream_of", lambda dev: 100 + dev)
     for dev in (0, 3):
-        a = Fake(dev)
-        m._enqueue(lambda *x: seen.append((current[0], *x)) or 0, m._device(a, Fake(dev)), a, 7)
+        m._enqueue(lambda *x: seen.append((current[0], *x)) or 0, m._device(Fake(dev), Fake(dev)), 7)
     assert seen == [(0, 7, 100), (3, 7, 103)] and current == [0]
     with pytest.raises(ValueError, match="one device"):
         m._device(Fake(0), Fake(1))
