@@ -105,6 +105,11 @@ __device__ __forceinline__ Kv4Request kv4_request(const Kv4Args& a, int r, int G
   return q;
 }
 
+// The largest of three, NaN if one is (v_maximum3_f32: fmaxf would first quiet each of its arguments).
+__device__ __forceinline__ float max3(float x, float y, float z) {
+  return __builtin_elementwise_maximum(__builtin_elementwise_maximum(x, y), z);
+}
+
 __device__ __forceinline__ float max_over_groups(float x) {
   x = fmaxf(x, __shfl_xor(x, 16));
   return fmaxf(x, __shfl_xor(x, 32));
@@ -220,6 +225,11 @@ __device__ __forceinline__ void kv4_body(const Kv4Args& a) {
 
   const int page_mask = (1 << a.page_log2) - 1;
   const uint32_t page_bytes = (uint32_t)a.Hkv * ((uint32_t)(D + D / 16) << a.page_log2);     // (the host keeps it below 2^31)
+  // this lane's places within a record: key (or value) col of 16, its quarter of the row, that quarter's scale
+  const uint32_t k_off = (uint32_t)(col * (D / 2) + grp * (D / 8));
+  const uint32_t v_off = k_off + ((uint32_t)(D / 2) << a.page_log2);
+  const uint32_t ks_off = ((uint32_t)D << a.page_log2) + (uint32_t)(col * (D / 32) + (D == 128 ? grp : grp >> 1));
+  const uint32_t vs_off = ks_off + ((uint32_t)(D / 32) << a.page_log2);
   uint16_t* vw = vbuf[wave];
   auto vswz = [](int key) {
     const int low = 2 * (key & 3) | ((key >> 2) & 1);
@@ -277,23 +287,23 @@ __device__ __forceinline__ void kv4_body(const Kv4Args& a) {
           const int key = kKv4Step * s + 16 * i;
           const int id = i ? ids.y : ids.x;
           b.ok[i] = (unsigned)id < (unsigned)a.pages;
+          // the addresses' parts that all lanes share are scalar, the lanes' own do not change
           const uint8_t* rec = cache_h + (uint64_t)(b.ok[i] ? (uint32_t)id : 0u) * page_bytes;
-          const uint32_t off = (uint32_t)((key & page_mask) + col);
-          const uint32_t voff = off + (1u << a.page_log2);
-          const uint32_t sbase = (uint32_t)D << a.page_log2;
-          const uint32_t blk = D == 128 ? grp : grp >> 1;
+          const uint32_t in_page = (uint32_t)(key & page_mask);
+          const uint8_t* codes = rec + in_page * (D / 2);
+          const uint8_t* scales = rec + in_page * (D / 32);
           if constexpr (DW == 4) {
-            const u32x4 k4 = *reinterpret_cast<const u32x4*>(rec + (off * (D / 2) + grp * (D / 8)));
-            const u32x4 v4 = *reinterpret_cast<const u32x4*>(rec + (voff * (D / 2) + grp * (D / 8)));
+            const u32x4 k4 = *reinterpret_cast<const u32x4*>(codes + k_off);
+            const u32x4 v4 = *reinterpret_cast<const u32x4*>(codes + v_off);
 #pragma unroll
             for (int t = 0; t < DW; ++t) b.k[i][t] = k4[t], b.v[i][t] = v4[t];
           } else {
-            const uint2 k2 = *reinterpret_cast<const uint2*>(rec + (off * (D / 2) + grp * (D / 8)));
-            const uint2 v2 = *reinterpret_cast<const uint2*>(rec + (voff * (D / 2) + grp * (D / 8)));
+            const uint2 k2 = *reinterpret_cast<const uint2*>(codes + k_off);
+            const uint2 v2 = *reinterpret_cast<const uint2*>(codes + v_off);
             b.k[i][0] = k2.x, b.k[i][1] = k2.y, b.v[i][0] = v2.x, b.v[i][1] = v2.y;
           }
-          b.ks[i] = rec[sbase + off * (D / 32) + blk];
-          b.vs[i] = rec[sbase + voff * (D / 32) + blk];
+          b.ks[i] = scales[ks_off];
+          b.vs[i] = scales[vs_off];
         }
         return b;
       };
@@ -359,8 +369,8 @@ __device__ __forceinline__ void kv4_body(const Kv4Args& a) {
               for (int e = 0; e < 4; ++e)
                 if (key0 + 16 * i + 4 * grp + e >= lim[nt]) sc[nt][i][e] = -__builtin_inff();
           }
-          float mloc = fmaxf(fmaxf(fmaxf(sc[nt][0][0], sc[nt][0][1]), fmaxf(sc[nt][0][2], sc[nt][0][3])),
-                             fmaxf(fmaxf(sc[nt][1][0], sc[nt][1][1]), fmaxf(sc[nt][1][2], sc[nt][1][3])));
+          float mloc = max3(max3(sc[nt][0][0], sc[nt][0][1], sc[nt][0][2]), max3(sc[nt][0][3], sc[nt][1][0], sc[nt][1][1]),
+                            max3(sc[nt][1][2], sc[nt][1][3], sc[nt][1][3]));
           // The reference maximum moves, for all rows of the wave, only when some score passes its row's by more
           // than 8 in exp2 units: weights stay <= 2^8, and most steps exchange nothing between lanes.
           if (__any((mloc - m_run[nt]) * a.sl2 > 8.0f)) {
