@@ -7,6 +7,10 @@ carry the same names without the ``qgemm_`` prefix.
 
 The library must be built (``python -m paper_2607_19438_amd.build``); there is
 no fallback path, and a missing library raises ``QGemmError``.
+
+The serving functions' checks and allocations also exist compiled (``csrc/binding.cpp``, built
+beside the library): a call with good arguments on the current device goes that way where it
+is there. It answers ``NotImplemented`` to any other, and the code here says what is wrong.
 """
 from __future__ import annotations
 
@@ -64,6 +68,7 @@ class QGemmError(RuntimeError):
 
 
 _lib = None
+_fast = None      # the compiled way of the serving functions, once the library is loaded
 
 
 def lib_path() -> str:
@@ -72,7 +77,7 @@ def lib_path() -> str:
 
 def lib():
     """Load ``libqgemm.so`` (once) and declare every exported symbol's signature."""
-    global _lib
+    global _lib, _fast
     if _lib is None:
         if not os.path.exists(_LIB_PATH):
             raise QGemmError(-4, f"{_LIB_PATH} is not built; run `python -m paper_2607_19438_amd.build`")
@@ -82,7 +87,17 @@ def lib():
             fn.restype = res
             fn.argtypes = args
         _lib = handle
+        _fast = _compiled_way(handle)
     return _lib
+
+
+def _compiled_way(handle):
+    if _raw_stream is None or not os.path.exists(os.path.join(_HERE, "_binding.so")):
+        return None
+    from . import _binding
+    names = ("kv_plan", "rope", "kv4_store", "kv4_load", "attention_packed", "attention_kv4", "attention_kv4_workspace")
+    _binding.bind(_raw_stream, *[ctypes.cast(getattr(handle, "qgemm_" + n), ctypes.c_void_p).value for n in names])
+    return _binding
 
 
 def _check(rc: int):
@@ -455,6 +470,12 @@ def kv_plan(kv_len, q_len, block_table, free_pages, page: int, tokens: int, out:
     ``kv_len`` / ``q_len`` [R]: tokens in the cache / new ones; ``block_table`` [R][W] is updated in place from
     ``free_pages``; ``tokens``: rows of the step, those behind the last token have slot -1. ``out``: an earlier
     plan of the same sizes to write into."""
+    if _fast is not None and out is None:
+        r = _fast.kv_plan(kv_len, q_len, block_table, free_pages, page, tokens)
+        if r is not NotImplemented:
+            plan = KvPlan.__new__(KvPlan)
+            plan.cu_q, plan.kv_len, plan.used, plan.positions, plan.slots = r
+            return plan
     _need(kv_len, "kv_len", _I32, 1)
     _need(q_len, "q_len", _I32, 1)
     _need(block_table, "block_table", _I32, 2)
@@ -462,8 +483,8 @@ def kv_plan(kv_len, q_len, block_table, free_pages, page: int, tokens: int, out:
     R = kv_len.shape[0]
     if q_len.shape[0] != R or block_table.shape[0] != R:
         raise ValueError("kv_len, q_len and block_table disagree on the number of requests")
-    if tokens < 0:
-        raise ValueError("tokens must be >= 0")
+    if not (0 <= tokens < 1 << 31 and 0 < page < 1 << 31):
+        raise ValueError("tokens must be >= 0 and page > 0, both below 2^31")
     dev = _device(kv_len, q_len, block_table, free_pages)
     if out is None:
         out = KvPlan(R, tokens, kv_len.device)
@@ -504,11 +525,17 @@ def rope(x: torch.Tensor, positions: torch.Tensor, inv_freq: torch.Tensor, rot_h
     """Rotary positions on the first ``rot_heads`` heads of rows ``x`` [T][heads][D], fp32 or bf16, and their conversion
     to bf16 (``qgemm_rope``). The first ``2 * len(inv_freq)`` elements of a head are rotated, as pairs half of them
     apart or (``interleaved``) neighbouring. ``out``: bf16, may be a bf16 ``x`` itself."""
+    if _fast is not None:
+        r = _fast.rope(x, positions, inv_freq, rot_heads, interleaved, gain, out)
+        if r is not NotImplemented:
+            return r
     (T, heads, D), xs = _need_rows(x, "x", _ROWS)
     _need(positions, "positions", _I32, 1)
     _need(inv_freq, "inv_freq", _F64, 1)
     if positions.shape[0] != T:
         raise ValueError("x and positions disagree on T")
+    if not 0 <= rot_heads <= heads:
+        raise ValueError("rot_heads must lie in [0, heads]")
     if out is None:
         out = torch.empty((T, heads, D), dtype=torch.bfloat16, device=x.device)
         ys = heads * D
@@ -538,6 +565,8 @@ def _cache_sizes(cache: torch.Tensor, D: int):
 def kv4_store(k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, cache: torch.Tensor):
     """Quantises ``k``, ``v`` [T][Hkv][D] bf16 into the cache's ``slots`` [T] (``qgemm_kv4_store``); negative slots are
     skipped. ``cache``: uint8 of ``kv4_cache_shape``."""
+    if _fast is not None and _fast.kv4_store(k, v, slots, cache) is None:
+        return
     shape, ks = _need_rows(k, "k", _BF16)
     vshape, vs = _need_rows(v, "v", _BF16)
     _need(slots, "slots", _I32, 1)
@@ -552,6 +581,10 @@ def kv4_store(k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, cache: torc
 def kv4_load(cache: torch.Tensor, slots: torch.Tensor, D: int, k: torch.Tensor | None = None, v: torch.Tensor | None = None):
     """The keys and values of the cache's ``slots`` [T] as bf16 [T][Hkv][D] each (``qgemm_kv4_load``); rows of negative
     slots are left as they are in ``k`` and ``v``."""
+    if _fast is not None and k is None and v is None:
+        r = _fast.kv4_load(cache, slots, D)
+        if r is not NotImplemented:
+            return r
     _need(slots, "slots", _I32, 1)
     pages, Hkv, page = _cache_sizes(cache, D)
     shape = (slots.shape[0], Hkv, D)
@@ -575,6 +608,10 @@ def attention_packed(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu: torc
     """Causal attention over prompts packed end to end, prompt r in rows ``cu[r] .. cu[r+1]-1``
     (``qgemm_attention_packed``): q ``[T][H][D]``, k / v ``[T][Hkv][D]`` bf16, views of one projection row among
     them -> o ``[T][H][D]`` bf16. Rows behind the last prompt are not written."""
+    if _fast is not None:
+        r = _fast.attention_packed(q, k, v, cu, scale, out)
+        if r is not NotImplemented:
+            return r
     shape, qs = _need_rows(q, "q", _BF16)
     kshape, ks = _need_rows(k, "k", _BF16)
     vshape, vs = _need_rows(v, "v", _BF16)
@@ -611,6 +648,10 @@ def attention_kv4(q: torch.Tensor, cache: torch.Tensor, block_table: torch.Tenso
     ``[T][H][D]`` bf16. ``kv_len`` [R]: each request's keys, the new tokens' own (stored before) among them;
     ``cu_q`` [R+1]: first rows of the requests, or None where each has one token. Rows behind the last request
     are not written."""
+    if _fast is not None:
+        r = _fast.attention_kv4(q, cache, block_table, kv_len, cu_q, scale, out)
+        if r is not NotImplemented:
+            return r
     (T, H, D), qs = _need_rows(q, "q", _BF16)
     _need(block_table, "block_table", _I32, 2)
     _need(kv_len, "kv_len", _I32, 1)

@@ -1,4 +1,4 @@
-"""Build the gfx950 shared library ``libqgemm.so`` in-tree with hipcc.
+"""Build the gfx950 shared library ``libqgemm.so`` in-tree with hipcc, and the Python binding's compiled part.
 
 Usage: ``python -m paper_2607_19438_amd.build [--verbose]``.
 """
@@ -60,7 +60,36 @@ def build(verbose: bool = False, extra=None) -> str:
     return LIB
 
 
+BINDING = os.path.join(HERE, "_binding.so")
+BINDING_SOURCE = os.path.join(CSRC, "binding.cpp")
+
+
+def build_binding(verbose: bool = False) -> str:
+    """Compile the host code between Python and the library (the serving calls' checks and allocations) against the
+    installed torch; it replaces the old one in one step."""
+    import sysconfig
+
+    import torch
+    root = os.path.join(os.path.dirname(torch.__file__))
+    with tempfile.TemporaryDirectory(prefix="build-", dir=os.path.dirname(BINDING)) as tmp:
+        new = os.path.join(tmp, os.path.basename(BINDING))
+        cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-Wall",
+               f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-isystem", sysconfig.get_paths()["include"],
+               "-isystem", os.path.join(root, "include"), "-isystem", os.path.join(root, "include", "torch", "csrc", "api", "include"),
+               BINDING_SOURCE, "-o", new, "-L" + os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        res = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+        if res.returncode:
+            raise RuntimeError(f"{cmd[0]} failed ({res.returncode}):\n{res.stdout}")
+        if verbose and res.stdout.strip():
+            print(res.stdout)
+        os.replace(new, BINDING)
+    return BINDING
+
+
 if __name__ == "__main__":
     v = "--verbose" in sys.argv
     extra = ["-Rpass-analysis=kernel-resource-usage"] if "--resources" in sys.argv else None
     print(build(verbose=v or bool(extra), extra=extra))
+    print(build_binding(verbose=v))
