@@ -29,8 +29,10 @@ namespace {
 
 constexpr int kKv4Threads = 256;
 constexpr int kKv4Waves = kKv4Threads / 64;
-constexpr int kKv4Step = 32;                          // keys of a wave's step
-constexpr int kKv4Granule = kKv4Step * kKv4Waves;     // keys of a granule
+constexpr int kKv4StepLog2 = 5;
+constexpr int kKv4Step = 1 << kKv4StepLog2;           // keys of a wave's step
+constexpr int kKv4GranuleLog2 = 7;                    // keys of a granule at least: a step of every wave
+static_assert(1 << kKv4GranuleLog2 == kKv4Step * kKv4Waves, "a granule");
 constexpr int kKv4Bufs = 2;                           // steps of keys and values that a wave has in registers
 // What a unit's start (its queries and page numbers to fetch, its waves to join) counts in the split, in granules.
 // With 0 a workgroup of many short units is the last to end. Measured (us; 0, 1, 2, 4): 64 requests of 20 to 16000
@@ -62,6 +64,7 @@ struct Kv4Args {
   Kv4Head* head;            // [nwg]
   float* part;              // [nwg][2] partial results
   int T, R, H, Hkv, W, pages, page_log2, nwg;
+  int gran_log2;            // of the keys of a granule
   long qs;
   float sl2;
 };
@@ -83,7 +86,7 @@ struct Kv4Request {
   __device__ __forceinline__ void size(const Kv4Args& a, int G) {
     len = (int)min((long)kv, (long)a.W << a.page_log2);
     tiles = (n * G + 16 * NT - 1) / (16 * NT);
-    grans = max(1, (len + kKv4Granule - 1) / kKv4Granule);
+    grans = max(1, (len + (1 << a.gran_log2) - 1) >> a.gran_log2);
   }
   __device__ __forceinline__ unsigned int weight(int Hkv) const {
     return (unsigned)tiles * (unsigned)Hkv * (unsigned)(kKv4Start + grans);
@@ -273,7 +276,7 @@ __device__ __forceinline__ void kv4_body(const Kv4Args& a) {
       }
 
       const const_i32 trow = as_const(a.table) + (size_t)r * a.W;      // (indexed only if there is a key, so W >= 1)
-      const int s_end = min(a1 * kKv4Waves, (kmax + kKv4Step - 1) / kKv4Step);
+      const int s_end = min(a1 << (a.gran_log2 - kKv4StepLog2), (kmax + kKv4Step - 1) / kKv4Step);
       const uint8_t* cache_h = a.cache + (size_t)h * ((uint32_t)(D + D / 16) << a.page_log2);
       // pages of the two halves of a step (the last step's second half, or the step after it, may be past the table)
       auto pages_of = [&](int s) {
@@ -432,8 +435,8 @@ __device__ __forceinline__ void kv4_body(const Kv4Args& a) {
       // numbers of the next to be loaded. Every refill is issued, past the last step once more for that step: were
       // it skipped, the compiler could not tell how many loads are behind the one a step waits for, and would wait
       // for all of them.
-      if (a0 * kKv4Waves + wave < s_end) {
-        int s = a0 * kKv4Waves + wave, sl = s;
+      if ((a0 << (a.gran_log2 - kKv4StepLog2)) + wave < s_end) {
+        int s = (a0 << (a.gran_log2 - kKv4StepLog2)) + wave, sl = s;
         const int s_last = s + ((s_end - 1 - s) & ~(kKv4Waves - 1));
         int2 ids = pages_of(s);
         Kv4Keys<D> buf[kKv4Bufs];

@@ -68,6 +68,7 @@ constexpr long kCUs = 256;
 
 struct Kv4Plan {
   int nt;             // 16-row tiles that share a pass over the keys
+  int gran_log2;      // of the keys of a granule, which are not split
   int groups;         // workgroups
   long part_floats;   // of one partial result
 };
@@ -82,9 +83,21 @@ Kv4Plan kv4_plan(int T, int R, int H, int Hkv, int D, int W, int page) {
   // 33.7; 9 of 3 to 9 rows, 32/8 heads of 64 17.5, 17.2.)
   p.nt = rows <= 16 ? 1 : 2;
   const long tiles = ((long)T * G) / (16 * p.nt) + R;   // at least their number, requests of no tokens aside
-  const long grans = std::max<long>(1, qg::ceil_div((long)W * page, qg::kKv4Granule));
   // as many workgroups as the CUs hold at once, or fewer if there are not so many granules
   const long fill = kCUs * (p.nt == 2 ? qg::kKv4PerCU<128, 2> : D == 128 ? qg::kKv4PerCU<128, 1> : qg::kKv4PerCU<64, 1>);
+  // Short units are left whole: a granule as long as the longest, no second kernel, and no part to write. With more units
+  // than workgroups some of those would take two, so only very short ones. Measured (us, split, whole; by units and
+  // the longest request, lengths down to a thirtieth of it):
+  //   8 units, D=128    300 9.5, 7.3   500 9.6, 8.5    1000 9.8, 12.1
+  //   48                300 8.1, 6.5   500 9.0, 7.6    1000 10.1, 10.3 (12 requests 10.9, 10.2)  1500 10.4, 12.8
+  //   256               300 12.4, 7.6  500 13.4, 8.8   1000 14.1, 12.3  1500 15.6, 16.3
+  //   512, D=64         300 11.3, 7.4  500 12.4, 8.4   1000 13.8, 11.2  1500 14.8, 14.0  2000 16.4, 17.2
+  //   800, D=128        300 14.6, 13.2 500 15.9, 16.3  1000 20.0, 24.8
+  const long units = Hkv * std::max<long>(R, (long)T * G / (16 * p.nt)), most_keys = (long)W * page;
+  p.gran_log2 = qg::kKv4GranuleLog2;
+  if (most_keys <= (units > fill ? 256 : units >= 48 ? 1024 : 512))
+    while ((1L << p.gran_log2) < most_keys) ++p.gran_log2;
+  const long grans = std::max<long>(1, qg::ceil_div(most_keys, 1L << p.gran_log2));
   const long most = std::min(tiles, fill) * std::min<long>(Hkv, fill) * std::min(grans, fill);
   p.groups = (int)std::min(fill, most);
   p.part_floats = 16L * p.nt * (D + 2);
@@ -103,7 +116,7 @@ int check_kv4(int T, int R, int H, int Hkv, int D, int W, int page) {
   if ((long)W * page > (1 << 30)) return fail(QGEMM_EUNSUPPORTED, "W*page must be at most 2^30");
   if (R > (1 << 20)) return fail(QGEMM_EUNSUPPORTED, "more than 2^20 requests");
   // the kernel counts (16-row tile, key/value head, 128 keys) of all requests in 32 bits
-  const double grans = (double)std::max<long>(1, qg::ceil_div((long)W * page, qg::kKv4Granule)) + qg::kKv4Start;
+  const double grans = (double)std::max<long>(1, qg::ceil_div((long)W * page, 1L << qg::kKv4GranuleLog2)) + qg::kKv4Start;
   if ((double)((long)T * (H / Hkv) / 16 + R) * Hkv * grans >= 2147483648.0)
     return fail(QGEMM_EUNSUPPORTED, "T, R, Hkv and W*page are too large together");
   return QGEMM_OK;
@@ -383,8 +396,9 @@ int qgemm_attention_kv4(const void* q, const void* cache, const int32_t* block_t
   a.pages = pages;
   a.page_log2 = page_log2(page);
   a.nwg = plan.groups;
+  a.gran_log2 = plan.gran_log2;
   a.qs = q_stride;
-  const bool join = (long)W * page > qg::kKv4Granule;       // else every unit is one granule
+  const bool join = (long)W * page > (1L << plan.gran_log2);      // else every unit is one granule
   (void)hipGetLastError();
   rc = D == 128 ? launch_kv4_nt<128>(a, plan.nt, join, stream) : launch_kv4_nt<64>(a, plan.nt, join, stream);
   return rc == QGEMM_OK ? ok() : rc;
