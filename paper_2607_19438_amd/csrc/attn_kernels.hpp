@@ -31,7 +31,9 @@
 // row to i, so a workgroup walks the key blocks from the first row of its first row's prompt, and blocks on a
 // border are masked key by key as blocks on the diagonal are. ceil(T / rows) workgroups per head for any mix
 // of lengths (a tile per prompt would leave most of a tile empty for short ones), the number is known without
-// the lengths, and a border costs masked blocks in one tile only.
+// the lengths, and a border costs masked blocks in one tile only. Key blocks are walked from the last to the first.
+// Measured: prompts of 5204, 105, 2036 and 191 rows, 32/4 heads D=128 258 us (990 TFLOP/s), one of 4096 rows 138
+// (as a prompt by itself 148), 37 of 1 to 300 rows, 32/8 heads D=64 14.9.
 #pragma once
 
 #include "qgemm_kernels.hpp"

@@ -7,8 +7,9 @@
 // Work: a unit is (request, tile of 16 NT query rows, key/value head); the rows of a tile are the query heads
 // of the group times the request's new tokens. A unit's keys are cut into granules of 128, the granules of all
 // units (and a few more for the start of each) are numbered in one sequence, and workgroup w of n takes the w-th
-// n-th of them; n is what the CUs hold at once. So requests of any mix
-// of lengths load every workgroup alike, a long one is split over many, and the host needs to know no length.
+// n-th of them; n is what the CUs hold at once. So requests of any mix of lengths load every workgroup alike, a long
+// one is split over many, and the host needs to know no length. (Where the table is short a granule holds all of a
+// unit's keys: nothing is split then.)
 // A unit that lies in one workgroup is finished there; the others leave (output, maximum, sum) in the caller's
 // workspace, at most two per workgroup, and a second kernel joins them in granule order.
 //
@@ -19,6 +20,10 @@
 //   O^T += V^T P^T  the values need four keys of one dimension in a lane, so the unpacked rows go through
 //                a wave's own 32-row LDS tile and come back with the transposing read; no barrier is needed.
 // v_cvt_scalef32_pk_bf16_fp4 unpacks two levels and applies the block's scale in one instruction.
+//
+// Measured: 64 requests of 20 to 16000 keys, 32/8 heads of 128, 176 MB in 43 us (4.1 TB/s) and 4.5 us to join; one
+// request of 4097 keys, 32/4 heads, 6.3 us and 4.5; two chunks of 550 rows over 5000 keys, 32/8 heads, 157 us in all
+// (570 TFLOP/s).
 #pragma once
 
 #include "attn_kernels.hpp"
