@@ -437,6 +437,12 @@ def _device(first: torch.Tensor, *others) -> int:
     return dev
 
 
+def _sizes(*n):
+    """Sizes that the library counts in 32 bits (ctypes would cut them)."""
+    if max(n) >= 1 << 31:
+        raise ValueError("a size is 2^31 or more")
+
+
 def _stream_of(dev: int):
     return torch.cuda.current_stream(dev).cuda_stream if _raw_stream is None else _raw_stream(dev)
 
@@ -485,6 +491,7 @@ def kv_plan(kv_len, q_len, block_table, free_pages, page: int, tokens: int, out:
         raise ValueError("kv_len, q_len and block_table disagree on the number of requests")
     if not (0 <= tokens < 1 << 31 and 0 < page < 1 << 31):
         raise ValueError("tokens must be >= 0 and page > 0, both below 2^31")
+    _sizes(R, block_table.shape[1], free_pages.shape[0])
     dev = _device(kv_len, q_len, block_table, free_pages)
     if out is None:
         out = KvPlan(R, tokens, kv_len.device)
@@ -534,6 +541,7 @@ def rope(x: torch.Tensor, positions: torch.Tensor, inv_freq: torch.Tensor, rot_h
     _need(inv_freq, "inv_freq", _F64, 1)
     if positions.shape[0] != T:
         raise ValueError("x and positions disagree on T")
+    _sizes(T, heads, D)
     if not 0 <= rot_heads <= heads:
         raise ValueError("rot_heads must lie in [0, heads]")
     if out is None:
@@ -574,6 +582,7 @@ def kv4_store(k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, cache: torc
     pages, heads, page = _cache_sizes(cache, D)
     if vshape != shape or heads != Hkv or slots.shape[0] != T:
         raise ValueError("k, v, slots and cache disagree on T, Hkv or D")
+    _sizes(T, Hkv, D, pages, page)
     _enqueue(lib().qgemm_kv4_store, _device(k, v, slots, cache), k.data_ptr(), v.data_ptr(), slots.data_ptr(), cache.data_ptr(), T, Hkv,
              D, ks, vs, pages, page)
 
@@ -587,6 +596,7 @@ def kv4_load(cache: torch.Tensor, slots: torch.Tensor, D: int, k: torch.Tensor |
             return r
     _need(slots, "slots", _I32, 1)
     pages, Hkv, page = _cache_sizes(cache, D)
+    _sizes(slots.shape[0], Hkv, D, pages, page)
     shape = (slots.shape[0], Hkv, D)
     if k is None:
         k = torch.empty(shape, dtype=torch.bfloat16, device=cache.device)
@@ -620,6 +630,7 @@ def attention_packed(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu: torc
     if kshape != vshape or kshape[0] != T or kshape[2] != D:
         raise ValueError("q, k and v disagree on T or D")
     R = cu.shape[0] - 1
+    _sizes(T, H, D, R)
     if R < 0:
         raise ValueError("cu must have one entry more than there are prompts")
     if out is None:
@@ -657,6 +668,7 @@ def attention_kv4(q: torch.Tensor, cache: torch.Tensor, block_table: torch.Tenso
     _need(kv_len, "kv_len", _I32, 1)
     pages, Hkv, page = _cache_sizes(cache, D)
     R, W = block_table.shape
+    _sizes(T, H, D, R, W, pages, page)
     if kv_len.shape[0] != R or (cu_q is None and T != R):
         raise ValueError("q, block_table and kv_len disagree on the number of requests")
     if cu_q is not None:

@@ -223,19 +223,20 @@ inline bool attn_split(bool d64, bool causal, long S, long heads) {
 // the 128-row ones are few for the CUs, 2 of which a CU holds at D = 128 and 3 at D = 64. How few depends on how
 // uneven the chains are: with one or two prompts the longest is as long as T, or half of it, and decides; with
 // many of them all are short and the total does. Time of the 64-row form over that of the 128-row one, prompts of
-// one length, by the number of 128-row workgroups:
-//   D=128  R = 1    192 0.70  384 0.73  576 0.72-0.80  768 0.88-1.16  1024 1.20
-//          R = 3    256 0.86  384 0.97 (16 heads 0.72)  512 0.94  576 1.02  1024 0.98  1504 0.97-1.10
-//          R = 8    192 0.95 (8 heads 0.87)  256 0.93  288 0.94-1.09  384 1.05  576 1.03  1024 1.13
-//          R = 200  128 0.77  192 0.87  256 0.89  264 1.06  384 1.13  768 1.08
-//   D=64   R = 1    384 0.73  576 0.72  768 0.72 (24 heads 1.07)  1024 1.12  1504 0.98-1.11
-//          R = 3    384 0.80  576 0.83  768 0.83-0.89  1024 0.95  1504 0.90-1.08
-//          R = 8    288 0.83  384 0.89  432 0.86  512 1.08  576 1.03  768 1.14
-//          R = 200  256 0.87  352 0.88  384 0.89  432 1.12  576 1.12  1024 1.03
+// one length, 8 to 32 heads, by the number of 128-row workgroups:
+//   D=128  R = 1    192 0.76-0.82  320 0.78  432 0.85  512 0.88-0.94  576 0.99-1.03  768 1.14-1.20  1024 1.19-1.23
+//          R = 2    256 0.91-0.93  384 0.85-0.94  512 0.86-0.91  576 0.96-1.01  768 1.20
+//          R = 3    256 0.85-0.94  384 0.90-1.05  512 0.96-1.02  576 1.04-1.13  1024 1.08-1.14
+//          R = 5    192 0.87-0.94  256 0.89-0.96  288 1.02  384 1.05  576 1.03-1.12  1024 1.08-1.14
+//          R = 200  128 0.83  192 0.95-0.97  256 0.97  264 1.10  384 1.12  576 1.06-1.09
+//   D=64   R = 1    384 0.78-0.81  576 0.84-0.89  640 0.88  752 0.95  768 0.99-1.10  1024 1.18
+//          R = 3    256 0.83-0.94  384 0.90-1.00  432 0.91  512 0.81-0.89  576 1.02-1.06  768 0.89-0.91  1024 1.03-1.14
+//          R = 5    384 0.90-0.96  432 0.87  512 0.97-1.08  576 1.11  768 1.05-1.08
+//          R = 200  256 0.95  320 0.92  384 0.92  432 1.17  512 1.19  768 1.13
 inline bool attn_packed_split(bool d64, long T, long R, long heads) {
   const long wide = heads * ceil_div(T, 128);
-  if (d64) return wide <= (R <= 5 ? 768 : 400);
-  return wide <= (R <= 2 ? 640 : R <= 5 ? 512 : 256);
+  if (d64) return wide <= (R <= 2 ? 700 : R <= 5 ? 448 : 400);
+  return wide <= (R <= 2 ? 512 : R <= 3 ? 384 : 256);
 }
 
 }  // namespace qg

@@ -107,6 +107,26 @@ def test_all_codes_and_exponents_load():
         assert np.array_equal(got[ok], ref[ok])
 
 
+def test_a_slot_given_twice_touches_no_other():
+    """Which of the tokens it holds is not specified; every other slot is as without the second one."""
+    torch = torch_or_skip()
+    m = q()
+    x = torch.randn((8, 2, 64), device="cuda").to(torch.bfloat16)
+    slots = dev_i32(torch, [3, 9, 3, 20, 31, 9, 0, 3])
+    cache = torch.randint(0, 255, m.kv4_cache_shape(2, 2, 64, 16), device="cuda").to(torch.uint8)
+    before = [y.clone() for y in m.kv4_load(cache, torch.arange(32, dtype=torch.int32, device="cuda"), 64)]
+    m.kv4_store(x, x, slots, cache)
+    once = torch.zeros(m.kv4_cache_shape(2, 2, 64, 16), dtype=torch.uint8, device="cuda")
+    m.kv4_store(x, x, torch.arange(8, dtype=torch.int32, device="cuda"), once)
+    alone = m.kv4_load(once, torch.arange(8, dtype=torch.int32, device="cuda"), 64)
+    after = m.kv4_load(cache, torch.arange(32, dtype=torch.int32, device="cuda"), 64)
+    for b, a, o in zip(before, after, alone):
+        keep = [s for s in range(32) if s not in (3, 9, 20, 31, 0)]
+        assert torch.equal(a[keep].view(torch.int16), b[keep].view(torch.int16))
+        for s, t in ((20, 3), (31, 4), (0, 6)):
+            assert torch.equal(a[s], o[t])
+
+
 def test_nonfinite_blocks_are_nan_and_alone():
     torch = torch_or_skip()
     m = q()

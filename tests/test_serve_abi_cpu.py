@@ -172,6 +172,12 @@ def test_calls_go_to_the_device_of_their_tensors(m, monkeypatch):
         m._device(Fake(0), Fake(1))
 
 
+def test_sizes_past_31_bits_are_refused_not_cut(m):
+    m._sizes(1, (1 << 31) - 1)
+    with pytest.raises(ValueError, match="2\\^31"):
+        m._sizes(1, 1 << 31)
+
+
 def test_binding_refuses_host_tensors_and_shapes(m):
     import torch
     i = torch.zeros(4, dtype=torch.int32)
