@@ -399,6 +399,7 @@ int qgemm_attention_packed(const void* q, const void* k, const void* v, const in
  * qgemm_attention_kv4_workspace gives for the same sizes; it needs no
  * initialisation, and calls that can overlap need one each. W*page <= 2^30,
  * T*H*D < 2^31, R <= 2^20, (T*H/Hkv/16 + R) * Hkv * (W*page/128 + 2) < 2^31. R == 0 or T == 0 is a no-op.
+ * A cu_q that does not ascend gives unspecified rows.
  */
 int qgemm_attention_kv4(const void* q, const void* cache, const int32_t* block_table,
                         const int32_t* kv_len, const int32_t* cu_q, void* o, void* workspace,

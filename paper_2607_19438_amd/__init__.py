@@ -520,6 +520,7 @@ def rope_frequencies(rot: int, base: float = 10000.0, scaling: str = "none", fac
     the turns over it up to ``low`` of which a pair is divided by ``factor`` and from ``high`` on kept)."""
     if scaling not in _SCALINGS:
         raise ValueError(f"scaling must be one of {tuple(_SCALINGS)}")
+    _sizes(abs(rot))
     f = torch.empty(max(rot // 2, 1), dtype=torch.float64)
     gain = _f(1.0)
     _check(lib().qgemm_rope_frequencies(ctypes.cast(f.data_ptr(), ctypes.POINTER(_d)), ctypes.byref(gain), rot, base,
@@ -541,7 +542,7 @@ def rope(x: torch.Tensor, positions: torch.Tensor, inv_freq: torch.Tensor, rot_h
     _need(inv_freq, "inv_freq", _F64, 1)
     if positions.shape[0] != T:
         raise ValueError("x and positions disagree on T")
-    _sizes(T, heads, D)
+    _sizes(T, heads, D, 2 * inv_freq.shape[0])
     if not 0 <= rot_heads <= heads:
         raise ValueError("rot_heads must lie in [0, heads]")
     if out is None:
@@ -630,7 +631,7 @@ def attention_packed(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu: torc
     if kshape != vshape or kshape[0] != T or kshape[2] != D:
         raise ValueError("q, k and v disagree on T or D")
     R = cu.shape[0] - 1
-    _sizes(T, H, D, R)
+    _sizes(T, H, D, R, kshape[1])
     if R < 0:
         raise ValueError("cu must have one entry more than there are prompts")
     if out is None:

@@ -170,26 +170,34 @@ __device__ __forceinline__ void kv4_body(const Kv4Args& a) {
 
   // the workgroup's range of granules (a unit's start counted in), and the request that it begins in
   unsigned int total = 0, gs = 0, ge = 0;         // (the host keeps the largest possible total below 2^31)
+  constexpr unsigned int kNoSum = 0xffffffffu;
   unsigned int parts, each, more;                 // workgroups with work: `more` of each + 1 granules, then of each
   {
     const int per = (a.R + kKv4Threads - 1) / kKv4Threads;
     const int r0 = min(a.R, tid * per), r1 = min(a.R, r0 + per);
     unsigned int mine = 0;
-    for (int r = r0; r < r1; ++r) mine += kv4_request<NT>(a, r, G).weight(a.Hkv);
+    bool ascends = true;          // else requests share rows, and their work could pass what the host has bounded
+    for (int r = r0; r < r1; ++r) {
+      mine += kv4_request<NT>(a, r, G).weight(a.Hkv);
+      if (a.cu) ascends = ascends && as_const(a.cu)[r] <= as_const(a.cu)[r + 1];
+    }
+    const bool descent = __any(!ascends);
     unsigned int inc = mine;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
       const unsigned int up = __shfl_up(inc, d);
       if (lane >= d) inc += up;
     }
-    if (lane == 63) wsum[wave] = inc;
+    if (lane == 63) wsum[wave] = descent ? kNoSum : inc;
     __syncthreads();
-    unsigned int base = inc - mine;
+    unsigned int base = inc - mine, most = 0;
 #pragma unroll
     for (int i = 0; i < kKv4Waves; ++i) {
       if (i < wave) base += wsum[i];
       total += wsum[i];
+      most = max(most, wsum[i]);
     }
+    total = __builtin_amdgcn_readfirstlane(most == kNoSum ? 0u : total);      // then nothing is done
     parts = min((unsigned)a.nwg, total);
     each = parts ? total / parts : 0u;
     more = total - each * parts;

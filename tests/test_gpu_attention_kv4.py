@@ -195,6 +195,23 @@ def test_inconsistent_first_rows_stay_in_bounds():
         assert torch.all(buf[:32] == 9) and torch.all(buf[41:] == 9)
 
 
+def test_first_rows_that_descend_give_no_more_work_than_the_rows():
+    """Requests that share their rows, every second one with all of them: 10^10 granules if they were taken as they
+    are. The call ends, writes nothing outside its rows, and the next call is right."""
+    torch = torch_or_skip()
+    T, R, W = 4096, 2048, 1024
+    buf = torch.full((T + 64, 8, 64), 9.0, dtype=torch.bfloat16, device="cuda")
+    cache = torch.zeros(q().kv4_cache_shape(1, 1, 64, 1024), dtype=torch.uint8, device="cuda")
+    table = torch.zeros((R, W), dtype=torch.int32, device="cuda")
+    kv = torch.full((R,), W * 1024, dtype=torch.int32, device="cuda")
+    x = torch.zeros((T, 8, 64), dtype=torch.bfloat16, device="cuda")
+    cu = dev_i32(torch, [T * (r & 1) for r in range(R + 1)])
+    q().attention_kv4(x, cache, table, kv, cu, out=buf[32:-32])
+    torch.cuda.synchronize()
+    assert torch.all(buf[:32] == 9) and torch.all(buf[-32:] == 9)
+    check(torch, [300, 41], [3, 1], 8, 1, 64, 16, seed=17)
+
+
 def test_strided_queries_same_bits_every_time():
     torch = torch_or_skip()
     m = q()

@@ -178,6 +178,12 @@ def test_sizes_past_31_bits_are_refused_not_cut(m):
         m._sizes(1, 1 << 31)
 
 
+def test_rotated_sizes_past_31_bits_are_refused_not_cut(m):
+    for rot in ((1 << 32) + 64, 64 - (1 << 32), -(1 << 31)):
+        with pytest.raises(ValueError, match="2\\^31"):
+            m.rope_frequencies(rot, device="cpu")
+
+
 def test_binding_refuses_host_tensors_and_shapes(m):
     import torch
     i = torch.zeros(4, dtype=torch.int32)
