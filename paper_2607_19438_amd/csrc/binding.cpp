@@ -2,7 +2,7 @@
 // functions of the same names, for arguments that are as they should be and lie on the current device. For anything
 // else a function here answers NotImplemented, having done nothing, and the Python function goes its own way, which
 // says what is wrong. A decode step's calls take less time on the GPU than their checks take in Python: host time
-// of a call (us, Python alone and with this file) rope 6.8, 4.0; plan 8.4, 5.7; store and load 13.3, 7.7; packed
+// of a call (us, Python alone and with this file) rope 6.8, 4.0; plan 8.4, 4.9; store and load 13.3, 7.7; packed
 // prompts 6.3, 3.3; attention over the cache 10.6, 7.2; a launch is 2.4 of it, an allocation 0.6.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
@@ -107,6 +107,14 @@ int call(F&& f) {
   return rc;
 }
 
+// n elements of a dense tensor from `at` on, as a tensor of their own (five of them 0.7 us less than as views)
+at::Tensor piece(const at::Tensor& t, int64_t at, int64_t n) {
+  at::Tensor p = at::detail::make_tensor<c10::TensorImpl>(c10::TensorImpl::VIEW, c10::Storage(t.storage()), t.key_set(), t.dtype());
+  p.unsafeGetTensorImpl()->set_storage_offset(at);
+  p.unsafeGetTensorImpl()->set_sizes_contiguous({n});
+  return p;
+}
+
 // (kv_len, q_len, block_table, free_pages, page, tokens) -> (cu_q, kv_len, used, positions, slots)
 PyObject* kv_plan_(PyObject* const* a) {
   const at::Tensor *kv = tensor(a[0]), *ql = tensor(a[1]), *tab = tensor(a[2]), *fr = tensor(a[3]);
@@ -118,7 +126,6 @@ PyObject* kv_plan_(PyObject* const* a) {
   const int64_t R = kv->size(0), W = tab->size(1), F = fr->size(0);
   if (ql->size(0) != R || tab->size(0) != R || !small({R, W, F}) || !stream_of({kv, ql, tab, fr}, &s)) return not_here();
   const at::Tensor buf = at::empty({2 * R + 2 + 2 * (int64_t)T}, kv->options());
-  const auto out = buf.split_with_sizes({R + 1, R, 1, T, T});
   int32_t* p = static_cast<int32_t*>(buf.data_ptr());
   auto i32 = [](const at::Tensor* t) { return static_cast<int32_t*>(t->data_ptr()); };
   if (call([&] {
@@ -126,6 +133,8 @@ PyObject* kv_plan_(PyObject* const* a) {
                            (int)W, (int)F, page, T, s);
       }) != 0)
     return not_here();
+  const at::Tensor out[5] = {piece(buf, 0, R + 1), piece(buf, R + 1, R), piece(buf, 2 * R + 1, 1), piece(buf, 2 * R + 2, T),
+                             piece(buf, 2 * R + 2 + T, T)};
   PyObject* r = PyTuple_New(5);
   for (int i = 0; r && i < 5; ++i) PyTuple_SET_ITEM(r, i, THPVariable_Wrap(out[i]));
   return r;
