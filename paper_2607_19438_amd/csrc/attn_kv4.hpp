@@ -555,7 +555,7 @@ __device__ __forceinline__ void kv4_body(const Kv4Args& a) {
 }
 
 template <int D, int NT>
-constexpr int kKv4PerCU = NT == 2 ? 2 : D == 128 ? 3 : 4;      // workgroups that a CU holds, by the registers
+constexpr int kKv4PerCU = (D == 128 ? 3 : 4) - (NT - 1);      // workgroups that a CU holds, by the registers
 
 template <int D, int NT>
 __global__ __launch_bounds__(kKv4Threads, (kKv4PerCU<D, NT>)) void kv4_attn_kernel(Kv4Args a) {

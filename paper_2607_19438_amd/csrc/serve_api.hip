@@ -83,8 +83,16 @@ Kv4Plan kv4_plan(int T, int R, int H, int Hkv, int D, int W, int page) {
   // 33.7; 9 of 3 to 9 rows, 32/8 heads of 64 17.5, 17.2.)
   p.nt = rows <= 16 ? 1 : 2;
   const long tiles = ((long)T * G) / (16 * p.nt) + R;   // at least their number, requests of no tokens aside
-  // as many workgroups as the CUs hold at once, or fewer if there are not so many granules
-  const long fill = kCUs * (p.nt == 2 ? qg::kKv4PerCU<128, 2> : D == 128 ? qg::kKv4PerCU<128, 1> : qg::kKv4PerCU<64, 1>);
+  const long most_keys = (long)W * page;
+  // As many workgroups as the CUs hold at once, or fewer if there are not so many granules. Of the pairs of 64-wide tiles
+  // a CU holds three, which leaves each a third less of the work and more parts to join: taken from 24 granules of the
+  // longest table each. (us with two, three, by those granules and requests x tokens: 32/8 heads, 7 24 x 5-16 20.9, 22.4;
+  // 12 20 x 5-9 21.7, 22.8; 17 64 x 5-12 31.5, 32.2; 25 40 x 5-9 31.1, 30.3; 29 2 x 550 64.4, 61.8; 41 24 x 5-16 45.6,
+  // 43.3; 58 2 x 550 105.5, 96.6; 80 100 x 5-30 83.9, 77.5.)
+  long per_cu = D == 128 ? (p.nt == 2 ? qg::kKv4PerCU<128, 2> : qg::kKv4PerCU<128, 1>)
+                         : (p.nt == 2 ? qg::kKv4PerCU<64, 2> : qg::kKv4PerCU<64, 1>);
+  if (D == 64 && p.nt == 2 && tiles * Hkv * qg::ceil_div(most_keys, 1L << qg::kKv4GranuleLog2) < 24 * per_cu * kCUs) per_cu = 2;
+  const long fill = kCUs * per_cu;
   // Short units are left whole: a granule as long as the longest, no second kernel, and no part to write. With more units
   // than workgroups some of those would take two, so only very short ones. Measured (us, split, whole; by units and
   // the longest request, lengths down to a thirtieth of it):
@@ -93,7 +101,7 @@ Kv4Plan kv4_plan(int T, int R, int H, int Hkv, int D, int W, int page) {
   //   256               300 12.4, 7.6  500 13.4, 8.8   1000 14.1, 12.3  1500 15.6, 16.3
   //   512, D=64         300 11.3, 7.4  500 12.4, 8.4   1000 13.8, 11.2  1500 14.8, 14.0  2000 16.4, 17.2
   //   800, D=128        300 14.6, 13.2 500 15.9, 16.3  1000 20.0, 24.8
-  const long units = Hkv * std::max<long>(R, (long)T * G / (16 * p.nt)), most_keys = (long)W * page;
+  const long units = Hkv * std::max<long>(R, (long)T * G / (16 * p.nt));
   p.gran_log2 = qg::kKv4GranuleLog2;
   if (most_keys <= (units > fill ? 256 : units >= 48 ? 1024 : 512))
     while ((1L << p.gran_log2) < most_keys) ++p.gran_log2;

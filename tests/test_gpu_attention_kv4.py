@@ -101,6 +101,12 @@ def test_long_and_short_together(D, page):
     check(torch, kv, [4, 2, 5, 1, 3, 6], 16, 2, D, page, seed=8, rows=[0, 3, 4, 5, 6, 10, 11, 12, 14, 20])
 
 
+@pytest.mark.parametrize("width", [15, 120])
+def test_chunks_in_tables_of_either_length(width):
+    """Two chunks of prompts; the table's length, not the requests', chooses how many workgroups share them."""
+    check(torch_or_skip(), [900, 300], [300, 40], 32, 8, 64, 64, seed=18, rows=[0, 7, 150, 298, 299, 300, 301, 339], width=width)
+
+
 @pytest.mark.parametrize("std", [4.0, 16.0])
 def test_sharp(std):
     check(torch_or_skip(), [500, 77], [1, 1], 8, 2, 128, 16, seed=5, std=std)
