@@ -81,7 +81,12 @@ Kv4Plan kv4_plan(int T, int R, int H, int Hkv, int D, int W, int page) {
   // has the registers of a whole SIMD. (us, one tile, two, four: 2 chunks of 550 rows, 5000 keys, 32/8 heads of 128
   // 190, 159, 199; 6 requests of 8 to 32 rows and 32/4 heads 43.2, 41.5, 49.3; 16 of 6 rows and 32/8 heads 38.3,
   // 33.7; 9 of 3 to 9 rows, 32/8 heads of 64 17.5, 17.2.)
-  p.nt = rows <= 16 ? 1 : 2;
+  // Wide tiles unpack a key once for 128 rows, but each part of one is eight times a small tile's: taken where requests
+  // fill them and there are almost as many as workgroups, so that few are split. (us, pairs of tiles and wide, 32/8 heads
+  // of 128: chunks of 550 rows over 5000 keys 150, 131; 200 to 1500 over 12000 586, 436; a first chunk of 1000 45.8,
+  // 31.1; 4 of 60 to 300 rows 86.1, 86.0; 12 of 64 to 128 rows 52.6, 59.1; one of 256 over 4000 45.6, 48.2.)
+  const bool wide = rows >= 512 && (long)T * G / (16 * qg::kKv4Wide) * Hkv >= 208;
+  p.nt = rows <= 16 ? 1 : wide ? qg::kKv4Wide : 2;
   const long tiles = ((long)T * G) / (16 * p.nt) + R;   // at least their number, requests of no tokens aside
   const long most_keys = (long)W * page;
   // As many workgroups as the CUs hold at once, or fewer if there are not so many granules. Of the pairs of 64-wide tiles
@@ -89,8 +94,9 @@ Kv4Plan kv4_plan(int T, int R, int H, int Hkv, int D, int W, int page) {
   // longest table each. (us with two, three, by those granules and requests x tokens: 32/8 heads, 7 24 x 5-16 20.9, 22.4;
   // 12 20 x 5-9 21.7, 22.8; 17 64 x 5-12 31.5, 32.2; 25 40 x 5-9 31.1, 30.3; 29 2 x 550 64.4, 61.8; 41 24 x 5-16 45.6,
   // 43.3; 58 2 x 550 105.5, 96.6; 80 100 x 5-30 83.9, 77.5.)
-  long per_cu = D == 128 ? (p.nt == 2 ? qg::kKv4PerCU<128, 2> : qg::kKv4PerCU<128, 1>)
-                         : (p.nt == 2 ? qg::kKv4PerCU<64, 2> : qg::kKv4PerCU<64, 1>);
+  long per_cu = wide       ? qg::kKv4PerCU<128, qg::kKv4Wide>
+                : D == 128 ? (p.nt == 2 ? qg::kKv4PerCU<128, 2> : qg::kKv4PerCU<128, 1>)
+                           : (p.nt == 2 ? qg::kKv4PerCU<64, 2> : qg::kKv4PerCU<64, 1>);
   if (D == 64 && p.nt == 2 && tiles * Hkv * qg::ceil_div(most_keys, 1L << qg::kKv4GranuleLog2) < 24 * per_cu * kCUs) per_cu = 2;
   const long fill = kCUs * per_cu;
   // Short units are left whole: a granule as long as the longest, no second kernel, and no part to write. With more units
@@ -142,7 +148,8 @@ int launch_kv4(const qg::Kv4Args& a, bool join, hipStream_t s) {
 
 template <int D>
 int launch_kv4_nt(const qg::Kv4Args& a, int nt, bool join, hipStream_t s) {
-  return nt == 1 ? launch_kv4<D, 1>(a, join, s) : launch_kv4<D, 2>(a, join, s);
+  if (nt == 1) return launch_kv4<D, 1>(a, join, s);
+  return nt == 2 ? launch_kv4<D, 2>(a, join, s) : launch_kv4<D, qg::kKv4Wide>(a, join, s);
 }
 
 }  // namespace

@@ -107,6 +107,66 @@ def test_chunks_in_tables_of_either_length(width):
     check(torch_or_skip(), [900, 300], [300, 40], 32, 8, 64, 64, seed=18, rows=[0, 7, 150, 298, 299, 300, 301, 339], width=width)
 
 
+CHUNKS = [  # kv lengths, new tokens, H, Hkv, D, page, table width: 128 query rows to a tile
+    ([900, 500], [400, 433], 32, 8, 128, 16, None), ([1100], [833], 32, 4, 64, 64, 40), ([70, 0, 640, 9], [130, 0, 300, 9], 66, 2, 64, 16, None),
+    ([600], [520], 64, 64, 128, 32, None), ([417, 100], [417, 416], 32, 8, 64, 256, 60), ([5000, 64], [800, 40], 32, 8, 128, 128, None),
+]
+
+
+@pytest.mark.parametrize("kv,new,H,Hkv,D,page,width", CHUNKS)
+def test_chunks(kv, new, H, Hkv, D, page, width):
+    """Every border of a request and some rows between; [417, 100] has rows before the cache's start."""
+    cu = starts(new)
+    rows = sorted({t for c in cu for t in (c - 1, c, c + 1, c + 31, c + 33) if 0 <= t < cu[-1]} | {cu[-1] // 3, cu[-1] // 2})
+    rows = [t for t in rows if kv[int(np.searchsorted(cu, t, side="right") - 1)] - (cu[int(np.searchsorted(cu, t, side="right"))] - 1 - t) > 0]
+    out = check(torch_or_skip(), kv, new, H, Hkv, D, page, seed=19, pad=3, rows=rows, width=width)
+    for r, n in enumerate(new):
+        blind = max(0, n - kv[r])
+        assert not out[cu[r]:cu[r] + blind].any()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_what_pages_hold_behind_a_chunk_reaches_nothing(D):
+    """As below for tiles of 128 rows: NaN behind the last key changes no bit; NaN keys, values and pages reach the rows
+    that see them, a value block its own dimensions only."""
+    torch = torch_or_skip()
+    kv, new, H, Hkv, page = [470, 450], [430, 420], 32, 8, 16
+    case = make(kv, new, H, Hkv, D, page, seed=20)
+    table, cache, k, v, qn, bits, cu = case
+    clean = run(torch, case, kv, cu)
+    n0, sb = page * D, D // 32
+    dirty = cache.copy()
+    for r in range(2):
+        for p in range(kv[r], len(table[r]) * page):
+            if table[r, p // page] >= 0:
+                at = n0 + (p % page) * sb
+                dirty[table[r, p // page], :, at:at + sb] = 255
+                dirty[table[r, p // page], :, at + page * sb:at + page * sb + sb] = 255
+    assert torch.equal(run(torch, (table, dirty, k, v, qn, bits, cu), kv, cu), clean)
+    # request 0: a NaN value block of position 100 (first seen by token 60); request 1: a NaN key of position 200 (170)
+    for byte in (255, 254):
+        dirty[table[0, 100 // page], :, n0 + (page + 100 % page) * sb + 1] = byte
+        dirty[table[1, 200 // page], :, n0 + (200 % page) * sb] = 255
+        o = run(torch, (table, dirty, k, v, qn, bits, cu), kv, cu).float()
+        c = clean.float()
+        assert torch.equal(o[:60], c[:60]) and torch.equal(o[430:600], c[430:600])
+        assert torch.isnan(o[60:430, :, 32:64]).all() and torch.isnan(o[600:]).all()
+        keep = [i for i in range(D) if not 32 <= i < 64]
+        assert torch.equal(o[60:430][..., keep], c[60:430][..., keep])
+    wild = table.copy()
+    wild[0, 5] = len(cache)                      # positions 80 .. 95: token 40 is the first to see one
+    o = run(torch, (wild, cache, k, v, qn, bits, cu), kv, cu).float()
+    assert torch.equal(o[:40], clean[:40].float()) and torch.isnan(o[40:430]).all() and torch.equal(o[430:], clean[430:].float())
+
+
+def test_chunks_give_the_same_bits_every_time():
+    torch = torch_or_skip()
+    case = make([3000, 700], [600, 240], 32, 8, 64, 16, seed=21)
+    first = run(torch, case, [3000, 700], case[-1])
+    for _ in range(3):
+        assert torch.equal(run(torch, case, [3000, 700], case[-1]), first)
+
+
 @pytest.mark.parametrize("std", [4.0, 16.0])
 def test_sharp(std):
     check(torch_or_skip(), [500, 77], [1, 1], 8, 2, 128, 16, seed=5, std=std)
