@@ -189,7 +189,7 @@ __device__ __forceinline__ void kv4_wide(const Kv4Args& a, const Kv4Request& rq,
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) acc[dt] = f32x16{};
   float m_run = -__builtin_inff();
-  float l_run = rq.kv > rq.len ? __builtin_nanf("") : 0.0f;       // keys without a page to look in
+  float l_run = live && rq.kv - rq.n + rho / G >= rq.len ? __builtin_nanf("") : 0.0f;       // sees keys past the table
 
   const const_i32 trow = as_const(a.table) + (size_t)r * a.W;     // (indexed only if there is a key, so W >= 1)
   const int page_mask = (1 << a.page_log2) - 1;
@@ -520,12 +520,14 @@ __device__ __forceinline__ void kv4_body(const Kv4Args& a) {
         const int nrows = rq.n * G;
         int lim[NT];                                    // keys that the row sees
         bf16x8 qf[NT][DW];
+        f32x4 l_run[NT];                              // sum of the weights as they enter the product, four times
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
           const int rho = row0 + 16 * nt + col;
           const int i = rho / G;
           const bool live = rho < nrows;
           lim[nt] = live ? clamp_i(rq.kv - rq.n + i + 1, 0, rq.len) : 0;
+          l_run[nt] = f32x4{} + (live && rq.kv - rq.n + i >= rq.len ? __builtin_nanf("") : 0.0f);     // sees keys past the table
           const uint16_t* qp = a.q + (size_t)(rq.c0 + i) * a.qs + (size_t)(h * G + (rho - i * G)) * D + grp * (D / 4);
 #pragma unroll
           for (int t = 0; t < DW; ++t)
@@ -537,11 +539,9 @@ __device__ __forceinline__ void kv4_body(const Kv4Args& a) {
 
         f32x4 acc[NT][DT];
         float m_run[NT];
-        f32x4 l_run[NT];                              // sum of the weights as they enter the product, four times
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
           m_run[nt] = -__builtin_inff();
-          l_run[nt] = f32x4{} + (rq.kv > rq.len ? __builtin_nanf("") : 0.0f);   // keys without a page to look in
 #pragma unroll
           for (int dt = 0; dt < DT; ++dt) acc[nt][dt] = f32x4{};
         }

@@ -234,6 +234,27 @@ def test_missing_pages_are_nan():
     assert torch.isfinite(o[0]).all() and torch.all(o[1] == 0) and torch.isnan(o[2]).all() and torch.isfinite(o[3]).all()
 
 
+@pytest.mark.parametrize("H,Hkv,new,pages", [(4, 1, 5, 13), (32, 8, 840, 53)])
+def test_rows_before_the_end_of_a_short_table_are_whole(H, Hkv, new, pages):
+    """Two keys more than the table has pages for: the last two rows are NaN, those before as in the oracle."""
+    torch = torch_or_skip()
+    kv = pages * 16
+    case = make([kv], [new], H, Hkv, 64, 16, seed=22, width=pages)
+    table, cache, k, v, qn, bits, cu = case
+    o = host_bf16(torch, run(torch, case, [kv + 2], cu))
+    assert np.isnan(o[-2:]).all() and np.isfinite(o[:-2]).all()
+    kk, vv = oracle.gather_cache(k, v, table[0], kv, 16)
+    t = new - 3                                             # sees exactly the table's keys
+    ref, absv = np.zeros((1, H, 64)), np.zeros((1, H, 64))
+    for h in range(H):
+        g = h // (H // Hkv)
+        s = kk[:, g] @ qn[t, h] * 64 ** -0.5
+        p = np.exp(s - s.max())
+        p /= p.sum()
+        ref[0, h], absv[0, h] = p @ vv[:, g], p @ np.abs(vv[:, g])
+    assert oracle.attn_ratio(o[t:t + 1], ref, absv) <= 1.0
+
+
 def test_tables_of_no_pages():
     torch = torch_or_skip()
     m = q()
