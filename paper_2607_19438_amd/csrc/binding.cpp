@@ -98,13 +98,21 @@ bool cache_sizes(const at::Tensor* c, int64_t D, int* pages, int* Hkv, int* page
   return true;
 }
 
+// A tensor's memory, null for none; throws for a tensor that has no memory (one inside torch.vmap, say), so it is
+// read before the interpreter's lock is let go.
+template <typename T = void>
+T* memory(const at::Tensor* t) {
+  return t ? static_cast<T*>(t->data_ptr()) : nullptr;
+}
+
+// Calls f without the interpreter's lock (a launch may wait for room in the queue), which is held again however f ends.
 template <typename F>
 int call(F&& f) {
-  int rc;
-  Py_BEGIN_ALLOW_THREADS  // (a launch may wait for room in the queue)
-  rc = f();
-  Py_END_ALLOW_THREADS
-  return rc;
+  struct Unlocked {
+    PyThreadState* state = PyEval_SaveThread();
+    ~Unlocked() { PyEval_RestoreThread(state); }
+  } unlocked;
+  return f();
 }
 
 // n elements of a dense tensor from `at` on, as a tensor of their own (five of them 0.7 us less than as views)
@@ -126,11 +134,11 @@ PyObject* kv_plan_(PyObject* const* a) {
   const int64_t R = kv->size(0), W = tab->size(1), F = fr->size(0);
   if (ql->size(0) != R || tab->size(0) != R || !small({R, W, F}) || !stream_of({kv, ql, tab, fr}, &s)) return not_here();
   const at::Tensor buf = at::empty({2 * R + 2 + 2 * (int64_t)T}, kv->options());
-  int32_t* p = static_cast<int32_t*>(buf.data_ptr());
-  auto i32 = [](const at::Tensor* t) { return static_cast<int32_t*>(t->data_ptr()); };
+  int32_t *p = memory<int32_t>(&buf), *kvp = memory<int32_t>(kv), *qp = memory<int32_t>(ql), *tp = memory<int32_t>(tab),
+          *fp = memory<int32_t>(fr);
   if (call([&] {
-        return lib.kv_plan(i32(kv), i32(ql), i32(tab), i32(fr), p, p + 2 * R + 2, p + 2 * R + 2 + T, p + R + 1, p + 2 * R + 1, (int)R,
-                           (int)W, (int)F, page, T, s);
+        return lib.kv_plan(kvp, qp, tp, fp, p, p + 2 * R + 2, p + 2 * R + 2 + T, p + R + 1, p + 2 * R + 1, (int)R, (int)W, (int)F, page,
+                           T, s);
       }) != 0)
     return not_here();
   const at::Tensor out[5] = {piece(buf, 0, R + 1), piece(buf, R + 1, R), piece(buf, 2 * R + 1, 1), piece(buf, 2 * R + 2, T),
@@ -159,12 +167,11 @@ PyObject* rope_(PyObject* const* a) {
   } else if (!rows(o, &ys) || o->scalar_type() != at::kBFloat16 || o->sizes() != x->sizes()) {
     return not_here();
   }
-  void* y = o ? o->data_ptr() : made.data_ptr();
-  if (call([&] {
-        return lib.rope(x->data_ptr(), x->scalar_type() == at::kBFloat16 ? QGEMM_BF16 : QGEMM_F32, static_cast<const int32_t*>(pos->data_ptr()),
-                        static_cast<const double*>(f->data_ptr()), y, (int)T, (int)heads, rot_heads, (int)D, (int)(2 * f->size(0)), xs, ys,
-                        a[4] == Py_True, gain, s);
-      }) != 0)
+  void *y = memory(o ? o : &made), *xp = memory(x);
+  const int32_t* pp = memory<int32_t>(pos);
+  const double* fp = memory<double>(f);
+  const int type = x->scalar_type() == at::kBFloat16 ? QGEMM_BF16 : QGEMM_F32, rot = (int)(2 * f->size(0)), inter = a[4] == Py_True;
+  if (call([&] { return lib.rope(xp, type, pp, fp, y, (int)T, (int)heads, rot_heads, (int)D, rot, xs, ys, inter, gain, s); }) != 0)
     return not_here();
   return o ? Py_NewRef(a[6]) : THPVariable_Wrap(made);
 }
@@ -179,10 +186,10 @@ PyObject* kv4_store_(PyObject* const* a) {
       v->sizes() != k->sizes() || !cache_sizes(c, k->size(2), &pages, &Hkv, &page) || Hkv != k->size(1) || sl->size(0) != k->size(0) ||
       !small({k->size(0)}) || !stream_of({k, v, sl, c}, &s))
     return not_here();
-  if (call([&] {
-        return lib.store(k->data_ptr(), v->data_ptr(), static_cast<const int32_t*>(sl->data_ptr()), c->data_ptr(), (int)k->size(0), Hkv,
-                         (int)k->size(2), ks, vs, pages, page, s);
-      }) != 0)
+  void *kp = memory(k), *vp = memory(v), *cp = memory(c);
+  const int32_t* sp = memory<int32_t>(sl);
+  const int T = (int)k->size(0), D = (int)k->size(2);
+  if (call([&] { return lib.store(kp, vp, sp, cp, T, Hkv, D, ks, vs, pages, page, s); }) != 0)
     return not_here();
   Py_RETURN_NONE;
 }
@@ -198,9 +205,9 @@ PyObject* kv4_load_(PyObject* const* a) {
   const int64_t T = sl->size(0);
   const auto opt = c->options().dtype(at::kBFloat16);
   const at::Tensor k = at::empty({T, Hkv, D}, opt), v = at::empty({T, Hkv, D}, opt);
-  if (call([&] {
-        return lib.load(c->data_ptr(), static_cast<const int32_t*>(sl->data_ptr()), k.data_ptr(), v.data_ptr(), (int)T, Hkv, D, pages, page, s);
-      }) != 0)
+  void *kp = memory(&k), *vp = memory(&v), *cp = memory(c);
+  const int32_t* sp = memory<int32_t>(sl);
+  if (call([&] { return lib.load(cp, sp, kp, vp, (int)T, Hkv, D, pages, page, s); }) != 0)
     return not_here();
   PyObject* r = PyTuple_New(2);
   if (r) {
@@ -230,11 +237,10 @@ PyObject* attention_packed_(PyObject* const* a) {
   } else if (!rows(o, &ys) || o->scalar_type() != at::kBFloat16 || o->sizes() != q->sizes()) {
     return not_here();
   }
-  void* y = o ? o->data_ptr() : made.data_ptr();
-  if (call([&] {
-        return lib.packed(q->data_ptr(), k->data_ptr(), v->data_ptr(), static_cast<const int32_t*>(cu->data_ptr()), y, (int)T, (int)R, (int)H,
-                          (int)k->size(1), (int)D, qs, ks, vs, ys, scale, s);
-      }) != 0)
+  void *y = memory(o ? o : &made), *qp = memory(q), *kp = memory(k), *vp = memory(v);
+  const int32_t* cp = memory<int32_t>(cu);
+  const int Hkv = (int)k->size(1);
+  if (call([&] { return lib.packed(qp, kp, vp, cp, y, (int)T, (int)R, (int)H, Hkv, (int)D, qs, ks, vs, ys, scale, s); }) != 0)
     return not_here();
   return o ? Py_NewRef(a[5]) : THPVariable_Wrap(made);
 }
@@ -261,11 +267,10 @@ PyObject* attention_kv4_(PyObject* const* a) {
   if (!o) made = at::empty({T, H, D}, q->options());
   // of the call's own: torch's allocator keeps it from other streams, and inside a capture it is the graph's
   const at::Tensor ws = at::empty({need}, q->options().dtype(at::kByte));
-  void* y = o ? o->data_ptr() : made.data_ptr();
+  void *y = memory(o ? o : &made), *qp = memory(q), *cp = memory(c), *wp = memory(&ws);
+  const int32_t *tp = memory<int32_t>(tab), *kp = memory<int32_t>(kv), *up = memory<int32_t>(cu);
   if (call([&] {
-        return lib.kv4(q->data_ptr(), c->data_ptr(), static_cast<const int32_t*>(tab->data_ptr()), static_cast<const int32_t*>(kv->data_ptr()),
-                       cu ? static_cast<const int32_t*>(cu->data_ptr()) : nullptr, y, ws.data_ptr(), need, (int)T, (int)R, (int)H, Hkv, (int)D,
-                       (int)W, pages, page, qs, scale, s);
+        return lib.kv4(qp, cp, tp, kp, up, y, wp, need, (int)T, (int)R, (int)H, Hkv, (int)D, (int)W, pages, page, qs, scale, s);
       }) != 0)
     return not_here();
   return o ? Py_NewRef(a[6]) : THPVariable_Wrap(made);
