@@ -292,7 +292,8 @@ int qgemm_attention_prefill(const void* q, const void* k, const void* v, void* o
  *   used[0] = sum of (need - have); rows at or past cu_q[R]: position 0, slot -1
  * kv_len, q_len, total_len: int32 [R]; block_table: int32 [R][W]; free_pages:
  * int32 [F]; cu_q: int32 [R+1]; positions, slots: int32 [T]; used: int32 [1].
- * Outputs alias no input but block_table. Where the free list ends (used[0] > F)
+ * No array that is written (block_table too) may share memory with another: a total_len that is the next
+ * step's kv_len needs a second one to be written there (QGEMM_EINVAL otherwise). Where the free list ends (used[0] > F)
  * table entries become -1; such a token, one past W pages, one of a negative
  * table entry and one whose slot is 2^31 or more have slot -1. Tokens past T are
  * not planned (nor the pages that begin with them). R <= 4096.

@@ -479,7 +479,8 @@ def kv_plan(kv_len, q_len, block_table, free_pages, page: int, tokens: int, out:
 
     ``kv_len`` / ``q_len`` [R]: tokens in the cache / new ones; ``block_table`` [R][W] is updated in place from
     ``free_pages``; ``tokens``: rows of the step, those behind the last token have slot -1. ``out``: an earlier
-    plan of the same sizes to write into."""
+    plan of the same sizes to write into, with no tensor of it among the inputs: where ``kv_len`` is a plan's, ``out`` is
+    another plan (two that take turns), else the call is refused."""
     if _fast is not None and out is None:
         r = _fast.kv_plan(kv_len, q_len, block_table, free_pages, page, tokens)
         if r is not NotImplemented:

@@ -60,6 +60,27 @@ int check_rows(const char* name, const void* p, int64_t stride, int64_t row, int
   return QGEMM_OK;
 }
 
+// A plan's tables: none that is written may share memory with another, as workgroups write while others still read.
+struct PlanTable {
+  const char* name;
+  const int32_t* at;
+  int64_t n;
+};
+
+int check_apart(const PlanTable* written, int n_written, const PlanTable* read, int n_read) {
+  auto overlap = [](const PlanTable& a, const PlanTable& b) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a.at), y = reinterpret_cast<uintptr_t>(b.at);
+    return a.n > 0 && b.n > 0 && x < y + 4 * (uintptr_t)b.n && y < x + 4 * (uintptr_t)a.n;
+  };
+  for (int i = 0; i < n_written; ++i) {
+    for (int j = 0; j < i; ++j)
+      if (overlap(written[i], written[j])) return fail(QGEMM_EINVAL, "%s and %s overlap", written[j].name, written[i].name);
+    for (int j = 0; j < n_read; ++j)
+      if (overlap(written[i], read[j])) return fail(QGEMM_EINVAL, "%s, which is written, overlaps %s", written[i].name, read[j].name);
+  }
+  return QGEMM_OK;
+}
+
 // ---------------------------------------------------------------------------
 // attention over the cache: how many workgroups, and how many rows in a tile
 // ---------------------------------------------------------------------------
@@ -169,12 +190,17 @@ int qgemm_kv_plan(const int32_t* kv_len, const int32_t* q_len, int32_t* block_ta
   for (const void* p : {(const void*)kv_len, (const void*)q_len, (const void*)block_table, (const void*)free_pages,
                         (const void*)cu_q, (const void*)positions, (const void*)slots, (const void*)total_len, (const void*)used})
     if (!aligned(p, 4)) return fail(QGEMM_EALIGN, "the tables must be 4-byte aligned");
+  const PlanTable written[] = {{"block_table", block_table, (int64_t)R * W}, {"cu_q", cu_q, R + 1}, {"positions", positions, T},
+                               {"slots", slots, T},                          {"total_len", total_len, R}, {"used", used, 1}};
+  const PlanTable read[] = {{"kv_len", kv_len, R}, {"q_len", q_len, R}, {"free_pages", free_pages, F}};
+  int rc = check_apart(written, 6, read, 3);
+  if (rc != QGEMM_OK) return rc;
   (void)hipGetLastError();
   const qg::PlanArgs a{kv_len, q_len, block_table, free_pages, cu_q, positions, slots, total_len, used,
                        R,      W,     F,           page_log2(page), T};
   const unsigned groups = (unsigned)std::max<long>(1, qg::ceil_div(T, qg::kPlanTokens));
   hipLaunchKernelGGL(qg::kv_plan_kernel, dim3(groups), dim3(qg::kPlanThreads), (size_t)R * 3 * sizeof(int32_t), stream, a);
-  const int rc = check_launch("qgemm_kv_plan");
+  rc = check_launch("qgemm_kv_plan");
   return rc == QGEMM_OK ? ok() : rc;
 }
 

@@ -69,6 +69,34 @@ def test_plan_slots_past_31_bits_are_refused():
     check(torch, [0, 3], [1, 1], [[0], [2 ** 27 - 1]], [2 ** 27], 16, 2)
 
 
+def test_a_plan_is_not_written_over_its_own_input():
+    """Lengths fed back into the plan that they come from: refused, nothing written. Two plans in turn: as the oracle."""
+    torch = torch_or_skip()
+    m = q()
+    R, T, W, page = 300, 900, 40, 16
+    rng = np.random.default_rng(5)
+    kv = rng.integers(0, 400, R)
+    new = np.full(R, 3)
+    table = np.full((R, W), -1)
+    table[:, :25] = np.arange(R * 25).reshape(R, 25)
+    free = np.arange(1000) + 20000
+    tab, freed, newd = dev_i32(torch, table), dev_i32(torch, free), dev_i32(torch, new)
+    plans, kvd, at = (m.KvPlan(R, T, "cuda"), m.KvPlan(R, T, "cuda")), dev_i32(torch, kv), 0
+    for step in range(6):
+        want = oracle.kv_plan(kv, new, table, free[at:], page, T)
+        p = m.kv_plan(kvd, newd, tab, freed[at:].contiguous(), page, T, out=plans[step & 1])
+        for got, ref in zip((p.cu_q, p.positions, p.slots, tab, p.kv_len, p.used), want):
+            assert np.array_equal(got.cpu().numpy(), ref)
+        table, kv, kvd, at = want[3], want[4], p.kv_len, at + int(want[5][0])
+        before = [t.clone() for t in (p.cu_q, p.positions, p.slots, p.kv_len, p.used, tab)]
+        for bad in (lambda: m.kv_plan(p.kv_len, newd, tab, freed, page, T, out=p), lambda: m.kv_plan(kvd, p.kv_len, tab, freed, page, T, out=p),
+                    lambda: m.kv_plan(kvd, newd, tab, p.slots, page, T, out=p), lambda: m.kv_plan(kvd, newd, tab, tab.view(-1), page, T)):
+            with pytest.raises(m.QGemmError, match="overlap"):
+                bad()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(before, (p.cu_q, p.positions, p.slots, p.kv_len, p.used, tab)))
+
+
 def test_plan_writes_its_outputs_only():
     torch = torch_or_skip()
     m = q()

@@ -32,6 +32,19 @@ def test_kv_plan_refusals(m):
         assert call(**{name: 18}) == -2, name
 
 
+def test_kv_plan_refuses_tables_that_overlap_what_it_writes(m):
+    f = m.lib().qgemm_kv_plan
+    n = dict(kv=3, q=3, tab=6, free=5, cu=4, pos=7, slots=7, total=3, used=1)
+    at = {name: (i + 1) << 12 for i, name in enumerate(n)}
+    written = ("tab", "cu", "pos", "slots", "total", "used")
+    for a in written:
+        for b in n:
+            for shift in () if a == b else (0, 4 * (n[b] - 1), -4 * (n[a] - 1)):       # the same, and one entry in common
+                p = {**at, a: at[b] + shift}
+                assert f(*p.values(), 3, 2, 5, 16, 7, None) == -1, (a, b, shift)
+                assert "overlap" in m.last_error(), (a, b, shift)
+
+
 def test_rope_refusals(m):
     f = m.lib().qgemm_rope
     ok = dict(x=64, type=1, pos=64, freq=64, y=128, T=4, heads=3, rot_heads=2, D=64, rot=64, xs=192, ys=192, inter=0, gain=1.0)
