@@ -363,7 +363,7 @@ int qgemm_attention_packed(const void* q, const void* k, const void* v, const in
   if (rc != QGEMM_OK) return rc;
   if (!aligned(cu, 4)) return fail(QGEMM_EALIGN, "cu must be 4-byte aligned");
   // the kernel counts a tensor's bytes in 32 bits, and reads (as zeros) up to a key block past its end
-  if (((long)T + 128) * std::max({q_stride, k_stride, v_stride}) >= 0x7ffffff0L)
+  if (std::max({q_stride, k_stride, v_stride}) > (0x7ffffff0L - 1) / ((long)T + 128))
     return fail(QGEMM_EUNSUPPORTED, "q, k and v must each span less than 4 GiB");
   const bool split = qg::attn_packed_split(D == 64, T, R, H);
   const long groups = (long)H * qg::ceil_div(T, split ? qg::kAttnBQ<true> : qg::kAttnBQ<false>);

@@ -101,6 +101,17 @@ def test_attention_packed_refusals(m):
     assert call(T=0) == 0 and call(R=0) == 0
 
 
+def test_attention_packed_refuses_strides_whose_product_with_the_rows_passes_64_bits(m):
+    f = m.lib().qgemm_attention_packed
+    for T in (1, 16, 384, 896):                     # 129, 144, 512 and 1024 strides with the block past the end
+        for stride in (1 << 60, 1 << 59, 1 << 55, 1 << 54):
+            for at in range(3):
+                s = [256, 128, 128]
+                s[at] = stride
+                assert f(16, 16, 16, 16, 16, T, 2, 4, 2, 64, *s, 256, 0.1, None) == -3, (T, stride, at)
+                assert "4 GiB" in m.last_error()
+
+
 def test_attention_kv4_refusals(m):
     f, g = m.lib().qgemm_attention_kv4, m.lib().qgemm_attention_kv4_workspace
     ok = dict(q=16, cache=16, tab=16, kv=16, cu=16, o=16, ws=16, bytes=1 << 40, T=8, R=2, H=4, Hkv=2, D=64, W=4, pages=9, page=16, qs=256,
