@@ -387,7 +387,7 @@ int qgemm_attention_packed(const void* q, const void* k, const void* v, const in
  * T == R) and kv_len[r] keys in all, new token i is at position
  * p = kv_len[r] - n + i and sees the keys 0 .. p:
  *   o[cu_q[r] + i][h] = sum_j softmax_j(scale q . k_j[g]) v_j[g],  g = h / (H / Hkv)
- * A row that sees no key (p < 0) gives 0.
+ * A row that sees no key (p < 0) gives 0, one whose scores are all -inf NaN.
  * q: bf16 [T][H][D] at q_stride elements between rows (a multiple of 8); o: bf16
  * [T][H][D], dense; cache, block_table as above, kv_len: int32 [R]; cu_q: int32
  * [R+1], ascending, or null. fp32 scores, sums and accumulation; the softmax

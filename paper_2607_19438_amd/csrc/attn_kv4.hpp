@@ -132,6 +132,12 @@ __device__ __forceinline__ float part_weight(float m, float top, float sl2) {
   return m == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f((m - top) * sl2);
 }
 
+// What a row's weighted values are multiplied by at the end: one over the weights' sum, and 0 for a row before the
+// cache's start. A row that sees keys of score -inf only has the sum 0 too: its 0 times infinity is NaN, as its softmax.
+__device__ __forceinline__ float row_factor(float sum, int position) {
+  return sum == 0.0f && position < 0 ? 0.0f : 1.0f / sum;
+}
+
 template <int N>
 __device__ __forceinline__ void store_row(uint16_t* p, const float (&v)[N]) {
   static_assert(N == 4 || N == 8, "8 or 16 bytes");
@@ -376,7 +382,7 @@ __device__ __forceinline__ void kv4_wide(const Kv4Args& a, const Kv4Request& rq,
   const float sum = l_run + other_half(l_run);
   if (slot == nullptr) {
     if (live) {
-      const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+      const float inv = row_factor(sum, rq.kv - rq.n + rho / G);
       const int token = rho / G;
       uint16_t* orow = a.o + ((size_t)(rq.c0 + token) * a.H + (size_t)(h * G + (rho - token * G))) * D;
 #pragma unroll
@@ -768,10 +774,10 @@ __device__ __forceinline__ void kv4_body(const Kv4Args& a) {
           const int rho = row0 + 16 * nt + row;
           if (whole) {
             if (rho < nrows) {
-              const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+              const int i = rho / G;
+              const float inv = row_factor(sum, rq.kv - rq.n + i);
 #pragma unroll
               for (int e = 0; e < CH; ++e) out[e] *= inv;
-              const int i = rho / G;
               store_row<CH>(a.o + ((size_t)(rq.c0 + i) * a.H + (size_t)(h * G + (rho - i * G))) * D + ch * CH, out);
             }
           } else {
@@ -876,10 +882,10 @@ __global__ __launch_bounds__(64 * kKv4JoinRows) void kv4_join_kernel(Kv4Args a) 
 #pragma unroll
   for (int e = 0; e < CH; ++e) out[e] = sum_over_groups(wt * out[e]);
   if (lane >= 16) return;
-  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+  const int i = rho / G;
+  const float inv = row_factor(sum, max(a.kv_len[head.r], 0) - head.nrows / G + i);
 #pragma unroll
   for (int e = 0; e < CH; ++e) out[e] *= inv;
-  const int i = rho / G;
   store_row<CH>(a.o + ((size_t)(head.c0 + i) * a.H + (size_t)(head.h * G + (rho - i * G))) * D + ch * CH, out);
 }
 

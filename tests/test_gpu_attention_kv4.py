@@ -219,6 +219,36 @@ def test_what_pages_hold_behind_a_row_reaches_nothing():
     assert torch.equal(o[7:9][..., keep], c[7:9][..., keep]) and torch.equal(o[9], c[9])
 
 
+@pytest.mark.parametrize("kv,new,H,Hkv,D,page,width", [
+    ([40, 300], [1, 1], 8, 2, 128, 16, None), ([3000, 5], [1, 1], 4, 4, 64, 16, None), ([700, 90], [9, 20], 16, 2, 64, 32, None),
+    ([2500], [30], 8, 1, 128, 64, None), ([640], [600], 32, 8, 128, 32, 20), ([3000, 700], [600, 240], 32, 8, 64, 16, None)])
+def test_rows_whose_scores_are_all_minus_infinity_are_nan(kv, new, H, Hkv, D, page, width):
+    """Not zero as rows that see no key are: single and several tokens, tiles of 128 rows, split and whole, and no other row."""
+    torch = torch_or_skip()
+    table, cache, k, v, qn, bits, cu = make(kv, new, H, Hkv, D, page, seed=23, width=width)
+    byte = np.arange(page) * (D // 2) + 2                     # element 5 of every key is 1.0 (code 2)
+    cache[..., byte] = cache[..., byte] & 0x0f | 0x20
+    k, v = oracle.decode_cache(cache, D)
+    clean = run(torch, (table, cache, k, v, qn, bits, cu), kv, cu)
+    bad = [(0, H - 1), (int(cu[-1]) - 1, 0), (int(cu[-1]) // 2, H // 2)]
+    for t, h in bad:
+        qn[t, h, 5] = -np.inf
+        bits[t, h, 5] = 0xff80
+    want = torch.zeros(clean.shape, dtype=torch.bool, device="cuda")
+    for t, h in bad:
+        r = int(np.searchsorted(cu, t, side="right") - 1)
+        g = h // (H // Hkv)
+        kk, _ = oracle.gather_cache(k, v, table[r], int(kv[r]) - int(cu[r + 1] - 1 - t), page)
+        assert np.all(kk[:, g] @ qn[t, h] == -np.inf)
+        want[t, h] = True
+    o = run(torch, (table, cache, k, v, qn, bits, cu), kv, cu)
+    assert torch.isnan(o[want]).all()
+    # the others: both are within attn_tolerance, and sum_j p_j |v_j| is at most the largest value
+    other, was = o[~want].float(), clean[~want].float()
+    tol = 2 * (2.0 ** -7 * float(np.abs(v).max()) + 2.0 ** -8 * was.abs())
+    assert torch.all((other - was).abs() <= tol)
+
+
 def test_missing_pages_are_nan():
     torch = torch_or_skip()
     kv, H, Hkv, D, page = [40, 40, 200, 20], 4, 1, 64, 16
