@@ -10,13 +10,14 @@ no fallback path, and a missing library raises ``QGemmError``.
 
 The serving functions' checks and allocations also exist compiled (``csrc/binding.cpp``, built
 beside the library): a call with good arguments on the current device goes that way where it
-is there. It answers ``NotImplemented`` to any other, and the code here says what is wrong.
+is there and fits the library and torch. It answers ``NotImplemented`` to any other, and the code here says what is wrong.
 """
 from __future__ import annotations
 
 import ctypes
 import functools
 import os
+import warnings
 
 import torch  # imported before the library so that both share one HIP runtime
 
@@ -87,6 +88,8 @@ def lib():
             fn = getattr(handle, name)
             fn.restype = res
             fn.argtypes = args
+        if way is not None and _header_of(handle) != way.header:
+            way = _no_compiled_way("it was built from another header than the library")
         if way is not None:
             names = ("kv_plan", "rope", "kv4_store", "kv4_load", "attention_packed", "attention_kv4", "attention_kv4_workspace")
             way.bind(_raw_stream, *[ctypes.cast(getattr(handle, "qgemm_" + n), ctypes.c_void_p).value for n in names])
@@ -100,8 +103,25 @@ def _compiled_way():
     calls was measured 0.5 us longer (rope 4.6, not 4.1; plan 5.4, not 4.9), in every process."""
     if _raw_stream is None or not os.path.exists(os.path.join(_HERE, "_binding.so")):
         return None
-    from . import _binding
-    return _binding
+    try:
+        from . import _binding
+    except ImportError as e:
+        return _no_compiled_way(str(e))
+    built_for = getattr(_binding, "torch", None)
+    return _binding if built_for == torch.__version__ else _no_compiled_way(f"it was built for torch {built_for}, not {torch.__version__}")
+
+
+def _no_compiled_way(why: str):
+    """A binding that is there and does not fit: the library's functions all work without it, the serving ones slower."""
+    warnings.warn(f"_binding.so is not used: {why}; run `python -m paper_2607_19438_amd.build`", RuntimeWarning, stacklevel=4)
+
+
+def _header_of(handle):
+    """The stamp of the header that a library was built from."""
+    try:
+        return (ctypes.c_char * 17).in_dll(handle, "qgemm_header").value.decode()
+    except ValueError:
+        return None
 
 
 def _check(rc: int):

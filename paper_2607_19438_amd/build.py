@@ -4,6 +4,7 @@ Usage: ``python -m paper_2607_19438_amd.build [--verbose]``.
 """
 from __future__ import annotations
 
+import hashlib
 import os
 import subprocess
 import sys
@@ -33,13 +34,24 @@ FLAGS = [
 ]
 
 
+HEADER = os.path.join(os.path.dirname(HERE), "include", "qgemm.h")
+
+
+def header_stamp() -> str:
+    """What the library and the binding each carry of the header that they were built from: a binding calls only a library
+    of the same one."""
+    with open(HEADER, "rb") as f:
+        return hashlib.sha256(f.read()).hexdigest()[:16]
+
+
 def build(verbose: bool = False, extra=None) -> str:
     """Compile every source (side by side, one object each) and link the library. All of it in a folder of
     its own beside the library, which then replaces the old one in one step: builds may run at once."""
     with tempfile.TemporaryDirectory(prefix="build-", dir=os.path.dirname(LIB)) as tmp:
         objs = [os.path.join(tmp, os.path.basename(src) + ".o") for src in SOURCES]
         new = os.path.join(tmp, os.path.basename(LIB))
-        cmds = [[HIPCC, *FLAGS, *(extra or []), "-c", src, "-o", obj] for src, obj in zip(SOURCES, objs)]
+        stamp = f'-DQGEMM_HEADER="{header_stamp()}"'
+        cmds = [[HIPCC, *FLAGS, stamp, *(extra or []), "-c", src, "-o", obj] for src, obj in zip(SOURCES, objs)]
         link = [HIPCC, f"--offload-arch={ARCH}", "-shared", *objs, "-o", new]
         if verbose:
             for cmd in [*cmds, link]:
@@ -74,7 +86,8 @@ def build_binding(verbose: bool = False) -> str:
     with tempfile.TemporaryDirectory(prefix="build-", dir=os.path.dirname(BINDING)) as tmp:
         new = os.path.join(tmp, os.path.basename(BINDING))
         cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-Wall",
-               f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-isystem", sysconfig.get_paths()["include"],
+               f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", f'-DQGEMM_HEADER="{header_stamp()}"',
+               f'-DQGEMM_TORCH="{torch.__version__}"', "-isystem", sysconfig.get_paths()["include"],
                "-isystem", os.path.join(root, "include"), "-isystem", os.path.join(root, "include", "torch", "csrc", "api", "include"),
                BINDING_SOURCE, "-o", new, "-L" + os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]
         if verbose:

@@ -324,4 +324,16 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, n
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__binding(void) { return PyModule_Create(&module); }
+// What this was built from and against: the library's header and torch. The Python side compares both.
+#ifndef QGEMM_HEADER
+#define QGEMM_HEADER ""
+#endif
+#ifndef QGEMM_TORCH
+#define QGEMM_TORCH ""
+#endif
+
+PyMODINIT_FUNC PyInit__binding(void) {
+  PyObject* m = PyModule_Create(&module);
+  if (m && (PyModule_AddStringConstant(m, "header", QGEMM_HEADER) < 0 || PyModule_AddStringConstant(m, "torch", QGEMM_TORCH) < 0)) Py_CLEAR(m);
+  return m;
+}

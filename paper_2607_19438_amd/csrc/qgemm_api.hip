@@ -406,6 +406,13 @@ extern "C" {
 
 int qgemm_version(void) { return (1 << 16) | 0; }
 
+// What the build gives of the header's text; the Python binding's compiled part has it too.
+#ifndef QGEMM_HEADER
+#define QGEMM_HEADER ""
+#endif
+extern __attribute__((visibility("default"))) const char qgemm_header[];
+const char qgemm_header[] = QGEMM_HEADER;
+
 const char* qgemm_last_error(void) { return qg::g_last_error.c_str(); }
 
 int qgemm_dense(const void* x, const void* wq, const void* scales, float* y, int M, int N, int K, int fmt,
