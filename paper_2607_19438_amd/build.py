@@ -6,6 +6,7 @@ from __future__ import annotations
 
 import hashlib
 import os
+import shutil
 import subprocess
 import sys
 import tempfile
@@ -76,18 +77,23 @@ BINDING = os.path.join(HERE, "_binding.so")
 BINDING_SOURCE = os.path.join(CSRC, "binding.cpp")
 
 
-def build_binding(verbose: bool = False) -> str:
+def build_binding(verbose: bool = False):
     """Compile the host code between Python and the library (the serving calls' checks and allocations) against the
-    installed torch; it replaces the old one in one step."""
+    installed torch; it replaces the old one in one step. Without a host compiler or Python's headers, which the library
+    does not need, it is left unbuilt and None returned: the calls then go the Python way."""
     import sysconfig
 
     import torch
+    compiler, include = os.environ.get("CXX", "g++"), sysconfig.get_paths()["include"]
+    if shutil.which(compiler) is None or not os.path.exists(os.path.join(include, "Python.h")):
+        print(f"{os.path.basename(BINDING)} not built: " + ("no Python.h" if shutil.which(compiler) else f"no {compiler}"), flush=True)
+        return None
     root = os.path.join(os.path.dirname(torch.__file__))
     with tempfile.TemporaryDirectory(prefix="build-", dir=os.path.dirname(BINDING)) as tmp:
         new = os.path.join(tmp, os.path.basename(BINDING))
-        cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-Wall",
+        cmd = [compiler, "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-Wall",
                f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", f'-DQGEMM_HEADER="{header_stamp()}"',
-               f'-DQGEMM_TORCH="{torch.__version__}"', "-isystem", sysconfig.get_paths()["include"],
+               f'-DQGEMM_TORCH="{torch.__version__}"', "-isystem", include,
                "-isystem", os.path.join(root, "include"), "-isystem", os.path.join(root, "include", "torch", "csrc", "api", "include"),
                BINDING_SOURCE, "-o", new, "-L" + os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]
         if verbose:
@@ -105,4 +111,5 @@ if __name__ == "__main__":
     v = "--verbose" in sys.argv
     extra = ["-Rpass-analysis=kernel-resource-usage"] if "--resources" in sys.argv else None
     print(build(verbose=v or bool(extra), extra=extra))
-    print(build_binding(verbose=v))
+    if (binding := build_binding(verbose=v)) is not None:
+        print(binding)

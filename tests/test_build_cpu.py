@@ -1,7 +1,10 @@
 """Builds that run side by side do not disturb each other: every one ends with a whole library in place."""
 import os
 import stat
+import sysconfig
 import threading
+
+import pytest
 
 from paper_2607_19438_amd import build
 
@@ -51,3 +54,23 @@ def test_two_builds_at_once(tmp_path, monkeypatch):
         t.join()
     assert not errors, errors[0]
     assert sorted(os.listdir(tmp_path)) == ["a.hip", "b.hip", "cc", "lib.so"]       # nothing left behind
+
+
+def test_the_library_needs_no_host_compiler(tmp_path, monkeypatch, capsys):
+    """Without g++ or Python's headers the binding's compiled part is left out, and no build fails for it."""
+    monkeypatch.setattr(build, "BINDING", str(tmp_path / "_binding.so"))
+    monkeypatch.setenv("CXX", str(tmp_path / "no-compiler"))
+    assert build.build_binding() is None and "no-compiler" in capsys.readouterr().out
+    monkeypatch.setenv("CXX", "true")                      # a program that is there
+    paths = sysconfig.get_paths()
+    monkeypatch.setattr(sysconfig, "get_paths", lambda: {**paths, "include": str(tmp_path)})
+    assert build.build_binding() is None and "Python.h" in capsys.readouterr().out
+    assert os.listdir(tmp_path) == []
+
+
+def test_a_binding_that_does_not_compile_is_an_error(tmp_path, monkeypatch):
+    monkeypatch.setattr(build, "BINDING", str(tmp_path / "_binding.so"))
+    monkeypatch.setenv("CXX", "false")
+    with pytest.raises(RuntimeError, match="false failed"):
+        build.build_binding()
+    assert os.listdir(tmp_path) == []
