@@ -133,6 +133,41 @@ def test_prompts_do_not_touch_each_other(bad, H):
     assert torch.isfinite(o[cu[3] + 30:cu[4], :, 6].float()).all()
 
 
+@pytest.mark.parametrize("H,Hkv,D", [(2, 2, 64), (32, 4, 128)])
+def test_an_early_infinite_value_stays_cheap_and_in_its_element(H, Hkv, D):
+    """One infinite value near the start of a long prompt: its element of the rows that see it is infinite, everything else
+    as without it. And the call takes a few times as long, for looking at the keys that those rows do not see, not 200
+    times, for computing each of them by itself."""
+    torch = torch_or_skip()
+    m = q()
+    lens = [5, 4000, 40, 700]
+    row, bits, cu = make(lens, H, Hkv, D, seed=13)
+    d, cud = dev_bf16(torch, bits), dev_i32(torch, cu)
+
+    def us(x):
+        best = 1e9
+        for _ in range(3):
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            a.record()
+            o = m.attention_packed(*views(x, H, Hkv), cud)
+            b.record()
+            torch.cuda.synchronize()
+            best = min(best, 1e3 * a.elapsed_time(b))
+        return o.float(), best
+
+    us(d)
+    clean, t0 = us(d)
+    e = d.clone()
+    at = int(cu[1]) + 3
+    e[at, H + Hkv:, 5] = float("inf")
+    o, t1 = us(e)
+    print(f"[time] {H}/{Hkv}x{D}: {t0:.1f} us, with an infinite value {t1:.1f}", flush=True)
+    assert torch.all(o[at:cu[2], :, 5] == float("inf"))
+    o[at:cu[2], :, 5] = clean[at:cu[2], :, 5]
+    assert torch.all((o - clean).abs() <= 2.0 ** -6 * clean.abs() + 2.0 ** -7 * 4)
+    assert t1 < 20 * t0 + 100
+
+
 def test_strides_of_every_operand_and_determinism():
     torch = torch_or_skip()
     m = q()
