@@ -159,6 +159,28 @@ def test_what_pages_hold_behind_a_chunk_reaches_nothing(D):
     assert torch.equal(o[:40], clean[:40].float()) and torch.isnan(o[40:430]).all() and torch.equal(o[430:], clean[430:].float())
 
 
+@pytest.mark.parametrize("kv,new,H,Hkv,D,page", [
+    ([37, 5, 130], [4, 5, 1], 4, 2, 128, 16), ([3000, 200, 1], [1, 1, 1], 8, 1, 64, 16), ([900, 33], [30, 17], 16, 2, 64, 32),
+    ([470, 450], [430, 420], 32, 8, 128, 16), ([2000, 700], [600, 240], 32, 8, 64, 16)])
+def test_table_entries_behind_the_pages_of_a_request_may_be_anything(kv, new, H, Hkv, D, page):
+    """Single and several tokens and tiles of 128 rows: entries that look-ups ahead of the keys may fetch, of either sign,
+    just outside the pool, far outside and inside it."""
+    torch = torch_or_skip()
+    need = [-(-n // page) for n in kv]
+    case = make(kv, new, H, Hkv, D, page, seed=24, width=max(need) + 9)
+    table, cache, *rest = case
+    clean = run(torch, case, kv, case[-1])
+    assert torch.isfinite(clean.float()).all()
+    free = np.arange(table.shape[1])[None, :] >= np.array(need)[:, None]
+    values = [-2 ** 31, 2 ** 31 - 1, 10 ** 6, -1, len(cache), len(cache) - 1, 2 ** 30, 0]
+    for shift in range(len(values)):                     # every value is the first behind a request's pages once
+        wild = table.copy()
+        for r in range(len(kv)):
+            n = int(free[r].sum())
+            wild[r, free[r]] = np.resize(np.roll(values, -shift - r), n)
+        assert torch.equal(run(torch, (wild, cache, *rest), kv, case[-1]), clean)
+
+
 def test_chunks_give_the_same_bits_every_time():
     torch = torch_or_skip()
     case = make([3000, 700], [600, 240], 32, 8, 64, 16, seed=21)
