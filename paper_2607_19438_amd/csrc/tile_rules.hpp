@@ -233,9 +233,19 @@ inline bool attn_split(bool d64, bool causal, long S, long heads) {
 //          R = 3    256 0.83-0.94  384 0.90-1.00  432 0.91  512 0.81-0.89  576 1.02-1.06  768 0.89-0.91  1024 1.03-1.14
 //          R = 5    384 0.90-0.96  432 0.87  512 0.97-1.08  576 1.11  768 1.05-1.08
 //          R = 200  256 0.95  320 0.92  384 0.92  432 1.17  512 1.19  768 1.13
+// and again with 8, 16 and 32 heads, prompts of one length; each 1.6 times the next (the longer chains favour 64 rows):
+//   D=64   R = 1    512 0.80-0.83              576 0.78-0.89              640 0.83-0.93              704 0.90-0.96              768 0.93-0.97
+//          R = 2    512 0.83-0.87; 0.81-0.87   576 0.77-0.81; 0.84-0.87   640 0.77-0.86; 0.84-0.90   704 0.77-0.91; 0.76-0.87   896 0.98-1.07; 0.85-0.92
+//          R = 3    512 0.82-0.93; 0.81-0.88   576 0.90-1.04; 0.80-0.83   640 0.95-1.06; 0.80-0.89   704 0.96-1.01; 0.82-0.93   896 0.87-0.94; 0.82-0.93
+//          R = 4    448 0.87-0.99; 0.80-0.89   512 0.90-1.02; 0.80-0.87   576 0.92-1.00; 0.78-0.88   640 0.96-1.06; 0.75-0.88   896 1.06-1.15; 0.92-0.99
+//          R = 5    448 0.80-0.97; 0.77-0.85   512 0.98-1.10; 0.78-0.86   576 0.99-1.15; 0.84-0.92   640 0.80-1.00; 0.78-0.84   896 1.00-1.09; 0.89-0.94
+//          R = 40   384 0.89-0.92; 0.79-0.86   448 1.16-1.22; 0.75-0.83   512 1.13-1.22; 0.79-0.96   640 1.09-1.16; 0.86-0.97   896 1.02-1.07; 0.91-0.95
+//   D=128  R = 2    448 0.79-0.97; 0.82-0.95   512 0.84-0.96; 0.81-1.02   576 0.86-1.03; 0.88-1.08   704 0.98-1.17; 0.90-1.07
+//          R = 3    384 0.84-1.03; 0.82-1.03   448 0.89-0.99; 0.84-1.01   512 0.94-1.03; 0.79-0.93   640 1.06-1.13; 0.87-1.03
+// From four prompts on the limits are those of one length: how uneven the lengths are is not known here.
 inline bool attn_packed_split(bool d64, long T, long R, long heads) {
   const long wide = heads * ceil_div(T, 128);
-  if (d64) return wide <= (R <= 2 ? 700 : R <= 5 ? 448 : 400);
+  if (d64) return wide <= (R <= 3 ? 704 : R <= 5 ? 448 : 400);
   return wide <= (R <= 2 ? 512 : R <= 3 ? 384 : 256);
 }
 
