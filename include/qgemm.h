@@ -15,8 +15,8 @@
  * - Arrays are dense and row-major; no strides, but for the row strides that the
  *   serving entry points take. Every device pointer must be 16-byte aligned,
  *   except fp16 scale arrays, which need 2-byte alignment, and the tables of
- *   the serving entry points, which need that of their elements (QGEMM_EALIGN
- *   otherwise).
+ *   the serving entry points and qgemm_rope's rows, which need that of their
+ *   elements (QGEMM_EALIGN otherwise).
  * - Work is enqueued on `stream` (0 = the null stream) and the call returns
  *   without synchronising; device faults surface at the caller's next sync.
  *   The caller keeps every buffer alive until the stream has passed the call.
@@ -370,8 +370,8 @@ int qgemm_kv4_load(const void* cache, const int32_t* slots, void* k, void* v, in
  * prompt r (rows cu[r] .. cu[r+1]-1) over the keys cu[r] .. t.
  * q, o: bf16 [T][H][D]; k, v: bf16 [T][Hkv][D], at their strides (elements,
  * multiples of 8); cu: int32 [R+1], ascending, cu[0] == 0, cu[R] <= T; prompts
- * of no rows may stand among them. Rows at or past cu[R] are neither read nor
- * written. A prompt's rows depend on no other prompt, whatever that holds
+ * of no rows may stand among them. Rows at or past cu[R] are not written, and
+ * what they hold changes nothing, but q is loaded for all T rows. A prompt's rows depend on no other prompt, whatever that holds
  * (infinities and NaN included), nor on later rows. D is 64 or 128; T*H*D < 2^31;
  * q, k and v each span less than 4 GiB. Precision as qgemm_attention_prefill.
  * A cu that does not ascend gives unspecified rows.
@@ -391,7 +391,8 @@ int qgemm_attention_packed(const void* q, const void* k, const void* v, const in
  * q: bf16 [T][H][D] at q_stride elements between rows (a multiple of 8); o: bf16
  * [T][H][D], dense; cache, block_table as above, kv_len: int32 [R]; cu_q: int32
  * [R+1], ascending, or null. fp32 scores, sums and accumulation; the softmax
- * weights enter the output product as bf16. Keys of a page outside [0, pages) or
+ * weights enter the output product as bf16 (and the sum that divides it with that
+ * rounding, but without it in the tiles of 128 rows that chunks of prompts take). Keys of a page outside [0, pages) or
  * past the table's W entries make the rows that see them NaN, and a value block of scale
  * byte 253 or 254, which passes bf16's range, counts as one of NaN; nothing else that
  * the pages hold behind a row's position reaches it. Results do not depend on how the

@@ -529,7 +529,8 @@ __device__ __forceinline__ void attn_body(const AttnArgs& a) {
   if constexpr (SPLIT) {
     // Merge the two waves of the same queries: the second half's output, maximum and sum go through the
     // key and value buffers (the loop ends with a barrier), lane by lane. A wave that skipped every
-    // tile has maximum -inf and takes weight 0; the first half always holds key 0.
+    // tile has maximum -inf and takes weight 0, and so does a half whose keys are all masked (PACKED); the other
+    // half then holds the row's own key.
     typedef __attribute__((address_space(3))) float lds_float;
     lds_float* mo = (lds_float*)((wave & 1) ? (lds_char*)ks1 : (lds_char*)ks0);
     lds_float* ml = (lds_float*)((wave & 1) ? (lds_char*)vt1 : (lds_char*)vt0);

@@ -22,7 +22,8 @@
 // v_cvt_scalef32_pk_bf16_fp4 unpacks two levels and applies the block's scale in one instruction.
 //
 // Measured: 64 requests of 20 to 16000 keys, 32/8 heads of 128, 176 MB in 43 us (4.1 TB/s) and 4.5 us to join; one
-// request of 4097 keys, 32/4 heads, 6.3 us and 4.5; two chunks of 550 rows over 5000 keys, 32/8 heads, 131 us in all
+// request of 4097 keys, 32/4 heads, 6.3 us and 4.5 (of the 6.3: workgroups started 0.7, lengths scanned 1.4, page numbers
+// and first loads 1.6, its keys 1.2 to 2.2, waves joined 0.9); two chunks of 550 rows over 5000 keys, 32/8 heads, 131 us in all
 // (650 TFLOP/s; with pairs of tiles 150).
 #pragma once
 
@@ -162,7 +163,7 @@ constexpr int kKv4Wide = 8;          // NT of the wide form: 128 query rows
 // block. The block is unpacked once for all of them, a quarter of a row to a thread, into LDS; the products are the
 // prompt kernel's (v_mfma_f32_32x32x16_bf16). The next block's levels are in registers while a block is computed.
 // Bound by the matrix cores and the softmax as that kernel is, and by the parts: 64 KiB each, written and read again, for
-// two chunks of 550 rows over 5000 keys 25 of 131 us. (The value fragments a whole step ahead, as there, take 12
+// two chunks of 550 rows over 5000 keys 27 of 131 us. (The value fragments a whole step ahead, as there, take 12
 // registers too many at D = 128: 134 us.)
 template <int D>
 __device__ __forceinline__ void kv4_wide(const Kv4Args& a, const Kv4Request& rq, int r, int tile, int h, int a0, int a1,

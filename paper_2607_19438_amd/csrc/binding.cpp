@@ -2,8 +2,8 @@
 // functions of the same names, for arguments that are as they should be and lie on the current device. For anything
 // else a function here answers NotImplemented, having done nothing, and the Python function goes its own way, which
 // says what is wrong. A decode step's calls take less time on the GPU than their checks take in Python: host time
-// of a call (us, Python alone and with this file) rope 6.8, 4.0; plan 8.4, 4.9; store and load 13.3, 7.7; packed
-// prompts 6.3, 3.3; attention over the cache 10.6, 7.2; a launch is 2.4 of it, an allocation 0.6.
+// of a call of 16 rows (us, Python alone and with this file) rope 8.5, 4.4; plan 10.2, 5.1; store and load 16.5, 8.9;
+// packed prompts 9.0, 4.7; attention over the cache 10.5, 5.4; a launch is 2.4 of it, an allocation 0.6.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 

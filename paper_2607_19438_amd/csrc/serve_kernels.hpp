@@ -180,7 +180,8 @@ __device__ __forceinline__ void rotate(float& a, float& b, float2 w) {
 // The sine and cosine of every (token, pair) are evaluated once per workgroup and shared by all heads through
 // LDS. The angle is taken in turns in fp64 (position x frequency / 2 pi, less its whole turns): at position
 // 10^6 an fp32 product is off by 0.06 radians. What is left is below half a turn, so fp32 keeps 2^-25 of one.
-// Bound by HBM: 8192 rows of 40 x 128 from fp32 in 46.4 us, 5.4 TB/s; at 16 rows by its one launch, 3.2 us.
+// Bound by HBM: 8192 rows of 40 x 128 from fp32 in 46.4 us, 5.4 TB/s (40 into the buffer that the call before wrote, which
+// is still in the memory-side cache); at 16 rows by its one launch, 3.2 us.
 // WIDE: 16 elements per thread and step, with 16-byte accesses, where sizes, strides and addresses allow it;
 // else two elements. (The first step's loads before the sines, and each next step's before the last one's work:
 // 3000 rows of 24 x 64 5.2 -> 5.5 us, 8000 rows 10.0 -> 11.8, 16 rows of 40 x 128 3.1 -> 3.3. The waves are
