@@ -20,7 +20,7 @@
  * - Work is enqueued on `stream` (0 = the null stream) and the call returns
  *   without synchronising; device faults surface at the caller's next sync.
  *   The caller keeps every buffer alive until the stream has passed the call.
- * - Outputs are written, never accumulated into, and must not alias inputs.
+ * - Outputs are written, never accumulated into (but for qgemm_adapters' y), and must not alias inputs.
  * - Return value: QGEMM_OK (0) or a negative QGEMM_E* code. On an error return
  *   nothing has been enqueued and no output is written;
  *   qgemm_last_error() gives a message. No entry point throws.
@@ -408,6 +408,109 @@ int qgemm_attention_kv4(const void* q, const void* cache, const int32_t* block_t
                         int64_t workspace_bytes, int T, int R, int H, int Hkv, int D, int W, int pages,
                         int page, int64_t q_stride, float scale, hipStream_t stream);
 int qgemm_attention_kv4_workspace(int T, int R, int H, int Hkv, int D, int W, int page, int64_t* bytes);
+
+/*
+ * Many continuations and many tenants: a step of beam search, or of a batch whose requests share a prompt or have
+ * adapters of their own.
+ *
+ *   projections + qgemm_adapters -> ... -> qgemm_attention_kv4_shared -> ... -> logits -> qgemm_beam_select ->
+ *   qgemm_kv_reorder -> qgemm_kv4_copy (each layer's cache) -> the next step's qgemm_kv_plan
+ */
+
+/*
+ * qgemm_attention_kv4 for requests that share their first keys: the same result, up to fp32 summation order, with the
+ * shared keys read and unpacked once for all rows of a group (decode, Section 2.3, is bound by those bytes).
+ * Group g holds the requests groups[g] .. groups[g+1]-1, whose first prefix_len[g] keys are the same: the keys that are
+ * taken as shared are read through the table of the group's first request that has new tokens, the others through each
+ * request's own. Shared are min(prefix_len[g], the fewest keys that a request of the group has before its new tokens), down
+ * to a multiple of 64; a prefix_len of 0 or less, or one past the table, asks for none, or for no more than the table
+ * has. Requests before groups[0] or from groups[G] on share nothing.
+ * groups: int32 [G+1], ascending; prefix_len: int32 [G]; the other arguments as qgemm_attention_kv4, o unaliased.
+ * Rows behind the last request are left as they are. Keys of a page outside [0, pages) or past the table make the rows
+ * that see them NaN, shared ones those of the whole group. groups or a cu_q that do not ascend leave o unspecified.
+ * Results are the same on every call. workspace as there, of qgemm_attention_kv4_shared_workspace's bytes.
+ * R and G <= 4096; else the limits of qgemm_attention_kv4, with the larger of R and G in the last.
+ */
+int qgemm_attention_kv4_shared(const void* q, const void* cache, const int32_t* block_table,
+                               const int32_t* kv_len, const int32_t* cu_q, const int32_t* groups,
+                               const int32_t* prefix_len, void* o, void* workspace, int64_t workspace_bytes,
+                               int T, int R, int G, int H, int Hkv, int D, int W, int pages, int page,
+                               int64_t q_stride, float scale, hipStream_t stream);
+int qgemm_attention_kv4_shared_workspace(int T, int R, int G, int H, int Hkv, int D, int W, int page,
+                                         int64_t* bytes);
+
+/*
+ * The K best continuations of every request's B beams: of the candidates (beam b, token v), worth
+ *   scores[r][b] + x[v] - log sum_u exp x[u],  x the row r*B + b of logits,
+ * the K of largest value, in descending order, equal ones the lower beam first, of a beam the lower token:
+ *   out_scores[r][k] its value, out_parents[r][k] = b, out_tokens[r][k] = v
+ * A beam with finished[r][b] != 0 has one candidate, the token `end` at its own score; its logits are not read. No
+ * candidates are those worth -inf or NaN: all of a beam whose score is (a beam that is not there: before the first
+ * selection all but one of a prompt's), tokens of logit -inf, and all of a row that holds NaN or +inf. Behind the last
+ * candidate stand score -inf, parent -1 and token `end`. So finished is (out_tokens == end) for the next selection.
+ * logits: fp32 (as qgemm_dense writes them) or bf16 [R*B][V] at `stride` elements between rows, aligned to their
+ * elements; scores: fp32 [R][B]; finished: uint8 [R][B] or null; outputs [R][K]. Maximum and sum of a row in
+ * fp32 and fp64, values in fp64, rounded once. Results are the same on every call. B <= 64, K <= 128 (of more than one
+ * beam K = B continues as many, K = 2B leaves a choice), R*B <= 2^20, V <= 2^30. workspace: caller-owned, 16-byte aligned,
+ * of the bytes that qgemm_beam_select_workspace gives, without initialisation; calls that can overlap need one each.
+ */
+int qgemm_beam_select(const void* logits, int type, const float* scores, const uint8_t* finished,
+                      float* out_scores, int32_t* out_parents, int32_t* out_tokens, void* workspace,
+                      int64_t workspace_bytes, int R, int B, int V, int K, int64_t stride, int end,
+                      hipStream_t stream);
+int qgemm_beam_select_workspace(int R, int B, int V, int K, int64_t* bytes);
+
+/*
+ * Block tables of the beams after a selection. Rows come in requests of B; row k of a request continues its old row
+ * p = parents[r*B + k] in [0, B), and with any other parent nothing: it then has no tokens. With have = ceil(kv_len[p] / page):
+ *   new_len = kv_len[p]; new_table[j] = block_table[p][j] for j < have, -1 from there on
+ * A last page that is filled only in part is written by the next token, so one row alone may hold it: the first row (the lowest k)
+ * of a parent has it, and the others a page each of free_pages, by request and k, with its number in dst and the
+ * parent's in src (both -1 for all other rows): qgemm_kv4_copy brings the keys and values over. used[0]: pages taken; where
+ * the free list ends (used[0] > F) entries become -1, with nothing to copy.
+ * released: the pages that no new row of their request holds in the column that they had, each once, by request,
+ * column and old row; -1 behind them. n_released[0] counts them; with more than Q those past Q are missing from the
+ * list. Not listed: the first keep[r] columns (pages of a prompt that others hold too; keep may be null: none), and
+ * negative entries.
+ * block_table, new_table: int32 [R*B][W]; kv_len (negative counts as 0), parents, new_len, src, dst: int32 [R*B];
+ * free_pages: int32 [F]; keep: int32 [R]; used, n_released: int32 [1]; released: int32 [Q]. Nothing that is written may share
+ * memory with another array: a loop keeps two tables that take turns. B <= 64, R*B <= 65536, R*B*W < 2^31.
+ * workspace: caller-owned, 4-byte aligned, of qgemm_kv_reorder_workspace's bytes, without initialisation.
+ */
+int qgemm_kv_reorder(const int32_t* block_table, const int32_t* kv_len, const int32_t* parents,
+                     const int32_t* free_pages, const int32_t* keep, int32_t* new_table, int32_t* new_len,
+                     int32_t* src, int32_t* dst, int32_t* used, int32_t* released, int32_t* n_released,
+                     void* workspace, int64_t workspace_bytes, int R, int B, int W, int F, int Q, int page,
+                     hipStream_t stream);
+int qgemm_kv_reorder_workspace(int R, int W, int64_t* bytes);
+
+/*
+ * Whole pages within a 4-bit cache: page src[i] (all heads) to page dst[i] for i < n. Pairs with a page outside
+ * [0, pages) are skipped. No page may be a dst twice, nor a dst of one pair and the src of another (what such pages hold
+ * afterwards is unspecified). src, dst: int32 [n].
+ */
+int qgemm_kv4_copy(void* cache, const int32_t* src, const int32_t* dst, int n, int Hkv, int D, int pages,
+                   int page, hipStream_t stream);
+
+/*
+ * Low-rank adapters of many requests on top of a shared projection's output (qgemm_dense of the same x):
+ *   y[m][c] += gain[i] sum_{j < r} b[i][c][j] (sum_k a[i][j][k] x[m][k]),  i = ids[request of row m]
+ * The rows cu_q[q] .. cu_q[q+1]-1 are request q's (cu_q ascending; null: M == R, row q is request q's). Rows of no
+ * request, and of one whose id is outside [0, n), are neither read into a result nor written.
+ * x: bf16 [M][K] at x_stride elements between rows (a multiple of 8); a: bf16 [n][r][K]; b: bf16 [n][N][r]; ids: int32 [R];
+ * gain: fp32 [n] or null (1); y: fp32 [M][N] at y_stride elements, so that the columns of one projection within a wider
+ * row can be given. y is read and written (the one output here that is added to), and shares no memory with an input.
+ * K and r multiples of 8 (an adapter of lower rank has zeros behind it), r <= 128, M, N and K <= 2^28. fp32
+ * accumulation; the inner sums enter the second product as three bf16 numbers each, which hold them whole. What one
+ * adapter or request holds (infinities and NaN included) reaches no other's rows. Results are the same on every call.
+ * Rows of an adapter that stand next to each other share the reading of its weights.
+ * workspace: caller-owned, 16-byte aligned, of qgemm_adapters_workspace's bytes, without initialisation; calls that can
+ * overlap need one each.
+ */
+int qgemm_adapters(const void* x, const void* a, const void* b, const int32_t* ids, const int32_t* cu_q,
+                   const float* gain, float* y, void* workspace, int64_t workspace_bytes, int M, int N, int K,
+                   int r, int n, int R, int64_t x_stride, int64_t y_stride, hipStream_t stream);
+int qgemm_adapters_workspace(int M, int N, int K, int r, int64_t* bytes);
 
 /*
  * Measurement utility, not part of the GEMM path: runs `iters` rounds of four

@@ -11,5 +11,7 @@ from .attention_oracle import *  # noqa: F401,F403
 from .attention_oracle import __all__ as _attn_all
 from .serve_oracle import *  # noqa: F401,F403
 from .serve_oracle import __all__ as _serve_all
+from .step_oracle import *  # noqa: F401,F403
+from .step_oracle import __all__ as _step_all
 
-__all__ = list(_qgemm_all) + list(_attn_all) + list(_serve_all)
+__all__ = list(_qgemm_all) + list(_attn_all) + list(_serve_all) + list(_step_all)

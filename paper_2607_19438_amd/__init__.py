@@ -23,7 +23,8 @@ import torch  # imported before the library so that both share one HIP runtime
 
 __all__ = ["Q8", "Q4", "QGemmError", "lib", "lib_path", "dense", "moe", "moe_noalloc", "moe_bucket", "moe_grouped",
            "moe_gate_up_swiglu", "moe_down_combine", "swiglu", "moe_combine", "attention_prefill", "probe_mfma_clock", "last_error", "release", "version", "EXPORTS", "ExpertTable",
-           "KvPlan", "kv_plan", "rope_frequencies", "rope", "kv4_cache_shape", "kv4_store", "kv4_load", "attention_packed", "attention_kv4"]
+           "KvPlan", "kv_plan", "rope_frequencies", "rope", "kv4_cache_shape", "kv4_store", "kv4_load", "attention_packed", "attention_kv4",
+           "attention_kv4_shared", "beam_select", "KvReorder", "kv_reorder", "kv4_copy", "adapters"]
 
 Q8 = 0
 Q4 = 1
@@ -55,6 +56,15 @@ EXPORTS = {
     "qgemm_attention_packed": (_i, [_vp] * 5 + [_i] * 5 + [_l] * 4 + [_f, _vp]),
     "qgemm_attention_kv4": (_i, [_vp] * 7 + [_l] + [_i] * 8 + [_l, _f, _vp]),
     "qgemm_attention_kv4_workspace": (_i, [_i] * 7 + [ctypes.POINTER(_l)]),
+    "qgemm_attention_kv4_shared": (_i, [_vp] * 9 + [_l] + [_i] * 9 + [_l, _f, _vp]),
+    "qgemm_attention_kv4_shared_workspace": (_i, [_i] * 8 + [ctypes.POINTER(_l)]),
+    "qgemm_beam_select": (_i, [_vp, _i] + [_vp] * 6 + [_l] + [_i] * 4 + [_l, _i, _vp]),
+    "qgemm_beam_select_workspace": (_i, [_i] * 4 + [ctypes.POINTER(_l)]),
+    "qgemm_kv_reorder": (_i, [_vp] * 13 + [_l] + [_i] * 6 + [_vp]),
+    "qgemm_kv_reorder_workspace": (_i, [_i] * 2 + [ctypes.POINTER(_l)]),
+    "qgemm_kv4_copy": (_i, [_vp] * 3 + [_i] * 5 + [_vp]),
+    "qgemm_adapters": (_i, [_vp] * 8 + [_l] + [_i] * 6 + [_l, _l, _vp]),
+    "qgemm_adapters_workspace": (_i, [_i] * 4 + [ctypes.POINTER(_l)]),
     "qgemm_probe_mfma_clock": (_i, [_i, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_double), _vp]),
     "qgemm_last_error": (ctypes.c_char_p, []),
     "qgemm_release": (_i, []),
@@ -715,6 +725,224 @@ def attention_kv4(q: torch.Tensor, cache: torch.Tensor, block_table: torch.Tenso
              block_table.data_ptr(), kv_len.data_ptr(), None if cu_q is None else cu_q.data_ptr(), out.data_ptr(),
              ws.data_ptr(), need, T, R, H, Hkv, D, W, pages, page, qs, D ** -0.5 if scale is None else float(scale))
     return out
+
+
+# ---------------------------------------------------------------------------
+# serving: many continuations of a prompt, many tenants
+# ---------------------------------------------------------------------------
+
+@functools.lru_cache(maxsize=1024)
+def _workspace(name: str, *sizes) -> int:
+    """Bytes of a call's workspace, which follow from the sizes alone."""
+    n = _l(0)
+    _check(getattr(lib(), f"qgemm_{name}_workspace")(*sizes, ctypes.byref(n)))
+    return n.value
+
+
+def attention_kv4_shared(q: torch.Tensor, cache: torch.Tensor, block_table: torch.Tensor, kv_len: torch.Tensor,
+                         groups: torch.Tensor, prefix_len: torch.Tensor, cu_q: torch.Tensor | None = None,
+                         scale: float | None = None, out: torch.Tensor | None = None):
+    """``attention_kv4`` with the keys that the requests of a group share read once (``qgemm_attention_kv4_shared``).
+
+    ``groups`` [G+1]: first requests of the groups; ``prefix_len`` [G]: keys that a group's requests have in common. The other
+    arguments are ``attention_kv4``'s, and so are the results, up to the order of summation."""
+    (T, H, D), qs = _need_rows(q, "q", _BF16)
+    _need(block_table, "block_table", _I32, 2)
+    _need(kv_len, "kv_len", _I32, 1)
+    _need(groups, "groups", _I32, 1)
+    _need(prefix_len, "prefix_len", _I32, 1)
+    pages, Hkv, page = _cache_sizes(cache, D)
+    R, W = block_table.shape
+    G = prefix_len.shape[0]
+    _sizes(T, H, D, R, W, G, pages, page)
+    if kv_len.shape[0] != R or (cu_q is None and T != R):
+        raise ValueError("q, block_table and kv_len disagree on the number of requests")
+    if groups.shape[0] != G + 1:
+        raise ValueError("groups must have one entry more than prefix_len")
+    if cu_q is not None:
+        _need(cu_q, "cu_q", _I32, 1)
+        if cu_q.shape[0] != R + 1:
+            raise ValueError("cu_q must have one entry more than there are requests")
+        _device(q, cu_q)
+    if out is None:
+        out = torch.empty((T, H, D), dtype=torch.bfloat16, device=q.device)
+    else:
+        _need(out, "out", _BF16, 3)
+        if out.shape != q.shape:
+            raise ValueError("out must have the shape of q")
+    need = _workspace("attention_kv4_shared", T, R, G, H, Hkv, D, W, page)
+    ws = torch.empty(need, dtype=torch.uint8, device=q.device)
+    _enqueue(lib().qgemm_attention_kv4_shared, _device(q, cache, block_table, kv_len, groups, prefix_len, out), q.data_ptr(),
+             cache.data_ptr(), block_table.data_ptr(), kv_len.data_ptr(), None if cu_q is None else cu_q.data_ptr(), groups.data_ptr(),
+             prefix_len.data_ptr(), out.data_ptr(), ws.data_ptr(), need, T, R, G, H, Hkv, D, W, pages, page, qs,
+             D ** -0.5 if scale is None else float(scale))
+    return out
+
+
+_FLAGS = (torch.bool, torch.uint8)
+
+
+def beam_select(logits: torch.Tensor, scores: torch.Tensor, count: int | None = None, finished: torch.Tensor | None = None,
+                end: int = 0):
+    """The ``count`` (by default as many as beams) best continuations of every request's beams (``qgemm_beam_select``):
+    ``(scores, parents, tokens)``, each [R][count], fp32 and int32, best first.
+
+    ``logits`` [R*B][V] fp32 or bf16, rows at any stride; ``scores`` [R][B] fp32, -inf for a beam that is not there;
+    ``finished`` [R][B] bool or uint8: beams that go on with ``end`` at their own score. Where candidates are missing the score
+    is -inf, the parent -1 and the token ``end``, so that ``tokens == end`` is the next call's ``finished``."""
+    _need(scores, "scores", (torch.float32,), 2)
+    R, B = scores.shape
+    if not isinstance(logits, torch.Tensor):
+        raise TypeError("logits must be a torch.Tensor")
+    if not logits.is_cuda:
+        raise ValueError("logits must be a GPU tensor")
+    if logits.dtype not in _ROWS:
+        raise TypeError(f"logits has dtype {logits.dtype}, expected one of {_ROWS}")
+    if logits.dim() != 2 or logits.shape[0] != R * B:
+        raise ValueError("logits must be [R*B][V]")
+    V = logits.shape[1]
+    if V > 1 and R * B and logits.stride(1) != 1:
+        raise ValueError("the logits of a row must be contiguous")
+    if finished is not None:
+        _need(finished, "finished", _FLAGS, 2)
+        if finished.shape != scores.shape:
+            raise ValueError("finished must have the shape of scores")
+        _device(logits, finished)
+    K = B if count is None else int(count)
+    _sizes(R * B, V, K, abs(int(end)))
+    dev = _device(logits, scores)
+    need = _workspace("beam_select", R, B, V, K)
+    # one allocation, as a small selection is all latency
+    buf = torch.empty(need // 4 + 3 * R * K, dtype=torch.int32, device=logits.device)
+    ws, parents, tokens, best = buf.split_with_sizes((need // 4, R * K, R * K, R * K))
+    best = best.view(torch.float32)
+    _enqueue(lib().qgemm_beam_select, dev, logits.data_ptr(), 1 if logits.dtype is torch.bfloat16 else 0, scores.data_ptr(),
+             None if finished is None else finished.data_ptr(), best.data_ptr(), parents.data_ptr(), tokens.data_ptr(), ws.data_ptr(), need,
+             R, B, V, K, logits.stride(0) if R * B > 1 else V, int(end))
+    return best.view(R, K), parents.view(R, K), tokens.view(R, K)
+
+
+class KvReorder:
+    """What ``kv_reorder`` gives: ``block_table`` [R*B][W] and ``kv_len`` [R*B] of the new rows; ``src`` and ``dst`` [R*B], the pages
+    to copy (-1: none); ``used`` [1], pages taken from the free list; ``released`` [Q] and ``n_released`` [1], the
+    pages that no row holds any more and their number. All int32 on the GPU."""
+
+    __slots__ = ("block_table", "kv_len", "src", "dst", "used", "released", "n_released")
+
+    def __init__(self, rows: int, W: int, Q: int, device):
+        n = torch.empty(rows * (W + 3) + Q + 2, dtype=torch.int32, device=device)
+        table, self.kv_len, self.src, self.dst, self.released, self.used, self.n_released = n.split_with_sizes((rows * W, rows, rows, rows, Q, 1, 1))
+        self.block_table = table.view(rows, W)
+
+
+def kv_reorder(block_table: torch.Tensor, kv_len: torch.Tensor, parents: torch.Tensor, free_pages: torch.Tensor, page: int,
+               keep: torch.Tensor | None = None, released: int | None = None, out: KvReorder | None = None) -> KvReorder:
+    """Block tables of the beams after a selection (``qgemm_kv_reorder``).
+
+    ``block_table`` [R*B][W], ``kv_len`` [R*B]: the old rows; ``parents`` [R][B]: the old row, within the request, that each new
+    one continues, or -1; ``free_pages``: where second children of a partly filled page get a page of their own;
+    ``keep`` [R]: first columns whose pages are never listed as released; ``released``: length of that list (by default that
+    of the table, which is enough for all). ``out``: an earlier result of the same sizes to write into, with no tensor
+    of it among the inputs."""
+    _need(block_table, "block_table", _I32, 2)
+    _need(kv_len, "kv_len", _I32, 1)
+    _need(parents, "parents", _I32, 2)
+    _need(free_pages, "free_pages", _I32, 1)
+    rows, W = block_table.shape
+    R, B = parents.shape
+    if R * B != rows or kv_len.shape[0] != rows:
+        raise ValueError("block_table, kv_len and parents disagree on the number of rows")
+    Q = rows * W if released is None else int(released)
+    _sizes(rows, W, free_pages.shape[0], rows * W, Q)
+    if Q < 0 or not 0 < page < 1 << 31:
+        raise ValueError("released must be >= 0, and page > 0 and below 2^31")
+    dev = _device(block_table, kv_len, parents, free_pages)
+    if keep is not None:
+        _need(keep, "keep", _I32, 1)
+        if keep.shape[0] != R:
+            raise ValueError("keep must have one entry for each request")
+        _device(block_table, keep)
+    if out is None:
+        out = KvReorder(rows, W, Q, block_table.device)
+    else:
+        for name, shape in (("block_table", (rows, W)), ("kv_len", (rows,)), ("src", (rows,)), ("dst", (rows,)), ("used", (1,)),
+                            ("released", (Q,)), ("n_released", (1,))):
+            t = getattr(out, name)
+            _need(t, "out." + name, _I32, len(shape))
+            if t.shape != shape:
+                raise ValueError(f"out.{name} must have the shape {shape}")
+        _device(block_table, *(getattr(out, name) for name in KvReorder.__slots__))
+    need = _workspace("kv_reorder", R, W)
+    ws = torch.empty(need, dtype=torch.uint8, device=block_table.device)
+    _enqueue(lib().qgemm_kv_reorder, dev, block_table.data_ptr(), kv_len.data_ptr(), parents.data_ptr(), free_pages.data_ptr(),
+             None if keep is None else keep.data_ptr(), out.block_table.data_ptr(), out.kv_len.data_ptr(), out.src.data_ptr(),
+             out.dst.data_ptr(), out.used.data_ptr(), out.released.data_ptr(), out.n_released.data_ptr(), ws.data_ptr(), need, R, B, W,
+             free_pages.shape[0], Q, page)
+    return out
+
+
+def kv4_copy(cache: torch.Tensor, src: torch.Tensor, dst: torch.Tensor, D: int | None = None):
+    """Whole pages within a cache, page ``src[i]`` to page ``dst[i]`` (``qgemm_kv4_copy``); negative numbers are skipped.
+    A page's bytes are copied as they are, so the head dimension ``D`` need not be given."""
+    _need(cache, "cache", (torch.uint8,), 3)
+    _need(src, "src", _I32, 1)
+    _need(dst, "dst", _I32, 1)
+    if src.shape != dst.shape:
+        raise ValueError("src and dst must have the same length")
+    for d in (128, 64) if D is None else (D,):
+        if cache.shape[2] * 16 % (17 * d) == 0 and cache.shape[2] * 16 // (17 * d) >= 16:
+            break
+    pages, Hkv, page = _cache_sizes(cache, d)
+    _sizes(src.shape[0], Hkv, pages, page)
+    _enqueue(lib().qgemm_kv4_copy, _device(cache, src, dst), cache.data_ptr(), src.data_ptr(), dst.data_ptr(), src.shape[0], Hkv, d, pages,
+             page)
+
+
+def adapters(y: torch.Tensor, x: torch.Tensor, a: torch.Tensor, b: torch.Tensor, ids: torch.Tensor, gain: torch.Tensor | None = None,
+             cu_q: torch.Tensor | None = None):
+    """Adds the requests' low-rank adapters to a projection's output: ``y[m] += gain[i] * b[i] @ (a[i] @ x[m])`` with ``i`` the
+    entry of ``ids`` [R] for the row's request (``qgemm_adapters``); returns ``y``.
+
+    ``y`` [M][N] fp32 and ``x`` [M][K] bf16, rows at any stride (``x``'s a multiple of 8); ``a`` [n][r][K], ``b`` [n][N][r] bf16;
+    ``gain`` [n] fp32; ``cu_q`` [R+1]: first rows of the requests, or None where each has one. Rows of an id outside [0, n)
+    are left as they are."""
+    for t, name, dtypes in ((y, "y", (torch.float32,)), (x, "x", _BF16)):
+        if not isinstance(t, torch.Tensor):
+            raise TypeError(f"{name} must be a torch.Tensor")
+        if not t.is_cuda:
+            raise ValueError(f"{name} must be a GPU tensor")
+        if t.dtype not in dtypes:
+            raise TypeError(f"{name} has dtype {t.dtype}, expected one of {dtypes}")
+        if t.dim() != 2 or (t.numel() and t.shape[1] > 1 and t.stride(1) != 1):
+            raise ValueError(f"{name} must have 2 dimensions, the last of them contiguous")
+    _need(a, "a", _BF16, 3)
+    _need(b, "b", _BF16, 3)
+    _need(ids, "ids", _I32, 1)
+    M, K = x.shape
+    n, r, _ = a.shape
+    N, R = y.shape[1], ids.shape[0]
+    if y.shape[0] != M or a.shape[2] != K or b.shape != (n, N, r):
+        raise ValueError("y, x, a and b disagree on M, N, K, the rank or the number of adapters")
+    _sizes(M, N, K, r, n, R)
+    dev = _device(y, x, a, b, ids)
+    if gain is not None:
+        _need(gain, "gain", (torch.float32,), 1)
+        if gain.shape[0] != n:
+            raise ValueError("gain must have one entry for each adapter")
+        _device(y, gain)
+    if cu_q is not None:
+        _need(cu_q, "cu_q", _I32, 1)
+        if cu_q.shape[0] != R + 1:
+            raise ValueError("cu_q must have one entry more than there are requests")
+        _device(y, cu_q)
+    elif M != R:
+        raise ValueError("without cu_q every request has one row")
+    need = _workspace("adapters", M, N, K, r)
+    ws = torch.empty(need, dtype=torch.uint8, device=y.device)
+    _enqueue(lib().qgemm_adapters, dev, x.data_ptr(), a.data_ptr(), b.data_ptr(), ids.data_ptr(), None if cu_q is None else cu_q.data_ptr(),
+             None if gain is None else gain.data_ptr(), y.data_ptr(), ws.data_ptr(), need, M, N, K, r, n, R, x.stride(0) if M > 1 else K,
+             y.stride(0) if M > 1 else N)
+    return y
 
 
 def probe_mfma_clock(iters: int = 100000):

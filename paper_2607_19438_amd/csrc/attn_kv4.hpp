@@ -28,7 +28,7 @@
 #pragma once
 
 #include "attn_kernels.hpp"
-#include "serve_kernels.hpp"
+#include "kv4_levels.hpp"
 
 namespace qg {
 namespace {
@@ -97,6 +97,10 @@ struct Kv4Request {
   __device__ __forceinline__ unsigned int weight(int Hkv) const {
     return (unsigned)tiles * (unsigned)Hkv * (unsigned)(kKv4Start + grans);
   }
+  __device__ __forceinline__ int position(int i) const { return kv - n + i; }                        // of its new token i
+  __device__ __forceinline__ int sees(int i) const { return clamp_i(kv - n + i + 1, 0, len); }       // keys
+  __device__ __forceinline__ bool past(int i) const { return kv - n + i >= len; }                    // sees keys past the table
+  static constexpr int first = 0;                                                                    // key of its granule 0
 };
 
 template <int NT>
@@ -149,6 +153,21 @@ __device__ __forceinline__ void store_row(uint16_t* p, const float (&v)[N]) {
     *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
 }
 
+// Where a unit's result goes: finished rows to the output, a share's (output, maximum, sum) to a slot.
+struct Kv4Finish {
+  bool whole;
+  float* slot;
+  // what a row's weighted values are multiplied by before they are stored, and (once a row) the row's other results
+  __device__ __forceinline__ float begin_row(const Kv4Args&, size_t, float, float sum, int position, bool) const {
+    return row_factor(sum, position);
+  }
+  __device__ __forceinline__ uint16_t* at(const Kv4Args& a, size_t i) const { return a.o + i; }
+  template <int N>
+  static __device__ __forceinline__ void store(uint16_t* p, const float (&v)[N]) {
+    store_row<N>(p, v);
+  }
+};
+
 template <int D>
 struct Kv4Keys {                  // 32 keys and values as a wave's lanes hold them
   static constexpr int DW = D / 32;
@@ -165,12 +184,17 @@ constexpr int kKv4Wide = 8;          // NT of the wide form: 128 query rows
 // Bound by the matrix cores and the softmax as that kernel is, and by the parts: 64 KiB each, written and read again, for
 // two chunks of 550 rows over 5000 keys 27 of 131 us. (The value fragments a whole step ahead, as there, take 12
 // registers too many at D = 128: 134 us.)
-template <int D>
-__device__ __forceinline__ void kv4_wide(const Kv4Args& a, const Kv4Request& rq, int r, int tile, int h, int a0, int a1,
-                                         float* slot) {
+struct Kv4WideLds {
+  uint16_t *ks0, *ks1, *vt0, *vt1;                // [64 * D] each
+  unsigned long long* nans[2];                    // value blocks of NaN: bit 4 key + quarter of each wave's 16 keys
+};
+
+template <int D, typename Rq, typename Finish>
+__device__ __forceinline__ void kv4_wide(const Kv4Args& a, const Rq& rq, int r, int tile, int h, int a0, int a1, const Finish& fin,
+                                         const Kv4WideLds& lds) {
   constexpr int BK = 64, DW = D / 32, KSTEPS = D / 16, DT = D / 32;
-  __shared__ __attribute__((aligned(16))) uint16_t ks0[BK * D], ks1[BK * D], vt0[BK * D], vt1[BK * D];
-  __shared__ unsigned long long nans[2][kKv4Waves];     // value blocks of NaN: bit 4 key + quarter of each wave's 16 keys
+  uint16_t *const ks0 = lds.ks0, *const ks1 = lds.ks1, *const vt0 = lds.vt0, *const vt1 = lds.vt1;
+  unsigned long long* const nans[2] = {lds.nans[0], lds.nans[1]};
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 31, hh = lane >> 5;
@@ -178,7 +202,7 @@ __device__ __forceinline__ void kv4_wide(const Kv4Args& a, const Kv4Request& rq,
   const int row0 = tile * 16 * kKv4Wide, nrows = rq.n * G;
   const int rho = row0 + 32 * wave + col;
   const bool live = rho < nrows;
-  auto seen_by = [&](int row) { return clamp_i(rq.kv - rq.n + row / G + 1, 0, rq.len); };     // keys that a row sees
+  auto seen_by = [&](int row) { return rq.sees(row / G); };                       // keys that a row sees
   const int lim = live ? seen_by(rho) : 0;
   const int kmax = seen_by(min(row0 + 16 * kKv4Wide, nrows) - 1);                 // keys that any row sees,
   const int wrow = row0 + 32 * wave;
@@ -196,7 +220,7 @@ __device__ __forceinline__ void kv4_wide(const Kv4Args& a, const Kv4Request& rq,
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) acc[dt] = f32x16{};
   float m_run = -__builtin_inff();
-  float l_run = live && rq.kv - rq.n + rho / G >= rq.len ? __builtin_nanf("") : 0.0f;       // sees keys past the table
+  float l_run = live && rq.past(rho / G) ? __builtin_nanf("") : 0.0f;
 
   const const_i32 trow = as_const(a.table) + (size_t)r * a.W;     // (indexed only if there is a key, so W >= 1)
   const int page_mask = (1 << a.page_log2) - 1;
@@ -212,7 +236,8 @@ __device__ __forceinline__ void kv4_wide(const Kv4Args& a, const Kv4Request& rq,
   // (as the prompt kernel's, and the four keys of 16 writing threads on different 16-byte groups too)
   auto vswz = [](int key) { return D == 128 ? 5 * (key & 3) : 5 * ((key >> 1) & 1); };
 
-  const int jb0 = a0 << (a.gran_log2 - 6), jb1 = min(a1 << (a.gran_log2 - 6), (kmax + BK - 1) / BK);
+  const int base = rq.first / BK;
+  const int jb0 = base + (a0 << (a.gran_log2 - 6)), jb1 = min(base + (a1 << (a.gran_log2 - 6)), (kmax + BK - 1) / BK);
   struct Levels {
     uint32_t k[DW], v[DW], ks, vs;
     bool ok;
@@ -381,22 +406,23 @@ __device__ __forceinline__ void kv4_wide(const Kv4Args& a, const Kv4Request& rq,
 
   // lane (col, hh) holds o[row][32 dt + 8 e + 4 hh + {0..3}] in acc[dt][4 e ..]
   const float sum = l_run + other_half(l_run);
-  if (slot == nullptr) {
+  if (fin.whole) {
     if (live) {
-      const float inv = row_factor(sum, rq.kv - rq.n + rho / G);
       const int token = rho / G;
-      uint16_t* orow = a.o + ((size_t)(rq.c0 + token) * a.H + (size_t)(h * G + (rho - token * G))) * D;
+      const size_t row = (size_t)(rq.c0 + token) * a.H + (size_t)(h * G + (rho - token * G));
+      const float by = fin.begin_row(a, row, m_run, sum, rq.position(token), hh == 0);
+      auto* out = fin.at(a, row * D);
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          *reinterpret_cast<uint2*>(orow + dt * 32 + 8 * e + 4 * hh) =
-              make_uint2(pack_bf16x2(acc[dt][4 * e] * inv, acc[dt][4 * e + 1] * inv),
-                         pack_bf16x2(acc[dt][4 * e + 2] * inv, acc[dt][4 * e + 3] * inv));
+        for (int e = 0; e < 4; ++e) {
+          const float v[4] = {acc[dt][4 * e] * by, acc[dt][4 * e + 1] * by, acc[dt][4 * e + 2] * by, acc[dt][4 * e + 3] * by};
+          fin.store(out + dt * 32 + 8 * e + 4 * hh, v);
+        }
     }
   } else {
     const int row = 32 * wave + col;
-    float* po = slot + 2 * 16 * kKv4Wide + row * D;
+    float* po = fin.slot + 2 * 16 * kKv4Wide + row * D;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
@@ -404,19 +430,330 @@ __device__ __forceinline__ void kv4_wide(const Kv4Args& a, const Kv4Request& rq,
         *reinterpret_cast<f32x4*>(po + dt * 32 + 8 * e + 4 * hh) =
             f32x4{acc[dt][4 * e], acc[dt][4 * e + 1], acc[dt][4 * e + 2], acc[dt][4 * e + 3]};
     if (hh == 0) {
-      slot[2 * row] = m_run;
-      slot[2 * row + 1] = sum;
+      fin.slot[2 * row] = m_run;
+      fin.slot[2 * row + 1] = sum;
     }
+  }
+}
+
+// A thread's places: in the workgroup, and within a record (key or value col of 16, its quarter of the row, that quarter's scale).
+template <int D>
+struct Kv4Lane {
+  int tid, lane, wave, col, grp, G, page_mask;
+  uint32_t page_bytes, k_off, v_off, ks_off, vs_off;
+  __device__ __forceinline__ explicit Kv4Lane(const Kv4Args& a) {
+    tid = threadIdx.x, lane = tid & 63;
+    wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    col = lane & 15, grp = lane >> 4;
+    G = a.H / a.Hkv;
+    page_mask = (1 << a.page_log2) - 1;
+    page_bytes = (uint32_t)a.Hkv * ((uint32_t)(D + D / 16) << a.page_log2);     // (the host keeps it below 2^31)
+    k_off = (uint32_t)(col * (D / 2) + grp * (D / 8));
+    v_off = k_off + ((uint32_t)(D / 2) << a.page_log2);
+    ks_off = ((uint32_t)D << a.page_log2) + (uint32_t)(col * (D / 32) + (D == 128 ? grp : grp >> 1));
+    vs_off = ks_off + ((uint32_t)(D / 32) << a.page_log2);
+  }
+};
+
+// A unit's share of 16 NT query rows: the four waves take every fourth run of 32 keys and are joined at the end.
+template <int D, int NT, typename Rq, typename Finish>
+__device__ __forceinline__ void kv4_tile(const Kv4Args& a, const Rq& rq, int r, int tile, int h, int a0, int a1, const Finish& fin,
+                                         const Kv4Lane<D>& L, uint16_t (&vbuf)[kKv4Waves][32 * D], float (&ml)[kKv4Waves][16 * NT][2]) {
+  constexpr int DW = D / 32;            // dwords of packed levels in a lane: a quarter of a key's row
+  constexpr int DT = D / 16;            // 16-row tiles of O^T
+  constexpr int CH = D / 16;            // dimensions of a thread where parts are joined
+  const int row0 = tile * 16 * NT;
+  const int lane = L.lane, wave = L.wave, col = L.col, grp = L.grp, G = L.G, tid = L.tid;
+  const int page_mask = L.page_mask;
+  const uint32_t page_bytes = L.page_bytes, k_off = L.k_off, v_off = L.v_off, ks_off = L.ks_off, vs_off = L.vs_off;
+  uint16_t* vw = vbuf[wave];
+  auto vswz = [](int key) {
+    const int low = 2 * (key & 3) | ((key >> 2) & 1);
+    return D == 128 ? low | (key & 8) : low;
+  };
+
+  // this lane's query rows
+  const int nrows = rq.n * G;
+  int lim[NT];                                    // keys that the row sees
+  bf16x8 qf[NT][DW];
+  f32x4 l_run[NT];                              // sum of the weights as they enter the product, four times
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const int rho = row0 + 16 * nt + col;
+    const int i = rho / G;
+    const bool live = rho < nrows;
+    lim[nt] = live ? rq.sees(i) : 0;
+    l_run[nt] = f32x4{} + (live && rq.past(i) ? __builtin_nanf("") : 0.0f);
+    const uint16_t* qp = a.q + (size_t)(rq.c0 + i) * a.qs + (size_t)(h * G + (rho - i * G)) * D + grp * (D / 4);
+#pragma unroll
+    for (int t = 0; t < DW; ++t)
+      qf[nt][t] = live ? __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(qp + 8 * t)) : bf16x8{};
+  }
+  const int last = (min(row0 + 16 * NT, nrows) - 1) / G;
+  const int kmax = rq.sees(last);                             // keys that any row sees
+  const int kall = rq.sees(row0 / G);                         // keys that every row sees
+
+  f32x4 acc[NT][DT];
+  float m_run[NT];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    m_run[nt] = -__builtin_inff();
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) acc[nt][dt] = f32x4{};
+  }
+
+  const const_i32 trow = as_const(a.table) + (size_t)r * a.W;      // (indexed only if there is a key, so W >= 1)
+  const int base = rq.first / kKv4Step;
+  const int s_end = min(base + (a1 << (a.gran_log2 - kKv4StepLog2)), (kmax + kKv4Step - 1) / kKv4Step);
+  const uint8_t* cache_h = a.cache + (size_t)h * ((uint32_t)(D + D / 16) << a.page_log2);
+  // pages of the two halves of a step (the last step's second half, or the step after it, may be past the table)
+  auto pages_of = [&](int s) {
+    const int key = kKv4Step * s;
+    return make_int2(trow[min(key >> a.page_log2, a.W - 1)], trow[min((key + 16) >> a.page_log2, a.W - 1)]);
+  };
+  auto load = [&](int s, int2 ids) {
+    Kv4Keys<D> b;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int key = kKv4Step * s + 16 * i;
+      const int id = i ? ids.y : ids.x;
+      b.ok[i] = (unsigned)id < (unsigned)a.pages;
+      // the addresses' parts that all lanes share are scalar, the lanes' own do not change
+      const uint8_t* rec = cache_h + (uint64_t)(b.ok[i] ? (uint32_t)id : 0u) * page_bytes;
+      const uint32_t in_page = (uint32_t)(key & page_mask);
+      const uint8_t* codes = rec + in_page * (D / 2);
+      const uint8_t* scales = rec + in_page * (D / 32);
+      if constexpr (DW == 4) {
+        const u32x4 k4 = *reinterpret_cast<const u32x4*>(codes + k_off);
+        const u32x4 v4 = *reinterpret_cast<const u32x4*>(codes + v_off);
+#pragma unroll
+        for (int t = 0; t < DW; ++t) b.k[i][t] = k4[t], b.v[i][t] = v4[t];
+      } else {
+        const uint2 k2 = *reinterpret_cast<const uint2*>(codes + k_off);
+        const uint2 v2 = *reinterpret_cast<const uint2*>(codes + v_off);
+        b.k[i][0] = k2.x, b.k[i][1] = k2.y, b.v[i][0] = v2.x, b.v[i][1] = v2.y;
+      }
+      b.ks[i] = scales[ks_off];
+      b.vs[i] = scales[vs_off];
+    }
+    return b;
+  };
+
+  auto step = [&](Kv4Keys<D>& b, int s) {
+    const int key0 = kKv4Step * s;
+    const bool need_mask = key0 + kKv4Step > kall;
+    if (!(b.ok[0] && b.ok[1])) {          // a page that is none reads as NaN
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        if (!b.ok[i]) b.ks[i] = b.vs[i] = 255u;
+    }
+    f32x4 sc[NT][2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float unit = __builtin_bit_cast(float, b.ks[i] << 23);
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) sc[nt][i] = f32x4{};
+#pragma unroll
+      for (int t = 0; t < DW; ++t) {
+        const bf16x8 kf = __builtin_bit_cast(bf16x8, fp4_unit(b.k[i][t], unit));
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+          sc[nt][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[nt][t], sc[nt][i], 0, 0, 0);
+      }
+    }
+    // Values that no row may see are taken as zero, and NaN blocks too (a weight of 0 would not keep a NaN
+    // out of the product); rows that do see a NaN block get it below.
+    if (need_mask) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const bool hidden = key0 + 16 * i + col >= kmax;
+        b.vs[i] = hidden ? 0u : b.vs[i];
+#pragma unroll
+        for (int t = 0; t < DW; ++t) b.v[i][t] = hidden ? 0u : b.v[i][t];
+      }
+    }
+    const unsigned long long nan_at[2] = {__ballot(b.vs[0] >= kKv4NaN), __ballot(b.vs[1] >= kKv4NaN)};
+    if (nan_at[0] | nan_at[1]) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const bool nan = b.vs[i] >= kKv4NaN;
+        b.vs[i] = nan ? 0u : b.vs[i];
+#pragma unroll
+        for (int t = 0; t < DW; ++t) b.v[i][t] = nan ? 0u : b.v[i][t];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float unit = __builtin_bit_cast(float, b.vs[i] << 23);
+      const int key = 16 * i + col;
+#pragma unroll
+      for (int t = 0; t < DW; ++t)
+        *reinterpret_cast<u32x4*>(&vw[key * D + (((grp * DW + t) ^ vswz(key)) << 3)]) = fp4_unit(b.v[i][t], unit);
+    }
+    bf16x8 pb[NT];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      if (need_mask) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (key0 + 16 * i + 4 * grp + e >= lim[nt]) sc[nt][i][e] = -__builtin_inff();
+      }
+      float mloc = max3(max3(sc[nt][0][0], sc[nt][0][1], sc[nt][0][2]), max3(sc[nt][0][3], sc[nt][1][0], sc[nt][1][1]),
+                        max3(sc[nt][1][2], sc[nt][1][3], sc[nt][1][3]));
+      // The reference maximum moves, for all rows of the wave, only when some score passes its row's by more
+      // than 8 in exp2 units: weights stay <= 2^8, and most steps exchange nothing between lanes.
+      if (__any((mloc - m_run[nt]) * a.sl2 > 8.0f)) {
+        const float m_new = fmaxf(m_run[nt], max_over_groups(mloc));
+        const float alpha = m_new == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f((m_run[nt] - m_new) * a.sl2);
+        l_run[nt] *= alpha;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) acc[nt][dt] *= alpha;
+        m_run[nt] = m_new;
+      }
+      const float ms = m_run[nt] == -__builtin_inff() ? 0.0f : m_run[nt] * a.sl2;
+      float p[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[nt][e >> 2][e & 3], a.sl2, -ms));
+      pb[nt] = __builtin_bit_cast(bf16x8, u32x4{pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]),
+                                                pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7])});
+    }
+    // the weights' sum as a product with ones: rounded as they are, so that their rounding cancels where few weigh
+    const bf16x8 ones = __builtin_bit_cast(bf16x8, u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u});
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) l_run[nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pb[nt], l_run[nt], 0, 0, 0);
+    asm volatile("" ::: "memory");       // the tile's writes stay before its reads; a wave's LDS accesses run in order
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+      uint32_t f[4];
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const int key = 16 * half + 4 * grp + (col >> 2);
+        const int dim = 16 * dt + 4 * (lane & 3);
+        typedef short v4i16 __attribute__((ext_vector_type(4)));
+        const v4i16 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (__attribute__((address_space(3))) v4i16*)(vw + key * D + (((dim >> 3) ^ vswz(key)) << 3) + (dim & 7)));
+        const uint2 xx = __builtin_bit_cast(uint2, x);
+        f[2 * half] = xx.x;
+        f[2 * half + 1] = xx.y;
+      }
+      const bf16x8 vf = __builtin_bit_cast(bf16x8, u32x4{f[0], f[1], f[2], f[3]});
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+        acc[nt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pb[nt], acc[nt][dt], 0, 0, 0);
+    }
+    asm volatile("" ::: "memory");       // and the next tile's writes after them
+    if (nan_at[0] | nan_at[1]) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const uint32_t seen = (1u << clamp_i(lim[nt] - key0 - 16 * i, 0, 16)) - 1u;
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt) {
+            const uint32_t keys = (uint32_t)(nan_at[i] >> (D == 128 ? 16 * (dt >> 1) : 32 * (dt >> 1))) & 0xffffu;
+            if (keys & seen) acc[nt][dt] = f32x4{} + __builtin_nanf("");
+          }
+        }
+    }
+  };
+
+  // kKv4Bufs steps of keys and values in registers: while one is computed the others are in flight, and the page
+  // numbers of the next to be loaded. Every refill is issued, past the last step once more for that step: were
+  // it skipped, the compiler could not tell how many loads are behind the one a step waits for, and would wait
+  // for all of them.
+  if (base + (a0 << (a.gran_log2 - kKv4StepLog2)) + wave < s_end) {
+    int s = base + (a0 << (a.gran_log2 - kKv4StepLog2)) + wave, sl = s;
+    const int s_last = s + ((s_end - 1 - s) & ~(kKv4Waves - 1));
+    int2 ids = pages_of(s);
+    Kv4Keys<D> buf[kKv4Bufs];
+    auto refill = [&](Kv4Keys<D>& b) {
+      b = load(sl, ids);
+      sl = min(sl + kKv4Waves, s_last);
+      ids = pages_of(sl);
+    };
+#pragma unroll
+    for (int j = 0; j < kKv4Bufs; ++j) refill(buf[j]);
+    for (bool more = true; more;) {
+#pragma unroll
+      for (int j = 0; j < kKv4Bufs; ++j) {
+        step(buf[j], s);
+        s += kKv4Waves;
+        if (s >= s_end) {
+          more = false;
+          break;
+        }
+        refill(buf[j]);
+      }
+    }
+  }
+
+  // join the four waves, 16 rows at a time
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    float* ow = reinterpret_cast<float*>(vw);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+      *reinterpret_cast<f32x4*>(&ow[col * D + (((4 * dt + grp) ^ (col & 7)) << 2)]) = acc[nt][dt];
+    if (grp == 0) {
+      ml[wave][16 * nt + col][0] = m_run[nt];
+      ml[wave][16 * nt + col][1] = l_run[nt][0];
+    }
+    __syncthreads();
+    const int row = tid >> 4, ch = tid & 15;
+    float mw[kKv4Waves], top = -__builtin_inff();
+#pragma unroll
+    for (int i = 0; i < kKv4Waves; ++i) {
+      mw[i] = ml[i][16 * nt + row][0];
+      top = fmaxf(top, mw[i]);
+    }
+    float sum = 0.0f, out[CH] = {};
+#pragma unroll
+    for (int i = 0; i < kKv4Waves; ++i) {
+      const float wt = part_weight(mw[i], top, a.sl2);
+      const float li = ml[i][16 * nt + row][1];
+      sum += mw[i] == -__builtin_inff() ? li : wt * li;     // an empty part's 0, or NaN
+      const float* oi = reinterpret_cast<const float*>(vbuf[i]);
+#pragma unroll
+      for (int c = 0; c < CH / 4; ++c) {
+        const f32x4 x = *reinterpret_cast<const f32x4*>(&oi[row * D + (((ch * (CH / 4) + c) ^ (row & 7)) << 2)]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) out[4 * c + e] += wt * x[e];
+      }
+    }
+    const int rho = row0 + 16 * nt + row;
+    if (fin.whole) {
+      if (rho < nrows) {
+        const int i = rho / G;
+        const size_t at = (size_t)(rq.c0 + i) * a.H + (size_t)(h * G + (rho - i * G));
+        const float by = fin.begin_row(a, at, top, sum, rq.position(i), ch == 0);
+#pragma unroll
+        for (int e = 0; e < CH; ++e) out[e] *= by;
+        fin.store(fin.at(a, at * D + ch * CH), out);
+      }
+    } else {
+      float* po = fin.slot + 2 * 16 * NT + (16 * nt + row) * D + ch * CH;
+#pragma unroll
+      for (int c = 0; c < CH / 4; ++c)
+        *reinterpret_cast<f32x4*>(po + 4 * c) = f32x4{out[4 * c], out[4 * c + 1], out[4 * c + 2], out[4 * c + 3]};
+      if (ch == 0) {
+        fin.slot[2 * (16 * nt + row)] = top;
+        fin.slot[2 * (16 * nt + row) + 1] = sum;
+      }
+    }
+    __syncthreads();
   }
 }
 
 template <int D, int NT>
 __device__ __forceinline__ void kv4_body(const Kv4Args& a) {
-  constexpr int DW = D / 32;            // dwords of packed levels in a lane: a quarter of a key's row
-  constexpr int DT = D / 16;            // 16-row tiles of O^T
-  constexpr int CH = D / 16;            // dimensions of a thread where parts are joined
-  __shared__ __attribute__((aligned(16))) uint16_t vbuf[kKv4Waves][NT == kKv4Wide ? 8 : 32 * D];     // also 16 rows of O in fp32
-  __shared__ float ml[kKv4Waves][NT == kKv4Wide ? 1 : 16 * NT][2];
+  constexpr bool kWide = NT == kKv4Wide;
+  __shared__ __attribute__((aligned(16))) uint16_t vbuf[kKv4Waves][kWide ? 8 : 32 * D];     // also 16 rows of O in fp32
+  __shared__ float ml[kKv4Waves][kWide ? 1 : 16 * NT][2];
+  __shared__ __attribute__((aligned(16))) uint16_t ks0[kWide ? 64 * D : 8], ks1[kWide ? 64 * D : 8], vt0[kWide ? 64 * D : 8],
+      vt1[kWide ? 64 * D : 8];
+  __shared__ unsigned long long nans[2][kKv4Waves];
   __shared__ unsigned int wsum[kKv4Waves];
   __shared__ struct {
     int r, off, c0, n, kv;
@@ -424,7 +761,6 @@ __device__ __forceinline__ void kv4_body(const Kv4Args& a) {
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int col = lane & 15, grp = lane >> 4;
   const int G = a.H / a.Hkv;
   const int w = xcd_tile((int)blockIdx.x, a.nwg);
 
@@ -499,306 +835,23 @@ __device__ __forceinline__ void kv4_body(const Kv4Args& a) {
   bool first_segment = true;
   Kv4Head header{-1};
 
-  const int page_mask = (1 << a.page_log2) - 1;
-  const uint32_t page_bytes = (uint32_t)a.Hkv * ((uint32_t)(D + D / 16) << a.page_log2);     // (the host keeps it below 2^31)
-  // this lane's places within a record: key (or value) col of 16, its quarter of the row, that quarter's scale
-  const uint32_t k_off = (uint32_t)(col * (D / 2) + grp * (D / 8));
-  const uint32_t v_off = k_off + ((uint32_t)(D / 2) << a.page_log2);
-  const uint32_t ks_off = ((uint32_t)D << a.page_log2) + (uint32_t)(col * (D / 32) + (D == 128 ? grp : grp >> 1));
-  const uint32_t vs_off = ks_off + ((uint32_t)(D / 32) << a.page_log2);
-  uint16_t* vw = vbuf[wave];
-  auto vswz = [](int key) {
-    const int low = 2 * (key & 3) | ((key >> 2) & 1);
-    return D == 128 ? low | (key & 8) : low;
-  };
-
+  const Kv4Lane<D> places(a);
   while (g < ge) {
     // the unit's share, its start's granules left out: with nothing but those it is left to the next workgroup
     const int v1 = (int)min((unsigned)(kKv4Start + rq.grans), (unsigned)gi + (ge - g));
     const int a0 = max(0, gi - kKv4Start), a1 = v1 - kKv4Start;
     if (a1 > a0) {
       const bool whole = a0 == 0 && a1 == rq.grans;
-      float* slot = a.part + (size_t)(2 * w + (first_segment ? 0 : 1)) * kKv4PartFloats<D, NT>;
-      const int row0 = tile * 16 * NT;
+      const Kv4Finish fin{whole, a.part + (size_t)(2 * w + (first_segment ? 0 : 1)) * kKv4PartFloats<D, NT>};
       if constexpr (NT == kKv4Wide) {
-        kv4_wide<D>(a, rq, r, tile, h, a0, a1, whole ? nullptr : slot);
+        kv4_wide<D>(a, rq, r, tile, h, a0, a1, fin, Kv4WideLds{ks0, ks1, vt0, vt1, {nans[0], nans[1]}});
       } else {
-        // this lane's query rows
-        const int nrows = rq.n * G;
-        int lim[NT];                                    // keys that the row sees
-        bf16x8 qf[NT][DW];
-        f32x4 l_run[NT];                              // sum of the weights as they enter the product, four times
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          const int rho = row0 + 16 * nt + col;
-          const int i = rho / G;
-          const bool live = rho < nrows;
-          lim[nt] = live ? clamp_i(rq.kv - rq.n + i + 1, 0, rq.len) : 0;
-          l_run[nt] = f32x4{} + (live && rq.kv - rq.n + i >= rq.len ? __builtin_nanf("") : 0.0f);     // sees keys past the table
-          const uint16_t* qp = a.q + (size_t)(rq.c0 + i) * a.qs + (size_t)(h * G + (rho - i * G)) * D + grp * (D / 4);
-#pragma unroll
-          for (int t = 0; t < DW; ++t)
-            qf[nt][t] = live ? __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(qp + 8 * t)) : bf16x8{};
-        }
-        const int last = (min(row0 + 16 * NT, nrows) - 1) / G;
-        const int kmax = clamp_i(rq.kv - rq.n + last + 1, 0, rq.len);           // keys that any row sees
-        const int kall = clamp_i(rq.kv - rq.n + row0 / G + 1, 0, rq.len);       // keys that every row sees
-
-        f32x4 acc[NT][DT];
-        float m_run[NT];
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          m_run[nt] = -__builtin_inff();
-#pragma unroll
-          for (int dt = 0; dt < DT; ++dt) acc[nt][dt] = f32x4{};
-        }
-
-        const const_i32 trow = as_const(a.table) + (size_t)r * a.W;      // (indexed only if there is a key, so W >= 1)
-        const int s_end = min(a1 << (a.gran_log2 - kKv4StepLog2), (kmax + kKv4Step - 1) / kKv4Step);
-        const uint8_t* cache_h = a.cache + (size_t)h * ((uint32_t)(D + D / 16) << a.page_log2);
-        // pages of the two halves of a step (the last step's second half, or the step after it, may be past the table)
-        auto pages_of = [&](int s) {
-          const int key = kKv4Step * s;
-          return make_int2(trow[min(key >> a.page_log2, a.W - 1)], trow[min((key + 16) >> a.page_log2, a.W - 1)]);
-        };
-        auto load = [&](int s, int2 ids) {
-          Kv4Keys<D> b;
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const int key = kKv4Step * s + 16 * i;
-            const int id = i ? ids.y : ids.x;
-            b.ok[i] = (unsigned)id < (unsigned)a.pages;
-            // the addresses' parts that all lanes share are scalar, the lanes' own do not change
-            const uint8_t* rec = cache_h + (uint64_t)(b.ok[i] ? (uint32_t)id : 0u) * page_bytes;
-            const uint32_t in_page = (uint32_t)(key & page_mask);
-            const uint8_t* codes = rec + in_page * (D / 2);
-            const uint8_t* scales = rec + in_page * (D / 32);
-            if constexpr (DW == 4) {
-              const u32x4 k4 = *reinterpret_cast<const u32x4*>(codes + k_off);
-              const u32x4 v4 = *reinterpret_cast<const u32x4*>(codes + v_off);
-#pragma unroll
-              for (int t = 0; t < DW; ++t) b.k[i][t] = k4[t], b.v[i][t] = v4[t];
-            } else {
-              const uint2 k2 = *reinterpret_cast<const uint2*>(codes + k_off);
-              const uint2 v2 = *reinterpret_cast<const uint2*>(codes + v_off);
-              b.k[i][0] = k2.x, b.k[i][1] = k2.y, b.v[i][0] = v2.x, b.v[i][1] = v2.y;
-            }
-            b.ks[i] = scales[ks_off];
-            b.vs[i] = scales[vs_off];
-          }
-          return b;
-        };
-
-        auto step = [&](Kv4Keys<D>& b, int s) {
-          const int key0 = kKv4Step * s;
-          const bool need_mask = key0 + kKv4Step > kall;
-          if (!(b.ok[0] && b.ok[1])) {          // a page that is none reads as NaN
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-              if (!b.ok[i]) b.ks[i] = b.vs[i] = 255u;
-          }
-          f32x4 sc[NT][2];
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const float unit = __builtin_bit_cast(float, b.ks[i] << 23);
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) sc[nt][i] = f32x4{};
-#pragma unroll
-            for (int t = 0; t < DW; ++t) {
-              const bf16x8 kf = __builtin_bit_cast(bf16x8, fp4_unit(b.k[i][t], unit));
-#pragma unroll
-              for (int nt = 0; nt < NT; ++nt)
-                sc[nt][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[nt][t], sc[nt][i], 0, 0, 0);
-            }
-          }
-          // Values that no row may see are taken as zero, and NaN blocks too (a weight of 0 would not keep a NaN
-          // out of the product); rows that do see a NaN block get it below.
-          if (need_mask) {
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              const bool hidden = key0 + 16 * i + col >= kmax;
-              b.vs[i] = hidden ? 0u : b.vs[i];
-#pragma unroll
-              for (int t = 0; t < DW; ++t) b.v[i][t] = hidden ? 0u : b.v[i][t];
-            }
-          }
-          const unsigned long long nan_at[2] = {__ballot(b.vs[0] >= kKv4NaN), __ballot(b.vs[1] >= kKv4NaN)};
-          if (nan_at[0] | nan_at[1]) {
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              const bool nan = b.vs[i] >= kKv4NaN;
-              b.vs[i] = nan ? 0u : b.vs[i];
-#pragma unroll
-              for (int t = 0; t < DW; ++t) b.v[i][t] = nan ? 0u : b.v[i][t];
-            }
-          }
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const float unit = __builtin_bit_cast(float, b.vs[i] << 23);
-            const int key = 16 * i + col;
-#pragma unroll
-            for (int t = 0; t < DW; ++t)
-              *reinterpret_cast<u32x4*>(&vw[key * D + (((grp * DW + t) ^ vswz(key)) << 3)]) = fp4_unit(b.v[i][t], unit);
-          }
-          bf16x8 pb[NT];
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            if (need_mask) {
-#pragma unroll
-              for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                  if (key0 + 16 * i + 4 * grp + e >= lim[nt]) sc[nt][i][e] = -__builtin_inff();
-            }
-            float mloc = max3(max3(sc[nt][0][0], sc[nt][0][1], sc[nt][0][2]), max3(sc[nt][0][3], sc[nt][1][0], sc[nt][1][1]),
-                              max3(sc[nt][1][2], sc[nt][1][3], sc[nt][1][3]));
-            // The reference maximum moves, for all rows of the wave, only when some score passes its row's by more
-            // than 8 in exp2 units: weights stay <= 2^8, and most steps exchange nothing between lanes.
-            if (__any((mloc - m_run[nt]) * a.sl2 > 8.0f)) {
-              const float m_new = fmaxf(m_run[nt], max_over_groups(mloc));
-              const float alpha = m_new == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f((m_run[nt] - m_new) * a.sl2);
-              l_run[nt] *= alpha;
-#pragma unroll
-              for (int dt = 0; dt < DT; ++dt) acc[nt][dt] *= alpha;
-              m_run[nt] = m_new;
-            }
-            const float ms = m_run[nt] == -__builtin_inff() ? 0.0f : m_run[nt] * a.sl2;
-            float p[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[nt][e >> 2][e & 3], a.sl2, -ms));
-            pb[nt] = __builtin_bit_cast(bf16x8, u32x4{pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]),
-                                                      pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7])});
-          }
-          // the weights' sum as a product with ones: rounded as they are, so that their rounding cancels where few weigh
-          const bf16x8 ones = __builtin_bit_cast(bf16x8, u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u});
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) l_run[nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pb[nt], l_run[nt], 0, 0, 0);
-          asm volatile("" ::: "memory");       // the tile's writes stay before its reads; a wave's LDS accesses run in order
-#pragma unroll
-          for (int dt = 0; dt < DT; ++dt) {
-            uint32_t f[4];
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-              const int key = 16 * half + 4 * grp + (col >> 2);
-              const int dim = 16 * dt + 4 * (lane & 3);
-              typedef short v4i16 __attribute__((ext_vector_type(4)));
-              const v4i16 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                  (__attribute__((address_space(3))) v4i16*)(vw + key * D + (((dim >> 3) ^ vswz(key)) << 3) + (dim & 7)));
-              const uint2 xx = __builtin_bit_cast(uint2, x);
-              f[2 * half] = xx.x;
-              f[2 * half + 1] = xx.y;
-            }
-            const bf16x8 vf = __builtin_bit_cast(bf16x8, u32x4{f[0], f[1], f[2], f[3]});
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-              acc[nt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pb[nt], acc[nt][dt], 0, 0, 0);
-          }
-          asm volatile("" ::: "memory");       // and the next tile's writes after them
-          if (nan_at[0] | nan_at[1]) {
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-              for (int i = 0; i < 2; ++i) {
-                const uint32_t seen = (1u << clamp_i(lim[nt] - key0 - 16 * i, 0, 16)) - 1u;
-#pragma unroll
-                for (int dt = 0; dt < DT; ++dt) {
-                  const uint32_t keys = (uint32_t)(nan_at[i] >> (D == 128 ? 16 * (dt >> 1) : 32 * (dt >> 1))) & 0xffffu;
-                  if (keys & seen) acc[nt][dt] = f32x4{} + __builtin_nanf("");
-                }
-              }
-          }
-        };
-
-        // kKv4Bufs steps of keys and values in registers: while one is computed the others are in flight, and the page
-        // numbers of the next to be loaded. Every refill is issued, past the last step once more for that step: were
-        // it skipped, the compiler could not tell how many loads are behind the one a step waits for, and would wait
-        // for all of them.
-        if ((a0 << (a.gran_log2 - kKv4StepLog2)) + wave < s_end) {
-          int s = (a0 << (a.gran_log2 - kKv4StepLog2)) + wave, sl = s;
-          const int s_last = s + ((s_end - 1 - s) & ~(kKv4Waves - 1));
-          int2 ids = pages_of(s);
-          Kv4Keys<D> buf[kKv4Bufs];
-          auto refill = [&](Kv4Keys<D>& b) {
-            b = load(sl, ids);
-            sl = min(sl + kKv4Waves, s_last);
-            ids = pages_of(sl);
-          };
-#pragma unroll
-          for (int j = 0; j < kKv4Bufs; ++j) refill(buf[j]);
-          for (bool more = true; more;) {
-#pragma unroll
-            for (int j = 0; j < kKv4Bufs; ++j) {
-              step(buf[j], s);
-              s += kKv4Waves;
-              if (s >= s_end) {
-                more = false;
-                break;
-              }
-              refill(buf[j]);
-            }
-          }
-        }
-
-        // join the four waves, 16 rows at a time
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          float* ow = reinterpret_cast<float*>(vw);
-#pragma unroll
-          for (int dt = 0; dt < DT; ++dt)
-            *reinterpret_cast<f32x4*>(&ow[col * D + (((4 * dt + grp) ^ (col & 7)) << 2)]) = acc[nt][dt];
-          if (grp == 0) {
-            ml[wave][16 * nt + col][0] = m_run[nt];
-            ml[wave][16 * nt + col][1] = l_run[nt][0];
-          }
-          __syncthreads();
-          const int row = tid >> 4, ch = tid & 15;
-          float mw[kKv4Waves], top = -__builtin_inff();
-#pragma unroll
-          for (int i = 0; i < kKv4Waves; ++i) {
-            mw[i] = ml[i][16 * nt + row][0];
-            top = fmaxf(top, mw[i]);
-          }
-          float sum = 0.0f, out[CH] = {};
-#pragma unroll
-          for (int i = 0; i < kKv4Waves; ++i) {
-            const float wt = part_weight(mw[i], top, a.sl2);
-            const float li = ml[i][16 * nt + row][1];
-            sum += mw[i] == -__builtin_inff() ? li : wt * li;     // an empty part's 0, or NaN
-            const float* oi = reinterpret_cast<const float*>(vbuf[i]);
-#pragma unroll
-            for (int c = 0; c < CH / 4; ++c) {
-              const f32x4 x = *reinterpret_cast<const f32x4*>(&oi[row * D + (((ch * (CH / 4) + c) ^ (row & 7)) << 2)]);
-#pragma unroll
-              for (int e = 0; e < 4; ++e) out[4 * c + e] += wt * x[e];
-            }
-          }
-          const int rho = row0 + 16 * nt + row;
-          if (whole) {
-            if (rho < nrows) {
-              const int i = rho / G;
-              const float inv = row_factor(sum, rq.kv - rq.n + i);
-#pragma unroll
-              for (int e = 0; e < CH; ++e) out[e] *= inv;
-              store_row<CH>(a.o + ((size_t)(rq.c0 + i) * a.H + (size_t)(h * G + (rho - i * G))) * D + ch * CH, out);
-            }
-          } else {
-            float* po = slot + 2 * 16 * NT + (16 * nt + row) * D + ch * CH;
-#pragma unroll
-            for (int c = 0; c < CH / 4; ++c)
-              *reinterpret_cast<f32x4*>(po + 4 * c) = f32x4{out[4 * c], out[4 * c + 1], out[4 * c + 2], out[4 * c + 3]};
-            if (ch == 0) {
-              slot[2 * (16 * nt + row)] = top;
-              slot[2 * (16 * nt + row) + 1] = sum;
-            }
-          }
-          __syncthreads();
-        }
-
+        kv4_tile<D, NT>(a, rq, r, tile, h, a0, a1, fin, places, vbuf, ml);
       }
       if (a0 == 0 && a1 < rq.grans) {          // the unit goes on: this workgroup's block of the second kernel joins it
         const unsigned int end = g + (unsigned)(kKv4Start + rq.grans - gi) - 1, wide = more * (each + 1);   // its last granule,
         const unsigned int last_w = end < wide ? end / (each + 1) : more + (end - wide) / each;             // in workgroup:
-        header = {r, (int)last_w, first_segment ? 0 : 1, rq.c0, rq.n * G, row0, h, 0};
+        header = {r, (int)last_w, first_segment ? 0 : 1, rq.c0, rq.n * G, tile * 16 * NT, h, 0};
       }
       first_segment = false;
     }

@@ -1,0 +1,450 @@
+// Attention over the paged 4-bit cache for requests that share their first keys: a group's common keys are read once
+// for all of its rows.
+//
+// The rows of a group, one request after another, are the rows of one unit over the shared keys (a tile of them, a
+// key/value head), and every request's rows are those of a unit over the keys behind them. Both leave (output, maximum,
+// sum) of their rows, and a second kernel joins the two. The softmax of a row is one over both sets of keys:
+//   m = max(m_p, m_t),  l = l_p e^(m_p - m) + l_t e^(m_t - m),  o = (o_p e^(m_p - m) + o_t e^(m_t - m)) / l.
+// A shared key is read once instead of once per request, so what bounds the call moves from the cache's bytes to the
+// matrix cores, which see 16 to 128 rows of a key where they saw the few query heads of one.
+//
+// Units over shared keys and units behind them are two sequences of granules, each cut evenly over workgroups of its
+// own, as the units of the kernel over single requests are; the workgroups are dealt to the two by what their granules
+// cost, and alternate over the chip, so that a CU holds some of both: one kind is bound by the matrix cores, the
+// other by loads.
+//
+// Shared are the keys that all of a group's rows see: the prefix as given is cut to the shortest history before the
+// new tokens, and to blocks of 64, so that no unit over shared keys needs a mask and no unit behind them begins inside
+// a block.
+#pragma once
+
+#include "attn_kv4.hpp"
+
+namespace qg {
+namespace {
+
+constexpr int kSharedMaxR = 4096;          // requests (and groups, each of which takes 12 bytes of LDS)
+constexpr int kSharedBlock = 64;           // shared keys come in blocks of so many
+
+struct SharedRow {          // where a request's rows have their results
+  int c0, n, first;         // its first row and rows; shared keys
+  unsigned base, grans;     // of the keys behind them: first granule of its first unit, granules of each
+  int pre_c0;               // first row of its group
+  unsigned pre_base, pre_grans;
+};
+
+struct SharedCut {          // of the workgroups: `np` over shared keys; each + 1 granules for the first `more` of a kind
+  int ok, np;
+  unsigned each[2], more[2];
+};
+
+struct SharedArgs {
+  Kv4Args k;
+  const int32_t* groups;    // [Gn + 1]
+  const int32_t* prefix;    // [Gn]
+  int Gn;
+  int cost;                 // of a granule over shared keys, in sixteenths of one behind them
+  SharedCut* cut;
+  SharedRow* rows;          // [R]
+  float* whole;             // [2][T * H][D] rows of units that one workgroup has finished: shared keys, others
+  float* whole_ml;          // [2][T * H][2] their maxima and sums
+  long part_floats;         // of one slot of k.part
+};
+
+// A unit's rows and keys as the tile functions see them.
+struct SharedUnit {
+  int c0, n, kv, len, tiles, grans;
+  int first;                // key of its granule 0
+  bool pre;                 // over shared keys, of which every row sees all
+  template <int NT>
+  __device__ __forceinline__ void size(const Kv4Args& a, int G) {
+    tiles = (n * G + 16 * NT - 1) / (16 * NT);
+    grans = (len - first + (1 << kKv4GranuleLog2) - 1) >> kKv4GranuleLog2;
+    grans = pre ? grans : max(1, grans);
+  }
+  __device__ __forceinline__ unsigned weight(int Hkv) const {
+    return grans == 0 ? 0u : (unsigned)tiles * (unsigned)Hkv * (unsigned)(kKv4Start + grans);
+  }
+  __device__ __forceinline__ int position(int i) const { return kv - n + i; }
+  __device__ __forceinline__ int sees(int i) const { return pre ? len : clamp_i(kv - n + i + 1, 0, len); }
+  __device__ __forceinline__ bool past(int i) const { return !pre && kv - n + i >= len; }
+};
+
+// Rows that are whole go, unscaled, to the place of their own; the others to the workgroup's slot.
+template <int D>
+struct SharedFinish {
+  bool whole;
+  float* slot;
+  float* rows;
+  float* ml;
+  __device__ __forceinline__ float begin_row(const Kv4Args&, size_t row, float m, float sum, int, bool once) const {
+    if (once) *reinterpret_cast<float2*>(ml + 2 * row) = make_float2(m, sum);
+    return 1.0f;
+  }
+  __device__ __forceinline__ float* at(const Kv4Args&, size_t i) const { return rows + i; }
+  template <int N>
+  static __device__ __forceinline__ void store(float* p, const float (&v)[N]) {
+#pragma unroll
+    for (int e = 0; e < N; e += 4) *reinterpret_cast<f32x4*>(p + e) = f32x4{v[e], v[e + 1], v[e + 2], v[e + 3]};
+  }
+};
+
+template <int D, bool WIDE, int NT>
+struct SharedTileLds {
+  uint16_t vbuf[kKv4Waves][32 * D];
+  float ml[kKv4Waves][16 * NT][2];
+};
+template <int D>
+struct SharedWideLds {
+  uint16_t tile[4][64 * D];
+  unsigned long long nans[2][kKv4Waves];
+};
+
+// A workgroup's granules of a sequence: `more` workgroups of each + 1, then of each.
+__device__ __forceinline__ unsigned cut_begin(unsigned w, unsigned each, unsigned more) { return each * w + min(w, more); }
+__device__ __forceinline__ unsigned cut_owner(unsigned g, unsigned each, unsigned more) {
+  const unsigned wide = more * (each + 1);
+  return g < wide ? g / (each + 1) : more + (g - wide) / each;
+}
+
+// NP, NT: 16-row tiles of a unit over shared keys, and of one behind them.
+template <int D, int NP, int NT>
+__global__ __launch_bounds__(kKv4Threads, (kKv4PerCU<D, (NP > NT ? NP : NT)>)) void kv4_shared_kernel(SharedArgs sa) {
+  constexpr bool kAnyWide = NP == kKv4Wide || NT == kKv4Wide;
+  constexpr int kMostTile = (NP == kKv4Wide ? 1 : NP) > (NT == kKv4Wide ? 1 : NT) ? (NP == kKv4Wide ? 1 : NP) : (NT == kKv4Wide ? 1 : NT);
+  using TileLds = SharedTileLds<D, false, kMostTile>;
+  using WideLds = SharedWideLds<D>;
+  constexpr size_t kLds = kAnyWide && sizeof(WideLds) > sizeof(TileLds) ? sizeof(WideLds) : sizeof(TileLds);
+  __shared__ __attribute__((aligned(16))) char lds[kLds];
+  extern __shared__ int32_t group_lds[];
+  __shared__ unsigned wsum[2][kKv4Waves];
+  __shared__ struct {
+    int v;
+    unsigned off;
+  } where;
+  const Kv4Args& a = sa.k;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int G = a.H / a.Hkv, R = a.R, Gn = sa.Gn;
+  int32_t* gstart = group_lds;               // [Gn + 1] first requests of the groups
+  int32_t* gkeys = group_lds + Gn + 1;       // [Gn] their shared keys
+  unsigned* gbase = reinterpret_cast<unsigned*>(gkeys + Gn);       // [Gn] first granules of their units
+
+  // ---- the groups' shared keys, and where the units are in the two sequences of granules
+  bool ascends = true;
+  const int most_keys = a.W << a.page_log2;
+  for (int i = tid; i <= Gn; i += kKv4Threads) {
+    const int at = sa.groups[i];
+    gstart[i] = clamp_i(at, 0, R);
+    if (i < Gn) {
+      gkeys[i] = clamp_i(sa.prefix[i], 0, most_keys);
+      ascends = ascends && at <= sa.groups[i + 1];
+    }
+  }
+  __syncthreads();
+  auto rows_of = [&](int r, int& c0, int& n) {
+    c0 = a.cu ? clamp_i(a.cu[r], 0, a.T) : r;
+    n = a.cu ? clamp_i(a.cu[r + 1], c0, a.T) - c0 : 1;
+  };
+  // the last group that begins at or before request r; it is the request's if it ends behind r
+  auto group_of = [&](int r) {
+    int lo = 0, hi = Gn - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (gstart[mid] <= r) lo = mid;
+      else hi = mid - 1;
+    }
+    return lo;
+  };
+  auto in_group = [&](int g, int r) { return Gn > 0 && gstart[g] <= r && r < gstart[g + 1]; };
+  const int per = (R + kKv4Threads - 1) / kKv4Threads;
+  const int r0 = min(R, tid * per), r1 = min(R, r0 + per);
+  int g0 = Gn > 0 && r0 < R ? group_of(r0) : 0;
+  for (int r = r0, g = g0; r < r1; ++r) {
+    while (g + 1 < Gn && gstart[g + 1] <= r) ++g;
+    int c0, n;
+    rows_of(r, c0, n);
+    if (a.cu) ascends = ascends && a.cu[r] <= a.cu[r + 1];
+    if (n > 0 && in_group(g, r)) atomicMin(&gkeys[g], max(max(a.kv_len[r], 0) - n, 0));
+  }
+  const bool good = !__syncthreads_or(!ascends);
+  auto shared_keys = [&](int g) { return gkeys[g] & -kSharedBlock; };
+  auto tail_unit = [&](int r, int g) {
+    SharedUnit u;
+    rows_of(r, u.c0, u.n);
+    u.kv = max(a.kv_len[r], 0);
+    u.len = (int)min((long)u.kv, (long)most_keys);
+    u.first = in_group(g, r) ? shared_keys(g) : 0;
+    u.first = min(u.first, u.len & -kSharedBlock);         // (a request of no rows may have fewer)
+    u.pre = false;
+    u.size<NT>(a, G);
+    return u;
+  };
+  auto pre_unit = [&](int g) {
+    SharedUnit u;
+    int c1, n1;
+    const int first = gstart[g], last = gstart[g + 1];
+    u.c0 = u.n = 0;
+    if (last > first) {
+      rows_of(first, u.c0, u.n);
+      rows_of(last - 1, c1, n1);
+      u.n = c1 + n1 - u.c0;
+    }
+    u.len = shared_keys(g);
+    u.kv = u.len;
+    u.first = 0;
+    u.pre = true;
+    u.size<NP>(a, G);
+    return u;
+  };
+  const int gper = (Gn + kKv4Threads - 1) / kKv4Threads;
+  const int p0 = min(Gn, tid * gper), p1 = min(Gn, p0 + gper);
+  unsigned mine[2] = {0, 0};
+  for (int g = p0; g < p1; ++g) mine[0] += pre_unit(g).weight(a.Hkv);
+  for (int r = r0, g = g0; r < r1; ++r) {
+    while (g + 1 < Gn && gstart[g + 1] <= r) ++g;
+    mine[1] += tail_unit(r, g).weight(a.Hkv);
+  }
+  unsigned base[2], total[2];
+#pragma unroll
+  for (int kind = 0; kind < 2; ++kind) {
+    unsigned inc = mine[kind];
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const unsigned up = __shfl_up(inc, d);
+      if (lane >= d) inc += up;
+    }
+    if (lane == 63) wsum[kind][wave] = inc;
+    base[kind] = inc - mine[kind];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int kind = 0; kind < 2; ++kind) {
+    total[kind] = 0;
+#pragma unroll
+    for (int i = 0; i < kKv4Waves; ++i) {
+      if (i < wave) base[kind] += wsum[kind][i];
+      total[kind] += wsum[kind][i];
+    }
+    total[kind] = __builtin_amdgcn_readfirstlane(good ? total[kind] : 0u);
+  }
+  // ---- the workgroups: of nwg, np over shared keys
+  int np;
+  {
+    const float cp = (float)total[0] * (float)sa.cost, ct = (float)total[1] * 16.0f;
+    np = cp + ct > 0.0f ? (int)((float)a.nwg * cp / (cp + ct) + 0.5f) : 0;
+    if (total[0] && np < 1) np = 1;
+    if (total[1] && np > a.nwg - 1) np = a.nwg - 1;
+    np = min(np, (int)min(total[0], (unsigned)a.nwg));
+    np = __builtin_amdgcn_readfirstlane(np);
+  }
+  const unsigned nwgs[2] = {(unsigned)np, min((unsigned)(a.nwg - np), total[1])};
+  unsigned each[2], more[2];
+#pragma unroll
+  for (int kind = 0; kind < 2; ++kind) {
+    each[kind] = nwgs[kind] ? total[kind] / nwgs[kind] : 1u;
+    more[kind] = nwgs[kind] ? total[kind] - each[kind] * nwgs[kind] : 0u;
+  }
+  // the kinds alternate over the launch
+  const unsigned bid = blockIdx.x;
+  const unsigned pb = (unsigned)((unsigned long long)bid * np / (unsigned)a.nwg);
+  const unsigned pe = (unsigned)((unsigned long long)(bid + 1) * np / (unsigned)a.nwg);
+  const int kind = pe > pb ? 0 : 1;
+  const unsigned w = kind == 0 ? pb : bid - pb;
+  const unsigned ww = kind == 0 ? w : (unsigned)np + w;        // its place among all, and its slots'
+  unsigned gs = 0, ge = 0;
+  if (w < nwgs[kind]) {
+    gs = cut_begin(w, each[kind], more[kind]);
+    ge = gs + each[kind] + (w < more[kind] ? 1u : 0u);
+  }
+  if (bid == 0) {                              // what the second kernel goes by
+    if (tid == 0) *sa.cut = {good && total[1] ? 1 : 0, np, {each[0], each[1]}, {more[0], more[1]}};
+    unsigned at = base[0];
+    for (int g = p0; g < p1; ++g) {
+      gbase[g] = at;
+      at += pre_unit(g).weight(a.Hkv);
+    }
+    __syncthreads();
+    at = base[1];
+    for (int r = r0, g = g0; r < r1; ++r) {
+      while (g + 1 < Gn && gstart[g + 1] <= r) ++g;
+      const SharedUnit u = tail_unit(r, g);
+      SharedRow row{u.c0, u.n, u.first, at, (unsigned)u.grans, 0, 0, 0};
+      if (in_group(g, r)) {
+        const SharedUnit p = pre_unit(g);
+        row.pre_c0 = p.c0, row.pre_base = gbase[g], row.pre_grans = p.weight(a.Hkv) ? (unsigned)p.grans : 0u;
+      }
+      sa.rows[r] = row;
+      at += u.weight(a.Hkv);
+    }
+  }
+  if (gs >= ge) return;
+  if (base[kind] <= gs && gs < base[kind] + mine[kind]) {
+    unsigned off = gs - base[kind];
+    int v = kind == 0 ? p0 : r0;
+    if (kind == 0) {
+      for (unsigned wt; off >= (wt = pre_unit(v).weight(a.Hkv)); ++v) off -= wt;
+    } else {
+      int g = g0;
+      for (;; ++v) {
+        while (g + 1 < Gn && gstart[g + 1] <= v) ++g;
+        const unsigned wt = tail_unit(v, g).weight(a.Hkv);
+        if (off < wt) break;
+        off -= wt;
+      }
+    }
+    where = {v, off};
+  }
+  __syncthreads();
+  // ---- the workgroup's units
+  int v = __builtin_amdgcn_readfirstlane(where.v);
+  int g = Gn > 0 ? (kind == 0 ? v : group_of(v)) : 0;
+  auto uniform = [&](SharedUnit u) {
+    u.c0 = __builtin_amdgcn_readfirstlane(u.c0), u.n = __builtin_amdgcn_readfirstlane(u.n);
+    u.kv = __builtin_amdgcn_readfirstlane(u.kv), u.len = __builtin_amdgcn_readfirstlane(u.len);
+    u.tiles = __builtin_amdgcn_readfirstlane(u.tiles), u.grans = __builtin_amdgcn_readfirstlane(u.grans);
+    u.first = __builtin_amdgcn_readfirstlane(u.first);
+    u.pre = kind == 0;
+    return u;
+  };
+  auto unit_at = [&]() { return uniform(kind == 0 ? pre_unit(v) : tail_unit(v, g)); };
+  // the request whose table a unit reads: of a group the first that has rows
+  auto table_of = [&]() {
+    if (kind == 1) return v;
+    int r = gstart[v];
+    for (int c0, n; r + 1 < gstart[v + 1]; ++r) {
+      rows_of(r, c0, n);
+      if (n > 0) break;
+    }
+    return __builtin_amdgcn_readfirstlane(r);
+  };
+  SharedUnit u = unit_at();
+  int r = table_of();
+  int tile, h, gi;
+  {
+    const unsigned off = (unsigned)__builtin_amdgcn_readfirstlane((int)where.off);
+    const unsigned len = (unsigned)(kKv4Start + u.grans), heads = off / len;
+    gi = (int)(off - heads * len);
+    tile = (int)(heads / (unsigned)a.Hkv);
+    h = (int)(heads - (unsigned)tile * (unsigned)a.Hkv);
+  }
+  const size_t nrows = (size_t)a.T * a.H;
+  unsigned at = gs;
+  bool first_segment = true;
+  const Kv4Lane<D> places(a);
+  while (at < ge) {
+    const int v1 = (int)min((unsigned)(kKv4Start + u.grans), (unsigned)gi + (ge - at));
+    const int a0 = max(0, gi - kKv4Start), a1 = v1 - kKv4Start;
+    if (a1 > a0) {
+      const SharedFinish<D> fin{a0 == 0 && a1 == u.grans, a.part + (size_t)(2 * ww + (first_segment ? 0 : 1)) * sa.part_floats,
+                                sa.whole + kind * nrows * D, sa.whole_ml + kind * nrows * 2};
+      auto tiles = [&](auto nt) {
+        constexpr int N = decltype(nt)::value;
+        if constexpr (N == kKv4Wide) {
+          WideLds& wl = *reinterpret_cast<WideLds*>(lds);
+          kv4_wide<D>(a, u, r, tile, h, a0, a1, fin, Kv4WideLds{wl.tile[0], wl.tile[1], wl.tile[2], wl.tile[3], {wl.nans[0], wl.nans[1]}});
+          __syncthreads();
+        } else {
+          SharedTileLds<D, false, N>& tl = *reinterpret_cast<SharedTileLds<D, false, N>*>(lds);
+          kv4_tile<D, N>(a, u, r, tile, h, a0, a1, fin, places, tl.vbuf, tl.ml);
+        }
+      };
+      if (NP == NT || kind == 0) tiles(std::integral_constant<int, NP>{});
+      else tiles(std::integral_constant<int, NT>{});
+      first_segment = false;
+    }
+    at += (unsigned)(v1 - gi);
+    gi = 0;
+    if (at < ge && ++h == a.Hkv) {
+      h = 0;
+      if (++tile == u.tiles) {
+        tile = 0;
+        do {
+          ++v;
+          if (kind == 1) while (g + 1 < Gn && gstart[g + 1] <= v) ++g;
+          u = unit_at();
+        } while (u.weight(a.Hkv) == 0);       // (granules are left, so a unit with some is)
+        r = table_of();
+      }
+    }
+  }
+}
+
+constexpr int kSharedJoinRows = 4;         // rows of a workgroup, one to a wave
+
+// A row's parts: over shared keys, then behind them, each in granule order; 16 lanes across the dimensions, and every
+// fourth part to each quarter of the wave.
+template <int D, int NP, int NT>
+__global__ __launch_bounds__(64 * kSharedJoinRows) void kv4_shared_join_kernel(SharedArgs sa) {
+  constexpr int CH = D / 16;
+  const Kv4Args& a = sa.k;
+  const int lane = threadIdx.x & 63, ch = lane & 15, quarter = lane >> 4;
+  const long row = (long)blockIdx.x * kSharedJoinRows + (threadIdx.x >> 6);       // (token, head)
+  if (row >= (long)a.T * a.H) return;
+  const SharedCut cut = *sa.cut;
+  if (!cut.ok) return;
+  const int G = a.H / a.Hkv, t = (int)(row / a.H), hq = (int)(row - (long)t * a.H), h = hq / G;
+  int r = t;
+  if (a.cu) {                  // requests that end at or before the row: two looks of 64 entries each
+    const int step = (a.R + 63) / 64;
+    const int mark = min((lane + 1) * step, a.R);
+    const int blocks = __builtin_popcountll(__ballot(lane * step < a.R && a.cu[mark] <= t));
+    r = blocks * step;
+    const int i = r + lane + 1;
+    r += __builtin_popcountll(__ballot(lane < step && i <= a.R && a.cu[i] <= t));
+    if (r >= a.R) return;
+  }
+  const SharedRow of = sa.rows[r];
+  if (t < of.c0 || t >= of.c0 + of.n) return;
+  float top = -__builtin_inff(), sum = 0.0f, out[CH] = {};
+  auto add = [&](float m, float l, const float* x) {
+    const float to = fmaxf(top, m);
+    const float was = part_weight(top, to, a.sl2), wt = part_weight(m, to, a.sl2);
+    sum = (top == -__builtin_inff() ? sum : was * sum) + (m == -__builtin_inff() ? l : wt * l);    // (NaN of an empty part stays)
+#pragma unroll
+    for (int c = 0; c < CH / 4; ++c) {
+      const f32x4 y = *reinterpret_cast<const f32x4*>(x + ch * CH + 4 * c);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) out[4 * c + e] = out[4 * c + e] * was + wt * y[e];
+    }
+    top = to;
+  };
+  auto parts = [&](int kind, int n16, unsigned base, unsigned grans, int c0) {
+    if (grans == 0) return;
+    const int rho = (t - c0) * G + (hq - h * G), tile = rho / n16, lr = rho - tile * n16;
+    const unsigned unit = base + ((unsigned)tile * (unsigned)a.Hkv + (unsigned)h) * (kKv4Start + grans);
+    const unsigned w0 = cut_owner(unit + kKv4Start, cut.each[kind], cut.more[kind]);
+    const unsigned w1 = cut_owner(unit + kKv4Start + grans - 1, cut.each[kind], cut.more[kind]);
+    if (w0 == w1) {
+      const size_t at = (size_t)kind * a.T * a.H + row;
+      if (quarter == kind) {
+        const float2 ml = *reinterpret_cast<const float2*>(sa.whole_ml + 2 * at);
+        add(ml.x, ml.y, sa.whole + at * D);
+      }
+      return;
+    }
+    // in its first workgroup the unit is the second segment where one before it has granules there
+    const unsigned second = cut_begin(w0, cut.each[kind], cut.more[kind]) < unit ? 1 : 0;
+    const unsigned np = kind ? (unsigned)cut.np : 0u;
+    for (unsigned w = w0 + quarter; w <= w1; w += 4) {
+      const float* sl = a.part + (size_t)(2 * (np + w) + (w == w0 ? second : 0u)) * sa.part_floats;
+      const float2 ml = *reinterpret_cast<const float2*>(sl + 2 * lr);
+      add(ml.x, ml.y, sl + 2 * n16 + lr * D);
+    }
+  };
+  parts(0, 16 * NP, of.pre_base, of.pre_grans, of.pre_c0);
+  parts(1, 16 * NT, of.base, of.grans, of.c0);
+  const float all = max_over_groups(top);
+  const float wt = part_weight(top, all, a.sl2);
+  sum = sum_over_groups(top == -__builtin_inff() ? sum : wt * sum);
+#pragma unroll
+  for (int e = 0; e < CH; ++e) out[e] = sum_over_groups(wt * out[e]);
+  if (quarter != 0) return;
+  const float inv = row_factor(sum, max(a.kv_len[r], 0) - of.n + (t - of.c0));
+#pragma unroll
+  for (int e = 0; e < CH; ++e) out[e] *= inv;
+  store_row<CH>(a.o + (size_t)row * D + ch * CH, out);
+}
+
+}  // namespace
+}  // namespace qg

@@ -5,6 +5,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "kv4_levels.hpp"
 #include "qgemm_kernels.hpp"
 
 namespace qg {
@@ -346,17 +347,6 @@ __global__ __launch_bounds__(kCacheThreads) void kv4_store_kernel(CacheArgs a) {
   uint8_t* rec = a.cache + ((size_t)page * a.Hkv + it.h) * a.lay.record();
   *reinterpret_cast<uint32_t*>(rec + a.lay.codes(it.which, off, it.unit)) = codes;
   if ((it.unit & 3) == 0) rec[a.lay.scale(it.which, off, it.unit >> 2)] = (uint8_t)e;
-}
-
-// Two levels of a packed byte (0..3 of w) times 2^(e-127); exact in bf16, NaN for e = 255.
-template <int B>
-__device__ __forceinline__ uint32_t fp4_pair(uint32_t w, float unit) {
-  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, unit, B));
-}
-
-// Eight levels of a packed dword times 2^(e-127), as bf16.
-__device__ __forceinline__ u32x4 fp4_unit(uint32_t w, float unit) {
-  return u32x4{fp4_pair<0>(w, unit), fp4_pair<1>(w, unit), fp4_pair<2>(w, unit), fp4_pair<3>(w, unit)};
 }
 
 __global__ __launch_bounds__(kCacheThreads) void kv4_load_kernel(CacheArgs a) {
