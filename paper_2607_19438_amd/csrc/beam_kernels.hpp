@@ -14,27 +14,30 @@ namespace {
 // ---------------------------------------------------------------------------
 //
 // A candidate (beam b, token v) is worth score[b] + x[b][v] - lse[b], lse = log sum_v exp x[b][v]. Within a beam the
-// order is that of the logits, so the first kernel needs no lse: a workgroup takes a piece of a row in one pass over
-// it, carries maximum and sum as an online softmax does, and keeps the piece's K largest logits. The second kernel
-// has the B * pieces * K of a request that are left and computes their values in 64 bits: what beams differ by
-// decides between candidates, and at a score of -100 steps of 32 bits are 2^-17.
+// order is that of the logits, so the first kernel needs no lse: it takes a piece of a row in one pass over it,
+// carries maximum and sum as an online softmax does, and keeps the piece's K largest logits. The second kernel has the
+// B * pieces * K of a request that are left and computes their values in 64 bits: what beams differ by decides
+// between candidates, and at a score of -100 steps of 32 bits are 2^-17.
 // Bound by the logits' bytes; with few rows by the chain load - bound - selection - second launch.
 
 constexpr int kBeamThreads = 256;
+constexpr int kBeamWaves = kBeamThreads / 64;
 constexpr int kBeamMaxB = 64;          // beams of a request
 constexpr int kBeamMaxK = 128;         // candidates that are taken
-constexpr int kBeamElems = 16;         // logits of a thread and step
-constexpr int kBeamStep = kBeamThreads * kBeamElems;
-constexpr int kBeamList = 16 * kBeamMaxK + kBeamMaxK;      // logits that a workgroup holds before it selects
-constexpr int kBeamMost = 8192;        // of a request that are left for the second kernel, at most
-static_assert(kBeamList % kBeamThreads == 128, "see beam_keep");
-constexpr int kBeamKept = kBeamMaxK * ((kBeamList + kBeamThreads - 1) / kBeamThreads);
+constexpr int kBeamElems = 16;         // logits of a lane and step
+constexpr int kBeamStep = 64 * kBeamElems;
+constexpr int kBeamPiece = kBeamWaves * kBeamStep;         // pieces of a row are multiples of it
+constexpr int kBeamList = 640;         // logits that a wave holds before it selects
+constexpr int kBeamMost = 1024;        // of a request that are left for the second kernel, where a row has several pieces
+static_assert(kBeamList % 64 == 0 && kBeamList >= kBeamMaxK + 64, "a selection makes room for a round");
 
-// A logit and its token as one number, larger logits first, then lower tokens. 0 stands for none.
-__device__ __forceinline__ uint64_t beam_key(float x, uint32_t v) {
+// A logit as an integer of the same order, above 0 but for NaN.
+__device__ __forceinline__ uint32_t beam_bits(float x) {
   const uint32_t u = __builtin_bit_cast(uint32_t, x + 0.0f);         // -0 as 0
-  return ((uint64_t)(u ^ ((u >> 31) ? 0xffffffffu : 0x80000000u)) << 32) | (0xffffffffu - v);
+  return u ^ ((u >> 31) ? 0xffffffffu : 0x80000000u);
 }
+// A logit and its token as one number, larger logits first, then lower tokens. 0 stands for none.
+__device__ __forceinline__ uint64_t beam_key(float x, uint32_t v) { return (uint64_t)beam_bits(x) << 32 | (0xffffffffu - v); }
 __device__ __forceinline__ float beam_logit(uint64_t key) {
   const uint32_t u = (uint32_t)(key >> 32);
   return __builtin_bit_cast(float, u ^ ((u >> 31) ? 0x80000000u : 0xffffffffu));
@@ -61,10 +64,12 @@ struct BeamArgs {
   int32_t* out_beams;
   int32_t* out_tokens;
   BeamStat* stat;           // [R * B][pieces]
-  uint64_t* cand;           // [R * B][pieces][K]
+  uint64_t* cand;           // [R * B][pieces][K] in order, 0 for none
   long stride;
-  int R, B, V, K, pieces, piece;      // piece: logits of one, a multiple of kBeamStep
+  int R, B, V, K, pieces, piece;      // piece: logits of one, a multiple of kBeamPiece
   int end;
+  int pieces_log2;          // of the power of two from `pieces` on, at most 6
+  uint32_t per_inv;         // 2^32 / (pieces K), rounded up; 0 for pieces K = 1
 };
 
 // Whether a beam's logits are candidates: not those of an ended one, nor of one whose score leaves nothing.
@@ -72,60 +77,66 @@ __device__ __forceinline__ bool beam_reads(const BeamArgs& a, int row) {
   return a.scores[row] > -__builtin_inff() && !(a.finished && a.finished[row]);
 }
 
-struct BeamLds {
-  uint64_t list[kBeamList];
-  uint64_t kept[kBeamKept];
-  uint64_t each[kBeamThreads];
-  uint64_t bound;
-  int count, first_out, kept_n;
-};
-
-// How many threads' keys are larger than this one's.
-__device__ __forceinline__ int beam_place(BeamLds& s, uint64_t mine) {
-  s.each[threadIdx.x] = mine;
-  __syncthreads();
-  int n = 0;
-#pragma unroll 16
-  for (int i = 0; i < kBeamThreads; ++i) n += s.each[i] > mine;
-  __syncthreads();
-  return n;
+__device__ __forceinline__ int lanes_below(unsigned long long mask) {
+  return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
 }
 
-// The K-th largest of the threads' keys, 1 if there are fewer: a lower bound of the K-th largest of all that they
-// hold, which K threads at most reach. (Keys are distinct, but for 0.)
-__device__ __forceinline__ uint64_t beam_bound(BeamLds& s, uint64_t mine, int K) {
-  if (threadIdx.x == 0) s.bound = 1;
-  const int place = beam_place(s, mine);      // (its barriers are behind the write above)
-  if (place == K - 1 && mine) s.bound = mine;
-  __syncthreads();
-  const uint64_t bound = s.bound;
-  __syncthreads();
+// The largest number that K of the lanes' P numbers each reach, its bits from LOW on: a lower bound of the K-th largest
+// of all that the lanes hold (0 if fewer than K hold any). A count of lanes for each bit; comparing every lane's with
+// every other's takes eight times as long.
+template <int LOW, int P>
+__device__ __forceinline__ uint32_t wave_bound(const uint32_t (&mine)[P], int K) {
+  uint32_t bound = 0;
+#pragma unroll
+  for (int bit = 31; bit >= LOW; --bit) {
+    const uint32_t more = bound | 1u << bit;
+    int n = 0;
+#pragma unroll
+    for (int p = 0; p < P; ++p) n += __builtin_popcountll(__ballot(mine[p] >= more));
+    bound = n >= K ? more : bound;
+  }
   return bound;
 }
 
-// The K largest of list[0 .. n) to its front, in order; how many there are. list[.. K) behind them is 0.
-__device__ __forceinline__ int beam_keep(BeamLds& s, int n, int K) {
-  const int tid = threadIdx.x;
-  uint64_t top = 0;
-  for (int i = tid; i < n; i += kBeamThreads) top = max(top, s.list[i]);
-  if (tid == 0) s.kept_n = 0;
-  const uint64_t from = beam_bound(s, top, K);
-  for (int i = tid; i < n; i += kBeamThreads) {
-    const uint64_t k = s.list[i];
-    if (k >= from) s.kept[atomicAdd(&s.kept_n, 1)] = k;       // a set: their order does not matter
+// A wave's list[0 .. n) without what is below a bound that K of it reach: the bound, n as it is then. A wave's LDS
+// accesses run in order.
+__device__ __forceinline__ uint32_t wave_tighten(uint64_t* list, int& n, int K, int lane) {
+  asm volatile("" ::: "memory");
+  uint32_t top[2] = {0, 0};
+  for (int i = lane, h = 0; i < n; i += 64, h ^= 1) {
+    const uint32_t k = (uint32_t)(list[i] >> 32);
+    top[0] = max(top[0], h ? 0u : k);
+    top[1] = max(top[1], h ? k : 0u);
   }
-  __syncthreads();
-  const int m = s.kept_n;
-  for (int i = tid; i < K; i += kBeamThreads) s.list[i] = 0;
-  __syncthreads();
-  for (int i = tid; i < m; i += kBeamThreads) {
-    const uint64_t k = s.kept[i];
-    int p = 0;
-    for (int j = 0; j < m; ++j) p += s.kept[j] > k;
-    if (p < K) s.list[p] = k;
+  const uint32_t bound = wave_bound<12>(top, K);
+  int m = 0;
+  for (int i = 0; i < n; i += 64) {
+    const uint64_t k = i + lane < n ? list[i + lane] : 0;
+    const bool in = k && (uint32_t)(k >> 32) >= bound;
+    const unsigned long long all = __ballot(in);
+    if (in) list[m + lanes_below(all)] = k;
+    m += __builtin_popcountll(all);
   }
-  __syncthreads();
-  return min(m, K);
+  n = m;
+  asm volatile("" ::: "memory");
+  return bound;
+}
+
+// The K largest of a wave's list[0 .. n), in order, to its front, by way of sorted[K]; how many there are.
+__device__ __forceinline__ int wave_keep(uint64_t* list, uint64_t* sorted, int n, int K, int lane) {
+  if (n > K && n > 64) wave_tighten(list, n, K, lane);
+  asm volatile("" ::: "memory");
+  for (int c = 0; c < n; c += 64) {
+    const uint64_t mine = c + lane < n ? list[c + lane] : 0;
+    int place = 0;
+#pragma unroll 4
+    for (int j = 0; j < n; ++j) place += list[j] > mine;
+    if (mine && place < K) sorted[place] = mine;
+  }
+  asm volatile("" ::: "memory");
+  for (int i = lane; i < min(n, K); i += 64) list[i] = sorted[i];
+  asm volatile("" ::: "memory");
+  return min(n, K);
 }
 
 typedef uint32_t u32x4_by4 __attribute__((ext_vector_type(4), aligned(4)));      // rows need no more than their elements' alignment
@@ -136,54 +147,71 @@ struct BeamLoad {
   static constexpr int kWide = 16 / sizeof(T);      // logits of a load
   static constexpr int kLoads = kBeamElems / kWide;
   using vec = std::conditional_t<sizeof(T) == 4, u32x4_by4, u32x4_by2>;
+  // the place in a step of a lane's logit i
+  static __device__ __forceinline__ int place(int i, int lane) { return (i / kWide * 64 + lane) * kWide + i % kWide; }
   static __device__ __forceinline__ float one(const T* p) {
     if constexpr (sizeof(T) == 4) return *p;
     else return __builtin_bit_cast(float, (uint32_t)*p << 16);
   }
-  static __device__ __forceinline__ void spread(const u32x4& w, float* x) {
+  // A lane's logits of the step at v0, -inf from `end` on.
+  static __device__ __forceinline__ void step(const T* row, int v0, int end, int lane, float (&x)[kBeamElems]) {
+    if (v0 + kBeamStep <= end) {
+      u32x4 w[kLoads];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const uint32_t u = w[e];
-      if constexpr (sizeof(T) == 4) {
-        x[e] = __builtin_bit_cast(float, u);
-      } else {
-        x[2 * e] = __builtin_bit_cast(float, u << 16);
-        x[2 * e + 1] = __builtin_bit_cast(float, u & 0xffff0000u);
+      for (int j = 0; j < kLoads; ++j)
+        w[j] = __builtin_bit_cast(u32x4, *reinterpret_cast<const vec*>(row + v0 + place(j * kWide, lane)));
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t u = w[j][e];
+          if constexpr (sizeof(T) == 4) {
+            x[4 * j + e] = __builtin_bit_cast(float, u);
+          } else {
+            x[8 * j + 2 * e] = __builtin_bit_cast(float, u << 16);
+            x[8 * j + 2 * e + 1] = __builtin_bit_cast(float, u & 0xffff0000u);
+          }
+        }
+    } else {
+#pragma unroll
+      for (int i = 0; i < kBeamElems; ++i) {
+        const int v = v0 + place(i, lane);
+        x[i] = v < end ? one(row + v) : -__builtin_inff();
       }
     }
   }
 };
 
+// A workgroup takes a piece of a row, each of its waves every fourth step, with a list of its own: no barrier but at
+// the end. A wave's first step gives a bound that K logits reach; from then on a logit is kept if it is above the bound,
+// which the list raises whenever it has grown by K or 64. One that equals it is not kept: its token is behind those of
+// the list. What a step costs beside its 16 exponentials is a round for each lane's logits above the bound: with the first
+// step's bound to the end, K of 1024 logits pass in every step (48 x 8 rows of 128000, K = 16: 52.8 us, bf16 49.4).
 template <typename T>
-__global__ __launch_bounds__(kBeamThreads) void beam_rows_kernel(BeamArgs a) {
+__global__ __launch_bounds__(kBeamThreads, 4) void beam_rows_kernel(BeamArgs a) {
   using L = BeamLoad<T>;
-  __shared__ BeamLds s;
-  __shared__ double wave_sum[kBeamThreads / 64];
-  __shared__ float wave_top[kBeamThreads / 64];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  __shared__ uint64_t lists[kBeamWaves][kBeamList], sorted[kBeamWaves][kBeamMaxK];
+  __shared__ double wave_sum[kBeamWaves];
+  __shared__ float wave_top[kBeamWaves];
+  __shared__ int wave_count[kBeamWaves];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int row = blockIdx.x / a.pieces, piece = blockIdx.x - row * a.pieces;
-  if (!beam_reads(a, row)) return;                  // the second kernel asks the same
   const T* x0 = static_cast<const T*>(a.x) + (size_t)row * a.stride;
-  const int v_begin = piece * a.piece, v_end = min(a.V, v_begin + a.piece);
+  const int v_begin = piece * a.piece + wave * kBeamStep, v_end = min(a.V, (piece + 1) * a.piece);
+  const int K = a.K;
   const float ninf = -__builtin_inff(), log2e = 1.4426950408889634f;
+  uint64_t* list = lists[wave];
   float top = ninf;
   double sum = 0.0;
-  uint64_t from = 0;             // candidates are above it
-  if (tid == 0) s.count = 0, s.first_out = kBeamList;
-  __syncthreads();
-  for (int v0 = v_begin; v0 < v_end; v0 += kBeamStep) {
-    float x[kBeamElems];
-    auto token = [&](int i) { return v0 + ((i / L::kWide) * kBeamThreads + tid) * L::kWide + i % L::kWide; };
-#pragma unroll
-    for (int j = 0; j < L::kLoads; ++j) {
-      const int v = token(j * L::kWide);
-      if (v + L::kWide <= v_end) {
-        L::spread(__builtin_bit_cast(u32x4, *reinterpret_cast<const typename L::vec*>(x0 + v)), x + j * L::kWide);
-      } else {
-#pragma unroll
-        for (int e = 0; e < L::kWide; ++e) x[j * L::kWide + e] = v + e < v_end ? L::one(x0 + v + e) : ninf;
-      }
-    }
+  float from = ninf;             // logits that are kept are above it
+  int count = 0, limit = 2 * max(K, 32);
+  float x[kBeamElems];
+  if (v_begin < v_end) L::step(x0, v_begin, v_end, lane, x);
+  if (!beam_reads(a, row)) return;                  // (asked while the loads are on their way; the second kernel asks the same)
+  for (int v0 = v_begin; v0 < v_end; v0 += kBeamPiece) {
+    float next[kBeamElems];
+    if (v0 + kBeamPiece < v_end) L::step(x0, v0 + kBeamPiece, v_end, lane, next);
     float most = x[0];
 #pragma unroll
     for (int i = 1; i < kBeamElems; ++i) most = fmaxf(most, x[i]);
@@ -196,157 +224,205 @@ __global__ __launch_bounds__(kBeamThreads) void beam_rows_kernel(BeamArgs a) {
 #pragma unroll
     for (int i = 0; i < kBeamElems; ++i) part += __builtin_amdgcn_exp2f((x[i] - ref) * log2e);
     sum += (double)part;
-    // what is above the bound, into the list
+    auto token = [&](int i) { return (uint32_t)(v0 + L::place(i, lane)); };
     uint32_t pending = 0;
-    uint64_t mine = 0;
-#pragma unroll
-    for (int i = 0; i < kBeamElems; ++i) {
-      const uint64_t k = x[i] > ninf ? beam_key(x[i], (uint32_t)token(i)) : 0;
-      if (k > from) pending |= 1u << i;
-      mine = max(mine, k);
-    }
     if (v0 == v_begin) {
-      from = beam_bound(s, mine, a.K) - 1;
+      float half[2] = {x[0], x[1]};
 #pragma unroll
-      for (int i = 0; i < kBeamElems; ++i)
-        if (!(x[i] > ninf) || beam_key(x[i], (uint32_t)token(i)) <= from) pending &= ~(1u << i);
+      for (int i = 2; i < kBeamElems; ++i) half[i & 1] = fmaxf(half[i & 1], x[i]);
+      const uint32_t two[2] = {half[0] > ninf ? beam_bits(half[0]) : 0u, half[1] > ninf ? beam_bits(half[1]) : 0u};
+      const uint32_t one[1] = {max(two[0], two[1])};
+      const uint32_t bound = K <= 32 ? wave_bound<12>(one, K) : wave_bound<12>(two, K);
+      if (bound) from = beam_logit((uint64_t)bound << 32);
+#pragma unroll
+      for (int i = 0; i < kBeamElems; ++i) pending |= x[i] > ninf && x[i] >= from ? 1u << i : 0u;
+    } else if (__any(most > from)) {
+#pragma unroll
+      for (int i = 0; i < kBeamElems; ++i) pending |= x[i] > from ? 1u << i : 0u;
     }
-    while (__syncthreads_or(pending != 0)) {
-      if (pending) {
-        const int n = __builtin_popcount(pending);
-        int at = atomicAdd(&s.count, n);
-        if (at + n <= kBeamList) {
+    // one logit of each lane to a round
+    for (unsigned long long in; (in = __ballot(pending != 0)) != 0;) {
+      if (count + 64 > kBeamList) {
+        count = wave_keep(list, sorted[wave], count, K, lane);
+        const uint64_t last = list[K - 1];
+        const uint32_t behind = (uint32_t)beam_token(last);
+        from = beam_logit(last);
+        uint32_t above = 0;
 #pragma unroll
-          for (int i = 0; i < kBeamElems; ++i)
-            if (pending >> i & 1) s.list[at++] = beam_key(x[i], (uint32_t)token(i));
-          pending = 0;
-        } else {
-          atomicMin(&s.first_out, at);        // from here on the list holds nothing
-        }
+        for (int i = 0; i < kBeamElems; ++i) above |= x[i] > from || (x[i] == from && token(i) < behind) ? 1u << i : 0u;
+        pending &= above;
+        continue;
       }
-      __syncthreads();
-      if (s.count > kBeamList) {              // full: keep the best, and try again with what is still above them
-        const int n = beam_keep(s, min(s.first_out, kBeamList), a.K);
-        if (n == a.K) from = s.list[a.K - 1];
-        __syncthreads();
-        if (tid == 0) s.count = n, s.first_out = kBeamList;
+      const int i = pending ? __builtin_ctz(pending) : 0;
+      // (values, as a choice between two places would put the array into memory)
+      auto pick = [](bool second, float p, float q) { return second ? q : p; };
+      float v[kBeamElems / 2];
 #pragma unroll
-        for (int i = 0; i < kBeamElems; ++i)
-          if (beam_key(x[i], (uint32_t)token(i)) <= from) pending &= ~(1u << i);
-      }
+      for (int j = 0; j < 8; ++j) v[j] = pick(i & 8, x[j], x[8 + j]);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] = pick(i & 4, v[j], v[4 + j]);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) v[j] = pick(i & 2, v[j], v[2 + j]);
+      const float mine = pick(i & 1, v[0], v[1]);
+      if (pending) list[count + lanes_below(in)] = beam_key(mine, token(i));
+      count += __builtin_popcountll(in);
+      pending &= pending - 1;
     }
+    if (count >= limit) {
+      from = beam_logit((uint64_t)wave_tighten(list, count, K, lane) << 32);       // (more than K: there is a bound)
+      limit = count + max(K, 64);
+    }
+#pragma unroll
+    for (int i = 0; i < kBeamElems; ++i) x[i] = next[i];
   }
-  beam_keep(s, s.count, a.K);
-  uint64_t* out = a.cand + (size_t)blockIdx.x * a.K;
-  for (int i = tid; i < a.K; i += kBeamThreads) out[i] = s.list[i];
-  // the threads' maxima and sums as one
+  count = wave_keep(list, sorted[wave], count, K, lane);
+  for (int i = count + lane; i < K; i += 64) list[i] = 0;
+  // the lanes' and the waves' maxima and sums as one
   float all = top;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) all = fmaxf(all, __shfl_xor(all, d));
-  if (lane == 0) wave_top[wave] = all;
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < kBeamThreads / 64; ++i) all = fmaxf(all, wave_top[i]);
   sum = top == ninf ? sum : sum * exp((double)top - (double)all);
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
-  if (lane == 0) wave_sum[wave] = sum;
+  if (lane == 0) wave_top[wave] = all, wave_sum[wave] = sum, wave_count[wave] = count;
   __syncthreads();
-  if (tid == 0) {
-    double t = 0.0;
+  if (tid < kBeamWaves) {
+    const float mine = wave_top[tid];
 #pragma unroll
-    for (int i = 0; i < kBeamThreads / 64; ++i) t += wave_sum[i];
-    a.stat[blockIdx.x] = {t, all, 0.0f};
+    for (int i = 0; i < kBeamWaves; ++i) all = fmaxf(all, wave_top[i]);
+    double t = mine == ninf ? wave_sum[tid] : wave_sum[tid] * exp((double)mine - (double)all);
+#pragma unroll
+    for (int d = 1; d < kBeamWaves; d <<= 1) t += __shfl_xor(t, d);
+    if (tid == 0) a.stat[blockIdx.x] = {t, all, 0.0f};
   }
+  // and their lists: a logit's place is its own in its list, and how many of each other list are above it
+  uint64_t* out = a.cand + (size_t)blockIdx.x * K;
+  for (int e = tid; e < kBeamWaves * K; e += kBeamThreads) {
+    const int w = e / K, i = e - w * K;
+    const uint64_t k = lists[w][i];
+    if (!k) continue;
+    int place = i, at[kBeamWaves - 1] = {};
+    for (int half = 1 << (31 - __builtin_clz(K)); half; half >>= 1)       // at: entries that are above k, of the first so many
+#pragma unroll
+      for (int o = 1; o < kBeamWaves; ++o) {
+        const int to = at[o - 1] + half;
+        if (to <= K && lists[(w + o) % kBeamWaves][to - 1] > k) at[o - 1] = to;
+      }
+#pragma unroll
+    for (int o = 1; o < kBeamWaves; ++o) place += at[o - 1];
+    if (place < K) out[place] = k;
+  }
+  int total = 0;
+#pragma unroll
+  for (int w = 0; w < kBeamWaves; ++w) total += wave_count[w];
+  for (int i = total + tid; i < K; i += kBeamThreads) out[i] = 0;
 }
 
 // One workgroup to a request. Candidate e = (beam, piece, place in the piece's list); equal values go to the lower e.
+// MOST: candidates at most.
+template <int MOST>
 __global__ __launch_bounds__(kBeamThreads) void beam_join_kernel(BeamArgs a) {
-  extern __shared__ uint64_t kept_value[];
-  __shared__ double lse[kBeamMaxB];
+  __shared__ uint64_t kept_value[MOST];   // (all of them where all are worth the same)
+  __shared__ uint16_t kept_at[MOST];
+  constexpr int kHeld = 4;                // of a thread's candidates, in registers
+  __shared__ double off[kBeamMaxB];       // score - lse
   __shared__ float score[kBeamMaxB];
-  __shared__ uint64_t each[kBeamThreads];
-  __shared__ int each_at[kBeamThreads];
-  __shared__ uint64_t bound;
-  __shared__ int bound_at, kept_n;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = blockIdx.x;
-  const int per = a.pieces * a.K, n = a.B * per;
-  int* kept_at = reinterpret_cast<int*>(kept_value + min(n, a.K * ((n + kBeamThreads - 1) / kBeamThreads)));
-  const float ninf = -__builtin_inff();
-  for (int b = wave; b < a.B; b += kBeamThreads / 64) {
-    const int row = r * a.B + b;
-    if (lane == 0) score[b] = a.scores[row];
-    double sum = 0.0;
-    float top = ninf;
-    if (beam_reads(a, row)) {
-      for (int p = lane; p < a.pieces; p += 64) top = fmaxf(top, a.stat[(size_t)row * a.pieces + p].top);
-#pragma unroll
-      for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
-      for (int p = lane; p < a.pieces; p += 64) {
-        const BeamStat st = a.stat[(size_t)row * a.pieces + p];
-        sum += st.top == ninf ? st.sum : st.sum * exp((double)st.top - (double)top);
-      }
-#pragma unroll
-      for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
-    }
-    if (lane == 0) lse[b] = (double)top + log(sum);       // NaN where a logit is NaN or +inf: its beam has no candidates
-  }
-  if (tid == 0) bound = 1, bound_at = n, kept_n = 0;
-  __syncthreads();
+  __shared__ int reads[kBeamMaxB];
+  __shared__ uint32_t each[kBeamThreads];
+  __shared__ int kept_n;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = blockIdx.x, K = a.K;
+  const int per = a.pieces * K, n = a.B * per;
   const uint64_t* cand = a.cand + (size_t)r * n;
+  const float ninf = -__builtin_inff();
+  uint64_t held[kHeld];
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) held[i] = tid + i * kBeamThreads < n ? cand[tid + i * kBeamThreads] : 0;
+  if (tid == 0) kept_n = 0;
+  {
+    // a row's pieces in neighbouring lanes, as many rows to a wave as fit
+    const int lg = a.pieces_log2, sub = lane & ((1 << lg) - 1);
+    for (int b = (wave * 64 + lane) >> lg; (b & -(64 >> lg)) < a.B; b += kBeamThreads >> lg) {
+      const bool in = b < a.B;
+      const int row = r * a.B + (in ? b : 0);
+      const BeamStat first = a.stat[(size_t)row * a.pieces + min(sub, a.pieces - 1)];       // (not written for a beam that is not read)
+      const bool take = in && beam_reads(a, row);
+      const bool some = take && sub < a.pieces;
+      double sum = some ? first.sum : 0.0;
+      float top = some ? first.top : ninf;
+      for (int p = sub + 64; take && p < a.pieces; p += 64) {         // (then a row takes a wave)
+        const BeamStat st = a.stat[(size_t)row * a.pieces + p];
+        const float to = fmaxf(top, st.top);
+        sum = (top == ninf ? sum : sum * exp((double)top - (double)to)) + (st.top == ninf ? st.sum : st.sum * exp((double)st.top - (double)to));
+        top = to;
+      }
+      float all = top;
+      for (int d = 1; d < 1 << lg; d <<= 1) all = fmaxf(all, __shfl_xor(all, d));
+      sum = top == ninf ? sum : sum * exp((double)top - (double)all);
+      for (int d = 1; d < 1 << lg; d <<= 1) sum += __shfl_xor(sum, d);
+      if (in && sub == 0) {
+        const float s = a.scores[row];
+        score[b] = s;
+        reads[b] = take;
+        off[b] = (double)all + log(sum);      // NaN where a logit is NaN or +inf: its beam has no candidates
+      }
+    }
+  }
+  __syncthreads();
   // a candidate's value as an ordered integer, 0 for none
-  auto value = [&](int e) -> uint64_t {
-    const int b = e / per;
-    if (!beam_reads(a, r * a.B + b)) {
+  auto beam_of = [&](int e) { return a.per_inv ? (int)__umulhi((uint32_t)e, a.per_inv) : e; };      // e / per, of e < 2^14
+  auto value = [&](int e, uint64_t k) -> uint64_t {
+    const int b = beam_of(e);
+    if (!reads[b]) {
       const bool one = e == b * per && score[b] > ninf;   // an ended beam's only candidate
       return one ? beam_order((double)score[b]) : 0;
     }
-    const uint64_t k = cand[e];
     if (!k) return 0;
-    const double v = (double)score[b] + ((double)beam_logit(k) - lse[b]);
+    const double v = (double)score[b] + ((double)beam_logit(k) - off[b]);
     return v > (double)ninf ? beam_order(v) : 0;
   };
-  uint64_t top = 0;
-  int top_at = n;
-  for (int e = tid; e < n; e += kBeamThreads) {
-    const uint64_t v = value(e);
-    if (v > top) top = v, top_at = e;
-  }
-  each[tid] = top;
-  each_at[tid] = top_at;
-  __syncthreads();
-  int place = 0;
-#pragma unroll 8
-  for (int i = 0; i < kBeamThreads; ++i) place += each[i] > top || (each[i] == top && each_at[i] < top_at);
-  if (place == a.K - 1 && top) bound = top, bound_at = top_at;
-  __syncthreads();
-  const uint64_t from = bound;
-  const int from_at = bound_at;
-  for (int e = tid; e < n; e += kBeamThreads) {
-    const uint64_t v = value(e);
-    if (v > from || (v == from && e <= from_at)) {
-      const int i = atomicAdd(&kept_n, 1);
-      kept_value[i] = v;
-      kept_at[i] = e;
+  auto for_each = [&](auto&& f) {
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) {
+      const int e = tid + i * kBeamThreads;
+      if (e < n) f(e, value(e, held[i]));
     }
+    for (int e = tid + kHeld * kBeamThreads; e < n; e += kBeamThreads) f(e, value(e, cand[e]));
+  };
+  uint32_t top = 0;
+  for_each([&](int, uint64_t v) { top = max(top, (uint32_t)(v >> 32)); });
+  // a bound that K candidates reach, from the threads' largest: with a candidate or two to a thread about K are left
+  uint64_t from = 0;
+  if (n > K) {
+    each[tid] = top;
+    __syncthreads();
+    const uint32_t mine[4] = {each[lane], each[64 + lane], each[128 + lane], each[192 + lane]};
+    from = (uint64_t)wave_bound<8>(mine, K) << 32;
   }
+  for_each([&](int e, uint64_t v) {
+    if (v && v >= from) {
+      const int i = atomicAdd(&kept_n, 1);          // a set: its order does not matter
+      kept_value[i] = v;
+      kept_at[i] = (uint16_t)e;
+    }
+  });
   __syncthreads();
   const int m = kept_n;
-  float* os = a.out_scores + (size_t)r * a.K;
-  int32_t* ob = a.out_beams + (size_t)r * a.K;
-  int32_t* ot = a.out_tokens + (size_t)r * a.K;
+  float* os = a.out_scores + (size_t)r * K;
+  int32_t* ob = a.out_beams + (size_t)r * K;
+  int32_t* ot = a.out_tokens + (size_t)r * K;
   for (int i = tid; i < m; i += kBeamThreads) {
     const uint64_t v = kept_value[i];
-    const int e = kept_at[i];
+    const int e = kept_at[i], b = beam_of(e);
+    const uint64_t k = cand[e];
     int p = 0;
+#pragma unroll 4
     for (int j = 0; j < m; ++j) p += kept_value[j] > v || (kept_value[j] == v && kept_at[j] < e);
-    if (p >= a.K) continue;
-    const int b = e / per;
+    if (p >= K) continue;
     os[p] = (float)__builtin_bit_cast(double, v ^ ((v >> 63) ? 1ull << 63 : ~0ull));
     ob[p] = b;
-    ot[p] = beam_reads(a, r * a.B + b) ? beam_token(cand[e]) : a.end;
+    ot[p] = reads[b] ? beam_token(k) : a.end;
   }
-  for (int p = m + tid; p < a.K; p += kBeamThreads) os[p] = ninf, ob[p] = -1, ot[p] = a.end;
+  for (int p = m + tid; p < K; p += kBeamThreads) os[p] = ninf, ob[p] = -1, ot[p] = a.end;
 }
 
 // ---------------------------------------------------------------------------

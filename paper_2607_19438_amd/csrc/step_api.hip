@@ -97,14 +97,17 @@ struct BeamPlan {
   long bytes;
 };
 
-// A row goes to as many workgroups as leave each a step of 4096 logits, while 1024 of all rows are not passed, nor what the
-// second kernel takes.
+// A row goes to as many workgroups as leave each of its waves a step, while 768 of all rows are not passed, nor the 1024
+// candidates that the second kernel takes fast; of more rows than that to three, so that the last workgroups are short.
+// (us, both kernels, by pieces: 4 rows of 32000, K = 4: 2 12.8, 4 11.2, 8 10.5; 85 of 50021, K = 10: 1 26.1, 3 17.4, 7 15.8,
+// 13 16.6; 384 of 128000, K = 16: 1 58.0, 2 47.3, 3 50.8, 8 53.1; 1200 of 32000, K = 8: 1 42.1, 3 39.5, 8 48.6; 8 of
+// 128000, K = 16: 4 21.3, 8 18.6, 16 19.4, 32 24.1.)
 BeamPlan beam_plan(int R, int B, int V, int K) {
   BeamPlan p{};
   const long rows = (long)R * B;
-  long pieces = std::min<long>(qg::ceil_div(V, qg::kBeamStep), std::max<long>(1, 1024 / rows));
+  long pieces = std::min<long>(qg::ceil_div(V, qg::kBeamPiece), rows <= 768 ? 768 / rows : 3);
   pieces = std::max<long>(1, std::min<long>(pieces, qg::kBeamMost / ((long)B * K)));
-  p.piece = (int)std::min<long>(qg::ceil_div(qg::ceil_div(V, pieces), qg::kBeamStep) * qg::kBeamStep, 0x7fffffffL / qg::kBeamStep * qg::kBeamStep);
+  p.piece = (int)(qg::ceil_div(qg::ceil_div(V, pieces), qg::kBeamPiece) * qg::kBeamPiece);
   p.pieces = (int)qg::ceil_div(V, p.piece);
   p.bytes = rows * p.pieces * ((long)sizeof(qg::BeamStat) + (long)K * (long)sizeof(uint64_t));
   return p;
@@ -283,14 +286,17 @@ int qgemm_beam_select(const void* logits, int type, const float* scores, const u
   a.pieces = plan.pieces;
   a.piece = plan.piece;
   a.end = end;
+  while (a.pieces_log2 < 6 && (1 << a.pieces_log2) < plan.pieces) ++a.pieces_log2;
+  const long per = (long)plan.pieces * K;
+  a.per_inv = per == 1 ? 0u : (uint32_t)(((1L << 32) + per - 1) / per);
   (void)hipGetLastError();
   const dim3 grid((unsigned)(rows * plan.pieces)), block(qg::kBeamThreads);
   if (type == QGEMM_F32) hipLaunchKernelGGL(qg::beam_rows_kernel<float>, grid, block, 0, stream, a);
   else hipLaunchKernelGGL(qg::beam_rows_kernel<uint16_t>, grid, block, 0, stream, a);
   rc = check_launch("qgemm_beam_select");
   if (rc != QGEMM_OK) return rc;
-  const long n = (long)B * plan.pieces * K, kept = std::min(n, K * qg::ceil_div(n, qg::kBeamThreads));
-  hipLaunchKernelGGL(qg::beam_join_kernel, dim3((unsigned)R), block, (size_t)kept * 12, stream, a);
+  if ((long)B * plan.pieces * K <= qg::kBeamMost) hipLaunchKernelGGL(qg::beam_join_kernel<qg::kBeamMost>, dim3((unsigned)R), block, 0, stream, a);
+  else hipLaunchKernelGGL((qg::beam_join_kernel<qg::kBeamMaxB * qg::kBeamMaxK>), dim3((unsigned)R), block, 0, stream, a);
   rc = check_launch("qgemm_beam_select (join)");
   return rc == QGEMM_OK ? ok() : rc;
 }
