@@ -482,7 +482,7 @@ int qgemm_kv_reorder(const int32_t* block_table, const int32_t* kv_len, const in
                      int32_t* src, int32_t* dst, int32_t* used, int32_t* released, int32_t* n_released,
                      void* workspace, int64_t workspace_bytes, int R, int B, int W, int F, int Q, int page,
                      hipStream_t stream);
-int qgemm_kv_reorder_workspace(int R, int W, int64_t* bytes);
+int qgemm_kv_reorder_workspace(int R, int B, int W, int64_t* bytes);
 
 /*
  * Whole pages within a 4-bit cache: page src[i] (all heads) to page dst[i] for i < n. Pairs with a page outside

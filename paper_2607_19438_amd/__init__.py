@@ -61,7 +61,7 @@ EXPORTS = {
     "qgemm_beam_select": (_i, [_vp, _i] + [_vp] * 6 + [_l] + [_i] * 4 + [_l, _i, _vp]),
     "qgemm_beam_select_workspace": (_i, [_i] * 4 + [ctypes.POINTER(_l)]),
     "qgemm_kv_reorder": (_i, [_vp] * 13 + [_l] + [_i] * 6 + [_vp]),
-    "qgemm_kv_reorder_workspace": (_i, [_i] * 2 + [ctypes.POINTER(_l)]),
+    "qgemm_kv_reorder_workspace": (_i, [_i] * 3 + [ctypes.POINTER(_l)]),
     "qgemm_kv4_copy": (_i, [_vp] * 3 + [_i] * 5 + [_vp]),
     "qgemm_adapters": (_i, [_vp] * 8 + [_l] + [_i] * 6 + [_l, _l, _vp]),
     "qgemm_adapters_workspace": (_i, [_i] * 4 + [ctypes.POINTER(_l)]),
@@ -872,7 +872,7 @@ def kv_reorder(block_table: torch.Tensor, kv_len: torch.Tensor, parents: torch.T
             if t.shape != shape:
                 raise ValueError(f"out.{name} must have the shape {shape}")
         _device(block_table, *(getattr(out, name) for name in KvReorder.__slots__))
-    need = _workspace("kv_reorder", R, W)
+    need = _workspace("kv_reorder", R, B, W)
     ws = torch.empty(need, dtype=torch.uint8, device=block_table.device)
     _enqueue(lib().qgemm_kv_reorder, dev, block_table.data_ptr(), kv_len.data_ptr(), parents.data_ptr(), free_pages.data_ptr(),
              None if keep is None else keep.data_ptr(), out.block_table.data_ptr(), out.kv_len.data_ptr(), out.src.data_ptr(),

@@ -428,6 +428,12 @@ __global__ __launch_bounds__(kBeamThreads) void beam_join_kernel(BeamArgs a) {
 // ---------------------------------------------------------------------------
 // tables and pages after a selection
 // ---------------------------------------------------------------------------
+//
+// A workgroup takes 256 columns of a request's tables. Every one counts for itself the pages that the requests before
+// take from the free list (a thread to a row: a few loads), so that nothing waits for another. Pages that no row holds any
+// more are left in the caller's workspace, and a second kernel, which knows how many the workgroups before have
+// found, moves them to their places in the list.
+// Bound by chains of loads: lengths and parents, old entries, then the counts of the first kernel.
 
 constexpr int kReorderThreads = 256;
 constexpr int kReorderMaxRows = 1 << 16;       // R * B
@@ -446,32 +452,60 @@ struct ReorderArgs {
   int32_t* released;          // [Q]
   int32_t* n_released;
   int32_t* counts;            // [R * blocks] pages that a workgroup's columns release
+  int32_t* gone;              // [R * blocks][256 B] the pages
   int R, B, W, F, Q, page_log2, blocks;
 };
 
 struct ReorderBeams {
   int len[kBeamMaxB], have[kBeamMaxB];                   // old rows: tokens, and pages (within the table)
-  int parent[kBeamMaxB], fresh[kBeamMaxB];               // new rows: old row or -1; place in the free list or -1
+  int parent[kBeamMaxB], fresh[kBeamMaxB];               // new rows: old row or -1; place in the request's free pages or -1
+  int4 row[kBeamMaxB];                                   // new rows: old row or 0; the column of a fresh page or -1, and the page;
+                                                         // whether there is an old row
   unsigned long long live, childless;                    // old rows that have children; that have pages and none
   int taken;                                             // new rows with a fresh page
   int wave[kReorderThreads / 64];
 };
 
-// The request's beams; returns how many pages the requests before it take from the free list. Every workgroup counts for
-// itself, so that nothing waits for another.
+// The request's beams; returns how many pages the requests before it take from the free list.
 __device__ __forceinline__ int reorder_beams(const ReorderArgs& a, int r, ReorderBeams& s) {
   const int tid = threadIdx.x, lane = tid & 63, B = a.B, mask = (1 << a.page_log2) - 1;
-  // whether new row k of request q takes a fresh page: not its parent's first child, and the parent's last page partly filled
-  auto takes_page = [&](int q, int k) {
-    const int32_t* of = a.parents + (size_t)q * B;
-    const int p = of[k];
-    if ((unsigned)p >= (unsigned)B || (max(a.kv_len[(size_t)q * B + p], 0) & mask) == 0) return false;
-    bool again = false;
-    for (int i = 0; i < k; ++i) again |= of[i] == p;
-    return again;
-  };
+  // a request to a thread: the rows that are not their parent's first child, of parents with a last page filled in part
   int mine = 0;
-  for (int row = tid; row < r * B; row += kReorderThreads) mine += takes_page(row / B, row % B);
+  for (int q = tid; q < r; q += kReorderThreads) {
+    const int32_t *len = a.kv_len + (size_t)q * B, *of = a.parents + (size_t)q * B;
+    unsigned long long part = 0, seen = 0;
+    int n[8], p[8];
+    auto load = [&](int b0) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        n[i] = len[min(b0 + i, B - 1)];
+        p[i] = of[min(b0 + i, B - 1)];
+      }
+    };
+    auto parts = [&](int b0) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) part |= (unsigned long long)((max(n[i], 0) & mask) != 0) << min(b0 + i, B - 1);
+    };
+    auto count = [&](int b0) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const unsigned long long bit = b0 + i < B && (unsigned)p[i] < (unsigned)B ? 1ull << p[i] : 0ull;
+        mine += (seen & part & bit) != 0;
+        seen |= bit;
+      }
+    };
+    for (int b0 = 8; b0 < B; b0 += 8) {          // (a parent may stand behind)
+      load(b0);
+      parts(b0);
+    }
+    load(0);
+    parts(0);
+    count(0);
+    for (int b0 = 8; b0 < B; b0 += 8) {
+      load(b0);
+      count(b0);
+    }
+  }
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) mine += __shfl_xor(mine, d);
   if (lane == 0) s.wave[tid >> 6] = mine;
@@ -481,7 +515,15 @@ __device__ __forceinline__ int reorder_beams(const ReorderArgs& a, int r, Reorde
     const int have = (int)min(((long)n + mask) >> a.page_log2, (long)a.W);
     const int of = in ? a.parents[(size_t)r * B + tid] : -1;
     const int p = (unsigned)of < (unsigned)B ? of : -1;
-    const unsigned long long fresh = __ballot(in && takes_page(r, in ? tid : 0));
+    // the first row of the same parent, and that parent's length, from the other lanes
+    bool again = false;
+    for (int i = 0; i < B; ++i) {
+      const int other = __shfl(p, i);
+      again |= i < tid && other == p;
+    }
+    const int of_parent = __shfl(n, max(p, 0));
+    const bool part = (of_parent & mask) != 0;
+    const unsigned long long fresh = __ballot(in && p >= 0 && again && part);
     if (in) {
       s.len[tid] = n;
       s.have[tid] = have;
@@ -501,89 +543,89 @@ __device__ __forceinline__ int reorder_beams(const ReorderArgs& a, int r, Reorde
   return before;
 }
 
-// Of the column's old entries, those that no new row holds any more: bit b for old row b. A page stands in the same column
-// of all rows that share it, and a row's children hold all of its pages, so only rows without children can lose one.
-__device__ __forceinline__ unsigned long long reorder_gone(const ReorderArgs& a, const ReorderBeams& s, const int32_t* old, int j) {
-  unsigned long long gone = 0;
-  for (unsigned long long m = s.childless; m; m &= m - 1) {
-    const int b = __builtin_ctzll(m);
-    if (j >= s.have[b]) continue;
-    const int id = old[(size_t)b * a.W + j];
-    bool stays = id < 0;
-    for (unsigned long long l = s.live; l && !stays; l &= l - 1) {
-      const int p = __builtin_ctzll(l);
-      stays = j < s.have[p] && old[(size_t)p * a.W + j] == id;
-    }
-    for (unsigned long long l = s.childless & ((1ull << b) - 1); l && !stays; l &= l - 1) {       // listed once
-      const int p = __builtin_ctzll(l);
-      stays = j < s.have[p] && old[(size_t)p * a.W + j] == id;
-    }
-    if (!stays) gone |= 1ull << b;
-  }
-  return gone;
-}
-
-// A workgroup takes 256 columns of a request's tables.
 __global__ __launch_bounds__(kReorderThreads) void kv_reorder_kernel(ReorderArgs a) {
+  extern __shared__ int32_t old_lds[];         // [B][256] the columns' old entries, each thread its own; -1 behind a row's pages
   __shared__ ReorderBeams s;
   __shared__ int gone_n[kReorderThreads / 64];
-  const int tid = threadIdx.x, lane = tid & 63, B = a.B;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, B = a.B;
   const int r = blockIdx.x / a.blocks, block = blockIdx.x - r * a.blocks;
-  const int before = reorder_beams(a, r, s);
   const int32_t* old = a.table + (size_t)r * B * a.W;
-  if (block == 0 && tid < B) {
-    const int p = s.parent[tid];
-    const size_t row = (size_t)r * B + tid;
-    int src = -1, dst = -1;
-    if (s.fresh[tid] >= 0) {
-      const int last = s.len[p] >> a.page_log2;
-      const long at = (long)before + s.fresh[tid];
-      if (at < a.F && last < a.W) {
-        src = old[(size_t)p * a.W + last];
-        dst = a.free_pages[at];
-      }
+  const int j = block * kReorderThreads + tid;
+  // the first eight rows' entries are on their way while the request's beams are looked up
+  int32_t x[8];
+  auto load = [&](int b0) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = b0 + i < B && j < a.W ? old[(size_t)(b0 + i) * a.W + j] : -1;
+  };
+  load(0);
+  const int first = a.keep ? max(a.keep[r], 0) : 0;
+  const int before = reorder_beams(a, r, s);
+  if (tid < B) {
+    const int p = s.parent[tid], fresh = s.fresh[tid], last = p < 0 ? 0 : s.len[p] >> a.page_log2;
+    const bool can = fresh >= 0 && last < a.W && (long)before + fresh < a.F;
+    const int page = can ? a.free_pages[(size_t)before + fresh] : -1;
+    s.row[tid] = make_int4(max(p, 0), fresh >= 0 ? last : -1, page, p >= 0);
+    if (block == 0) {
+      const size_t row = (size_t)r * B + tid;
+      a.new_len[row] = p < 0 ? 0 : s.len[p];
+      a.src[row] = can ? old[(size_t)p * a.W + last] : -1;
+      a.dst[row] = page;
     }
-    a.new_len[row] = p < 0 ? 0 : s.len[p];
-    a.src[row] = src;
-    a.dst[row] = dst;
   }
   if (r == a.R - 1 && block == 0 && tid == 0) a.used[0] = before + s.taken;
-  const int j = block * kReorderThreads + tid;
+  __syncthreads();
+  auto entry = [&](int b) -> int32_t& { return old_lds[b * kReorderThreads + tid]; };
+  for (int b0 = 0; b0 < B; b0 += 8) {
+    if (b0) load(b0);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (b0 + i < B) entry(b0 + i) = j < s.have[b0 + i] ? x[i] : -1;
+  }
   unsigned long long gone = 0;
   if (j < a.W) {
-    for (int k = 0; k < B; ++k) {
-      const int p = s.parent[k];
-      int id = -1;
-      if (p >= 0 && j < s.have[p]) {
-        if (s.fresh[k] >= 0 && j == s.len[p] >> a.page_log2) {
-          const long at = (long)before + s.fresh[k];
-          if (at < a.F) id = a.free_pages[at];
-        } else {
-          id = old[(size_t)p * a.W + j];
-        }
-      }
-      a.new_table[((size_t)r * B + k) * a.W + j] = id;
+    int32_t* out = a.new_table + (size_t)r * B * a.W + j;
+#pragma unroll 4
+    for (int k = 0; k < B; ++k, out += a.W) {
+      const int4 row = s.row[k];
+      *out = !row.w ? -1 : j == row.y ? row.z : entry(row.x);
     }
-    if (j >= (a.keep ? max(a.keep[r], 0) : 0)) gone = reorder_gone(a, s, old, j);
+    // Of the column's old entries, those that no new row holds any more. A page stands in the same column of all rows that
+    // share it, and a row's children hold all of its pages, so only rows without children can lose one.
+    if (j >= first)
+      for (unsigned long long m = s.childless; m; m &= m - 1) {
+        const int b = __builtin_ctzll(m), id = entry(b);
+        const unsigned long long others = s.live | (s.childless & ((1ull << b) - 1));      // (the lower ones list a page that they share)
+        bool stays = id < 0;
+#pragma unroll 8
+        for (int p = 0; p < B; ++p) stays |= entry(p) == id && (others >> p & 1);
+        if (!stays) gone |= 1ull << b;
+      }
   }
-  int n = __builtin_popcountll(gone);
+  // the pages, by column and row
+  const int n = __builtin_popcountll(gone);
+  int inc = n;
 #pragma unroll
-  for (int d = 1; d < 64; d <<= 1) n += __shfl_xor(n, d);
-  if (lane == 0) gone_n[tid >> 6] = n;
+  for (int d = 1; d < 64; d <<= 1) {
+    const int up = __shfl_up(inc, d);
+    if (lane >= d) inc += up;
+  }
+  if (lane == 63) gone_n[wave] = inc;
   __syncthreads();
-  if (tid == 0) {
-    int t = 0;
+  int at = inc - n, all = 0;
 #pragma unroll
-    for (int i = 0; i < kReorderThreads / 64; ++i) t += gone_n[i];
-    a.counts[blockIdx.x] = t;
+  for (int i = 0; i < kReorderThreads / 64; ++i) {
+    at += i < wave ? gone_n[i] : 0;
+    all += gone_n[i];
   }
+  if (tid == 0) a.counts[blockIdx.x] = all;
+  for (int32_t* out = a.gone + (size_t)blockIdx.x * kReorderThreads * B; gone; gone &= gone - 1) out[at++] = entry(__builtin_ctzll(gone));
 }
 
-// The pages that no row holds any more, by request, column and row, and -1 behind them.
+// The released pages to their places, -1 behind the last.
 __global__ __launch_bounds__(kReorderThreads) void kv_release_kernel(ReorderArgs a) {
-  __shared__ ReorderBeams s;
   __shared__ int sums[kReorderThreads / 64][2];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, nblk = a.R * a.blocks, me = (int)blockIdx.x;
+  const int tid = threadIdx.x, lane = tid & 63, nblk = a.R * a.blocks, me = (int)blockIdx.x;
+  const int mine = a.counts[me];
   int before = 0, all = 0;
   for (int i = tid; i < nblk; i += kReorderThreads) {
     const int c = a.counts[i];
@@ -592,33 +634,15 @@ __global__ __launch_bounds__(kReorderThreads) void kv_release_kernel(ReorderArgs
   }
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) before += __shfl_xor(before, d), all += __shfl_xor(all, d);
-  if (lane == 0) sums[wave][0] = before, sums[wave][1] = all;
+  if (lane == 0) sums[tid >> 6][0] = before, sums[tid >> 6][1] = all;
   __syncthreads();
   before = all = 0;
 #pragma unroll
   for (int i = 0; i < kReorderThreads / 64; ++i) before += sums[i][0], all += sums[i][1];
   if (me == 0 && tid == 0) a.n_released[0] = all;
   for (long i = (long)all + (long)me * kReorderThreads + tid; i < a.Q; i += (long)nblk * kReorderThreads) a.released[i] = -1;
-  if (a.counts[me] == 0) return;
-  __syncthreads();
-  const int r = me / a.blocks, block = me - r * a.blocks, j = block * kReorderThreads + tid;
-  reorder_beams(a, r, s);
-  const int32_t* old = a.table + (size_t)r * a.B * a.W;
-  unsigned long long gone = 0;
-  if (j < a.W && j >= (a.keep ? max(a.keep[r], 0) : 0)) gone = reorder_gone(a, s, old, j);
-  const int n = __builtin_popcountll(gone);
-  int inc = n;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int up = __shfl_up(inc, d);
-    if (lane >= d) inc += up;
-  }
-  if (lane == 63) s.wave[wave] = inc;
-  __syncthreads();
-  int at = before + inc - n;
-  for (int i = 0; i < wave; ++i) at += s.wave[i];
-  for (; gone; gone &= gone - 1, ++at)
-    if (at < a.Q) a.released[at] = old[(size_t)__builtin_ctzll(gone) * a.W + j];
+  const int32_t* from = a.gone + (size_t)me * kReorderThreads * a.B;
+  for (int i = tid; i < mine && before + i < a.Q; i += kReorderThreads) a.released[before + i] = from[i];
 }
 
 struct CopyArgs {

@@ -123,6 +123,9 @@ int check_beams(int R, int B, int V, int K) {
   return QGEMM_OK;
 }
 
+// int32 entries of the workspace: a count for each workgroup, and room for all of its columns' pages
+int64_t reorder_entries(int64_t blocks, int B) { return blocks * (1 + (int64_t)qg::kReorderThreads * B); }
+
 int reorder_blocks(int W) { return (int)std::max<long>(1, qg::ceil_div(W, qg::kReorderThreads)); }
 
 int check_reorder(int R, int B, int W, int F, int Q, int page) {
@@ -301,10 +304,11 @@ int qgemm_beam_select(const void* logits, int type, const float* scores, const u
   return rc == QGEMM_OK ? ok() : rc;
 }
 
-int qgemm_kv_reorder_workspace(int R, int W, int64_t* bytes) {
+int qgemm_kv_reorder_workspace(int R, int B, int W, int64_t* bytes) {
   if (!bytes) return fail(QGEMM_EINVAL, "null pointer argument");
-  if (R < 0 || W < 0) return fail(QGEMM_EINVAL, "R and W must be >= 0 (got %d, %d)", R, W);
-  *bytes = (int64_t)R * reorder_blocks(W) * (int64_t)sizeof(int32_t);
+  const int rc = check_reorder(R, B, W, 0, 0, 16);
+  if (rc != QGEMM_OK) return rc;
+  *bytes = reorder_entries((int64_t)R * reorder_blocks(W), B) * (int64_t)sizeof(int32_t);
   return ok();
 }
 
@@ -323,19 +327,20 @@ int qgemm_kv_reorder(const int32_t* block_table, const int32_t* kv_len, const in
                         (const void*)released, (const void*)n_released, (const void*)workspace})
     if (!aligned(p, 4)) return fail(QGEMM_EALIGN, "the tables must be 4-byte aligned");
   const int64_t rows = (int64_t)R * B, blocks = reorder_blocks(W), counts = R * blocks;
-  if (workspace_bytes < counts * (int64_t)sizeof(int32_t))
-    return fail(QGEMM_EINVAL, "a workspace of %lld bytes is needed (got %lld)", (long long)(counts * 4), (long long)workspace_bytes);
+  const int64_t entries = reorder_entries(counts, B);
+  if (workspace_bytes < entries * (int64_t)sizeof(int32_t))
+    return fail(QGEMM_EINVAL, "a workspace of %lld bytes is needed (got %lld)", (long long)(entries * 4), (long long)workspace_bytes);
   const PlanTable written[] = {{"new_table", new_table, rows * W}, {"new_len", new_len, rows}, {"src", src, rows}, {"dst", dst, rows}, {"used", used, 1},
-                               {"released", released, Q}, {"n_released", n_released, 1}, {"workspace", static_cast<int32_t*>(workspace), counts}};
+                               {"released", released, Q}, {"n_released", n_released, 1}, {"workspace", static_cast<int32_t*>(workspace), entries}};
   const PlanTable read[] = {{"block_table", block_table, rows * W}, {"kv_len", kv_len, rows}, {"parents", parents, rows},
                             {"free_pages", free_pages, F}, {"keep", keep, keep ? R : 0}};
   rc = check_apart(written, 8, read, 5);
   if (rc != QGEMM_OK) return rc;
   qg::ReorderArgs a{block_table, kv_len, parents, free_pages, keep, new_table, new_len, src, dst, used, released, n_released,
-                    static_cast<int32_t*>(workspace), R, B, W, F, Q, page_log2(page), (int)blocks};
+                    static_cast<int32_t*>(workspace), static_cast<int32_t*>(workspace) + counts, R, B, W, F, Q, page_log2(page), (int)blocks};
   if (!qg::grid_fits(counts, qg::kReorderThreads)) return fail(QGEMM_EUNSUPPORTED, "too many workgroups");
   (void)hipGetLastError();
-  hipLaunchKernelGGL(qg::kv_reorder_kernel, dim3((unsigned)counts), dim3(qg::kReorderThreads), 0, stream, a);
+  hipLaunchKernelGGL(qg::kv_reorder_kernel, dim3((unsigned)counts), dim3(qg::kReorderThreads), (size_t)B * qg::kReorderThreads * sizeof(int32_t), stream, a);
   rc = check_launch("qgemm_kv_reorder");
   if (rc != QGEMM_OK) return rc;
   hipLaunchKernelGGL(qg::kv_release_kernel, dim3((unsigned)counts), dim3(qg::kReorderThreads), 0, stream, a);

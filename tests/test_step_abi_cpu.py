@@ -60,18 +60,18 @@ def test_beam_select_refusals(m):
 
 def test_kv_reorder_refusals(m):
     names = ("tab", "kv", "par", "free", "keep", "new", "len", "src", "dst", "used", "rel", "nrel", "ws")
-    size = dict(tab=24, kv=6, par=6, free=5, keep=2, new=24, len=6, src=6, dst=6, used=1, rel=7, nrel=1, ws=2)
-    at = {name: (i + 1) << 12 for i, name in enumerate(names)}
-    ok = dict(at, bytes=8, R=2, B=3, W=4, F=5, Q=7, page=16)
+    size = dict(tab=24, kv=6, par=6, free=5, keep=2, new=24, len=6, src=6, dst=6, used=1, rel=7, nrel=1, ws=2 * (1 + 256 * 3))
+    at = {name: (i + 1) << 14 for i, name in enumerate(names)}
+    ok = dict(at, bytes=4 * size["ws"], R=2, B=3, W=4, F=5, Q=7, page=16)
     f = m.lib().qgemm_kv_reorder
     call = caller(f, ok)
-    for kw in ({"R": -1}, {"B": 0}, {"W": -1}, {"F": -1}, {"Q": -1}, {"page": 8}, {"page": 24}, {"page": 2048}, {"bytes": 7},
+    for kw in ({"R": -1}, {"B": 0}, {"W": -1}, {"F": -1}, {"Q": -1}, {"page": 8}, {"page": 24}, {"page": 2048}, {"bytes": 4 * size["ws"] - 1},
                *({n: 0} for n in names if n != "keep")):
         assert call(**kw) == -1, kw
     for kw in ({"B": 65}, {"R": 65536}, {"W": 1 << 30}):
         assert call(**kw) == -3, kw
     for n in names:
-        assert call(**{n: 4098}) == -2, n
+        assert call(**{n: at[n] + 2}) == -2, n
     assert call(R=0) == 0
     for a in ("new", "len", "src", "dst", "used", "rel", "nrel", "ws"):
         for b in names:
@@ -80,9 +80,9 @@ def test_kv_reorder_refusals(m):
                 assert "overlap" in m.last_error(), (a, b, shift)
     n = ctypes.c_int64(-1)
     w = m.lib().qgemm_kv_reorder_workspace
-    assert w(2, 4, None) == -1 and w(-1, 4, ctypes.byref(n)) == -1
-    assert w(2, 4, ctypes.byref(n)) == 0 and n.value == 8
-    assert w(3, 600, ctypes.byref(n)) == 0 and n.value == 36
+    assert w(2, 3, 4, None) == -1 and w(-1, 3, 4, ctypes.byref(n)) == -1 and w(2, 65, 4, ctypes.byref(n)) == -3
+    assert w(2, 3, 4, ctypes.byref(n)) == 0 and n.value == ok["bytes"]
+    assert w(3, 1, 600, ctypes.byref(n)) == 0 and n.value == 4 * 9 * 257
 
 
 def test_kv4_copy_refusals(m):
