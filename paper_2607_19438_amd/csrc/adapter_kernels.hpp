@@ -19,6 +19,7 @@ namespace {
 constexpr int kAdThreads = 256;
 constexpr int kAdWaves = kAdThreads / 64;
 constexpr int kAdMaxRank = 128;
+constexpr int kAdRun = 128;         // of K: what a wave loads at once, 256 bytes of each row
 
 struct AdapterArgs {
   const uint16_t* x;       // bf16 [M][K] at xs
@@ -34,7 +35,7 @@ struct AdapterArgs {
   int M, N, K, r, n, R;
   int splits, k_split;     // parts of K, and their length (a multiple of 32 kAdWaves)
   int lists;               // workgroups that share a tile's adapters
-  int vec;                 // y's rows and columns go 16 bytes at a time
+  int chunks;              // of the columns of a workgroup
 };
 
 // The adapter of row m: the last request that begins at or before it, if it has a row there.
@@ -55,39 +56,29 @@ __device__ __forceinline__ int adapter_of(const AdapterArgs& a, int m) {
   return (unsigned)id < (unsigned)a.n ? id : -1;
 }
 
-template <int ROWS>
-struct AdapterTile {
-  int id[ROWS];            // of the tile's rows
-  int list[ROWS];          // distinct ones, by their first rows
-  int n;
+typedef float f32x4_by4 __attribute__((ext_vector_type(4), aligned(4)));       // y's rows need no more than their elements' alignment
+
+// The distinct adapters of a tile's rows, a lane's row each (id -1: none), in the order of their first rows: next() gives one
+// after the other, the same in all lanes.
+struct AdapterList {
+  int id;
+  unsigned long long left;
+  __device__ __forceinline__ explicit AdapterList(int of) : id(of), left(__ballot(of >= 0)) {}
+  __device__ __forceinline__ int next() {
+    const int i = __builtin_amdgcn_readlane(id, __builtin_ctzll(left));
+    left &= ~__ballot(id == i);
+    return i;
+  }
 };
 
-// Lists the distinct adapters of a tile's rows (ROWS <= 64: a lane of the first wave to a row).
-template <int ROWS>
-__device__ __forceinline__ void adapter_list(AdapterTile<ROWS>& s, int id) {
-  const int lane = threadIdx.x;
-  if (lane < 64) {
-    if (lane < ROWS) s.id[lane] = id;
-    bool first = lane < ROWS && id >= 0;
-    for (int i = 0; i < ROWS; ++i) {
-      const int other = __shfl(id, i);
-      first = first && !(i < lane && other == id);
-    }
-    const unsigned long long firsts = __ballot(first);
-    if (first) s.list[__builtin_popcountll(firsts & ((1ull << lane) - 1))] = id;
-    if (lane == 0) s.n = __builtin_popcountll(firsts);
-  }
-  __syncthreads();
-}
-
-// mid[m][j] = gain sum_k a[id][j][k] x[m][k] over one part of K, whose runs of 32 the four waves take in turn.
-// MT: 16-row tiles of x; JT: 16-row tiles of A.
-template <int MT, int JT>
-__global__ __launch_bounds__(kAdThreads) void adapter_down_kernel(AdapterArgs a) {
-  constexpr int ROWS = 16 * MT;
-  __shared__ AdapterTile<ROWS> s;
-  __shared__ f32x4 red[kAdWaves][JT * MT][64];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 15, g = lane >> 4;
+// mid[m][j] = gain sum_k a[id][j][k] x[m][k] over one part of K, whose runs of 32 the WAVES waves take in turn, four runs'
+// loads at once. MT: 16-row tiles of x; JT: 16-row tiles of A.
+template <int MT, int JT, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void adapter_down_kernel(AdapterArgs a) {
+  constexpr int ROWS = 16 * MT, DEEP = kAdRun / 32;
+  __shared__ f32x4 red[WAVES][JT * MT][64];
+  const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int jb = (a.r + 16 * JT - 1) / (16 * JT);
   int w = blockIdx.x;
   const int j0 = w % jb * 16 * JT;
@@ -96,37 +87,52 @@ __global__ __launch_bounds__(kAdThreads) void adapter_down_kernel(AdapterArgs a)
   w /= a.splits;
   const int lane_of_list = w % a.lists;
   const int m0 = w / a.lists * ROWS;
-  const int own = tid < ROWS ? adapter_of(a, m0 + tid) : -1;
+  const int own = lane < ROWS ? adapter_of(a, m0 + lane) : -1;
   if (tid < ROWS && m0 + tid < a.M && split == 0 && lane_of_list == 0 && j0 == 0) a.row_id[m0 + tid] = own;
-  adapter_list(s, own);
   const int k_begin = split * a.k_split, k_end = min(a.K, k_begin + a.k_split);
   const uint16_t* xp[MT];
+  int mine[MT];
 #pragma unroll
-  for (int t = 0; t < MT; ++t) xp[t] = a.x + (size_t)min(m0 + 16 * t + col, a.M - 1) * a.xs + 8 * g;
-  for (int d = lane_of_list; d < s.n; d += a.lists) {
-    const int id = s.list[d];
+  for (int t = 0; t < MT; ++t) {
+    xp[t] = a.x + (size_t)min(m0 + 16 * t + col, a.M - 1) * a.xs;
+    mine[t] = __shfl(own, 16 * t + col);
+  }
+  AdapterList list(own);
+  for (int d = 0; list.left; ++d) {
+    const int id = list.next();
+    if (d % a.lists != lane_of_list) continue;
     const uint16_t* ap[JT];
 #pragma unroll
     for (int t = 0; t < JT; ++t)       // rows past the rank give products that nobody keeps
-      ap[t] = a.a + ((size_t)id * a.r + min(j0 + 16 * t + col, a.r - 1)) * a.K + 8 * g;
+      ap[t] = a.a + ((size_t)id * a.r + min(j0 + 16 * t + col, a.r - 1)) * a.K;
     f32x4 acc[JT][MT];
 #pragma unroll
     for (int j = 0; j < JT; ++j)
 #pragma unroll
       for (int t = 0; t < MT; ++t) acc[j][t] = f32x4{};
-    for (int k = k_begin + 32 * wave; k < k_end; k += 32 * kAdWaves) {
-      const bool in = k + 8 * g < k_end;              // (K is a multiple of 8)
-      bf16x8 xf[MT], af[JT];
+    for (int k0 = k_begin + kAdRun * wave; k0 < k_end; k0 += kAdRun * WAVES) {
+      u32x4 xf[DEEP][MT], af[DEEP][JT];
 #pragma unroll
-      for (int t = 0; t < MT; ++t)
-        xf[t] = in ? __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(xp[t] + k)) : bf16x8{};
+      for (int u = 0; u < DEEP; ++u) {          // (past the end the last elements once more, taken as zero below; K is a multiple of 8)
+        const int k = min(k0 + 32 * u + 8 * g, a.K - 8);
 #pragma unroll
-      for (int j = 0; j < JT; ++j)
-        af[j] = in ? __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(ap[j] + k)) : bf16x8{};
+        for (int t = 0; t < MT; ++t) xf[u][t] = *reinterpret_cast<const u32x4*>(xp[t] + k);
 #pragma unroll
-      for (int j = 0; j < JT; ++j)
+        for (int j = 0; j < JT; ++j) af[u][j] = *reinterpret_cast<const u32x4*>(ap[j] + k);
+      }
 #pragma unroll
-        for (int t = 0; t < MT; ++t) acc[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(af[j], xf[t], acc[j][t], 0, 0, 0);
+      for (int u = 0; u < DEEP; ++u) {
+        const bool in = k0 + 32 * u + 8 * g < k_end;
+#pragma unroll
+        for (int t = 0; t < MT; ++t) xf[u][t] = in ? xf[u][t] : u32x4{};
+#pragma unroll
+        for (int j = 0; j < JT; ++j) {
+          af[u][j] = in ? af[u][j] : u32x4{};
+#pragma unroll
+          for (int t = 0; t < MT; ++t)
+            acc[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, af[u][j]), __builtin_bit_cast(bf16x8, xf[u][t]), acc[j][t], 0, 0, 0);
+        }
+      }
     }
 #pragma unroll
     for (int j = 0; j < JT; ++j)
@@ -134,14 +140,19 @@ __global__ __launch_bounds__(kAdThreads) void adapter_down_kernel(AdapterArgs a)
       for (int t = 0; t < MT; ++t) red[wave][j * MT + t][lane] = acc[j][t];
     __syncthreads();
     const float gain = a.gain ? a.gain[id] : 1.0f;
-    for (int p = wave; p < JT * MT; p += kAdWaves) {      // the waves' sums, in their order
+#pragma unroll
+    for (int p0 = 0; p0 < JT * MT; p0 += WAVES) {      // the waves' sums, in their order
+      const int p = p0 + wave;
+      if (p >= JT * MT) break;
       f32x4 sum = red[0][p][lane];
 #pragma unroll
-      for (int i = 1; i < kAdWaves; ++i) sum += red[i][p][lane];
+      for (int i = 1; i < WAVES; ++i) sum += red[i][p][lane];
       const int t = p % MT, j = j0 + 16 * (p / MT) + 4 * g, row = 16 * t + col;
+      int of = mine[0];
+#pragma unroll
+      for (int i = 1; i < MT; ++i) of = t == i ? mine[i] : of;
       // (r is a multiple of 8, and 4 g of 4: a lane's four are all in the rank or none)
-      if (j < a.r && s.id[row] == id)
-        *reinterpret_cast<f32x4*>(a.mid + ((size_t)split * a.M + m0 + row) * a.r + j) = sum * gain;
+      if (j < a.r && of == id) *reinterpret_cast<f32x4*>(a.mid + ((size_t)split * a.M + m0 + row) * a.r + j) = sum * gain;
     }
     __syncthreads();
   }
@@ -158,23 +169,45 @@ __device__ __forceinline__ void split_bf16(float x, uint32_t (&p)[3]) {
   }
 }
 
-// y[m][c] += sum_j b[id][c][j] mid[m][j]. A wave takes 16 MT rows and 16 NT columns. S: runs of 32 of the rank.
-template <int MT, int NT, int S>
+// y[m][c] += sum_j b[id][c][j] mid[m][j]. A wave takes 16 MT rows and `chunks` times 16 NT columns, the next of which are on
+// their way while it computes; its rows' mid stays in registers. S: runs of 32 of the rank. U: adapters whose weights
+// are loaded at once.
+template <int MT, int NT, int S, int U>
 __global__ __launch_bounds__(kAdThreads) void adapter_up_kernel(AdapterArgs a) {
-  constexpr int ROWS = 16 * MT;
-  __shared__ AdapterTile<ROWS> s;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 15, g = lane >> 4;
-  const int nb = (a.N + 16 * NT * kAdWaves - 1) / (16 * NT * kAdWaves);
+  constexpr int ROWS = 16 * MT, COLS = 16 * NT * kAdWaves;
+  const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int nb = (a.N + COLS * a.chunks - 1) / (COLS * a.chunks);
   const int m0 = (int)blockIdx.x / nb * ROWS;
-  const int n0 = ((int)blockIdx.x % nb * kAdWaves + wave) * 16 * NT;
-  adapter_list(s, tid < ROWS && m0 + tid < a.M ? a.row_id[m0 + tid] : -1);
-  if (s.n == 0) return;
+  int n0 = (int)blockIdx.x % nb * a.chunks * COLS + wave * 16 * NT;
+  const int n_end = min(a.N, ((int)blockIdx.x % nb + 1) * a.chunks * COLS);
+  if (n0 >= n_end) return;
+  const int own = lane < ROWS && m0 + lane < a.M ? a.row_id[m0 + lane] : -1;
+  auto load = [&](int at, f32x4 (&y)[MT][NT]) {
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+      const float* yp = a.y + (size_t)min(m0 + 16 * t + col, a.M - 1) * a.ys + at + 4 * g;
+#pragma unroll
+      for (int c = 0; c < NT; ++c) {
+        if (at + 16 * NT <= a.N) {
+          y[t][c] = *reinterpret_cast<const f32x4_by4*>(yp + 16 * c);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) y[t][c][e] = at + 16 * c + 4 * g + e < a.N ? yp[16 * c + e] : 0.0f;
+        }
+      }
+    }
+  };
+  f32x4 out[MT][NT];
+  load(n0, out);
+  const AdapterList all(own);
+  if (!all.left) return;
   int mine[MT];
   bf16x8 mid[MT][S][3];
 #pragma unroll
   for (int t = 0; t < MT; ++t) {
     const int m = m0 + 16 * t + col;
-    mine[t] = s.id[16 * t + col];
+    mine[t] = __shfl(own, 16 * t + col);
 #pragma unroll
     for (int k = 0; k < S; ++k) {
       const int j = 32 * k + 8 * g;
@@ -200,49 +233,66 @@ __global__ __launch_bounds__(kAdThreads) void adapter_up_kernel(AdapterArgs a) {
       for (int i = 0; i < 3; ++i) mid[t][k][i] = __builtin_bit_cast(bf16x8, w[i]);
     }
   }
-  if (n0 >= a.N) return;
-  f32x4 out[MT][NT];
+  for (;;) {
+    f32x4 next[MT][NT];
+    const bool more = n0 + COLS < n_end;
+    if (more) load(n0 + COLS, next);
+    AdapterList list = all;
+    while (list.left) {
+      int id[U];
+      u32x4 bf[U][NT][S];
 #pragma unroll
-  for (int t = 0; t < MT; ++t)
+      for (int u = 0; u < U; ++u) id[u] = u == 0 || list.left ? list.next() : id[0];       // (one of them again changes nothing)
 #pragma unroll
-    for (int c = 0; c < NT; ++c) out[t][c] = f32x4{};
-  for (int d = 0; d < s.n; ++d) {
-    const int id = s.list[d];
+      for (int u = 0; u < U; ++u)
 #pragma unroll
-    for (int c = 0; c < NT; ++c) {
-      const uint16_t* bp = a.b + ((size_t)id * a.N + min(n0 + 16 * c + col, a.N - 1)) * a.r + 8 * g;
-      bf16x8 bf[S];
+        for (int c = 0; c < NT; ++c) {
+          const uint16_t* bp = a.b + ((size_t)id[u] * a.N + min(n0 + 16 * c + col, a.N - 1)) * a.r;
 #pragma unroll
-      for (int k = 0; k < S; ++k)
-        bf[k] = 32 * k + 8 * g < a.r ? __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(bp + 32 * k)) : bf16x8{};
+          for (int k = 0; k < S; ++k) bf[u][c][k] = *reinterpret_cast<const u32x4*>(bp + min(32 * k + 8 * g, a.r - 8));
+        }
 #pragma unroll
-      for (int t = 0; t < MT; ++t) {
-        f32x4 acc = f32x4{};
+      for (int u = 0; u < U; ++u) {
 #pragma unroll
-        for (int i = 2; i >= 0; --i)       // the smallest first
+        for (int c = 0; c < NT; ++c) {
 #pragma unroll
-          for (int k = 0; k < S; ++k) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf[k], mid[t][k][i], acc, 0, 0, 0);
+          for (int k = 0; k < S; ++k) bf[u][c][k] = 32 * k + 8 * g < a.r ? bf[u][c][k] : u32x4{};
 #pragma unroll
-        for (int e = 0; e < 4; ++e) out[t][c][e] = mine[t] == id ? acc[e] : out[t][c][e];
+          for (int t = 0; t < MT; ++t) {
+            f32x4 acc = f32x4{};
+#pragma unroll
+            for (int i = 2; i >= 0; --i)       // the smallest first
+#pragma unroll
+              for (int k = 0; k < S; ++k)
+                acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, bf[u][c][k]), mid[t][k][i], acc, 0, 0, 0);
+            const bool keep = mine[t] == id[u] && (u == 0 || id[u] != id[0]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) out[t][c][e] = keep ? out[t][c][e] + acc[e] : out[t][c][e];
+          }
+        }
       }
     }
-  }
 #pragma unroll
-  for (int t = 0; t < MT; ++t) {
-    if (mine[t] < 0) continue;
-    float* yp = a.y + (size_t)(m0 + 16 * t + col) * a.ys;
+    for (int t = 0; t < MT; ++t) {
+      if (mine[t] < 0) continue;
+      float* yp = a.y + (size_t)(m0 + 16 * t + col) * a.ys + n0 + 4 * g;
 #pragma unroll
-    for (int c = 0; c < NT; ++c) {
-      const int n = n0 + 16 * c + 4 * g;
-      if (a.vec && n + 3 < a.N) {
-        f32x4* q = reinterpret_cast<f32x4*>(yp + n);
-        *q = *q + out[t][c];
-      } else {
+      for (int c = 0; c < NT; ++c) {
+        if (n0 + 16 * NT <= a.N) {
+          *reinterpret_cast<f32x4_by4*>(yp + 16 * c) = out[t][c];
+        } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (n + e < a.N) yp[n + e] += out[t][c][e];
+          for (int e = 0; e < 4; ++e)
+            if (n0 + 16 * c + 4 * g + e < a.N) yp[16 * c + e] = out[t][c][e];
+        }
       }
     }
+    if (!more) break;
+    n0 += COLS;
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+#pragma unroll
+      for (int c = 0; c < NT; ++c) out[t][c] = next[t][c];
   }
 }
 

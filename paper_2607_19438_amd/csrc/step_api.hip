@@ -144,24 +144,32 @@ int check_reorder(int R, int B, int W, int F, int Q, int page) {
 
 struct AdapterPlan {
   int mt_down, jt, splits, k_split, lists;
-  int mt_up, nt, s;
+  int mt_up, nt, s, chunks;
   long at_mid, bytes;
 };
 
 AdapterPlan adapter_plan(int M, int N, int K, int r) {
   AdapterPlan p{};
-  p.mt_down = M > 1024 ? 2 : 1;
+  // mid: K is split over workgroups while they are few (us for splits of 1, 2, 4: 16 rows, rank 16 6.7, 5.0, 4.1; 96 rows, rank
+  // 32 10.0, 7.5, 7.0; 1252 rows, rank 8 12.4, 8.7, 6.3; 8500, rank 64 27.4, 23.3, 20.0; K = 2048 each). The second kernel
+  // adds the parts up, each of its workgroups those of its rows: 0.3 us for each of 96 rows of 8192 columns, but 10 to 20 of
+  // 8500 rows at rank 64.
+  p.mt_down = M > 4096 ? 2 : 1;
   p.jt = r <= 16 ? 1 : r <= 32 ? 2 : 4;
-  const long tiles = qg::ceil_div(M, 16L * p.mt_down) * qg::ceil_div(r, 16L * p.jt);
-  p.lists = M <= 256 ? 16 : 1;
-  const long step = 32 * qg::kAdWaves;
-  p.splits = (int)std::max<long>(1, std::min<long>({8, 512 / tiles, K / (4 * step)}));
-  p.k_split = (int)(qg::ceil_div(qg::ceil_div(K, p.splits), step) * step);
+  p.lists = M <= 256 ? 16 : 1;           // a tile's adapters side by side where each row may have its own
+  const long tiles = qg::ceil_div(r, 16L * p.jt);
+  const long want = M <= 256 ? 256 / (M * tiles) : std::min(768 / (qg::ceil_div(M, 16L * p.mt_down) * tiles), 64L / r);
+  p.splits = (int)std::max<long>(1, std::min<long>({4, want, K / 256}));
+  p.k_split = (int)(qg::ceil_div(qg::ceil_div(K, p.splits), qg::kAdRun) * qg::kAdRun);
   p.splits = (int)qg::ceil_div(K, p.k_split);
-  p.mt_up = M > 1024 ? 4 : 1;
-  p.nt = M > 256 ? 4 : 1;
+  // y: of few rows 16 columns to a wave and eight adapters at once (96 rows with 64 adapters, 8192 columns: 10.2 us, with 64
+  // columns 14.7 and 11.7 for one and two at once; 64 rows with 32, 4096 columns 5.6, with two at once 6.4); of many tiles
+  // of 32 by 32, four of them to a wave in turn (8500 rows of 8192, rank 64: 1, 2, 4, 8 in turn 177, 139, 136, 152 us, 32 by
+  // 64 169, 136, 151, 167; 2048 rows, rank 16 33.7, 31.2, 32.0, 38.8).
+  p.mt_up = p.nt = M <= 256 ? 1 : 2;
+  p.chunks = M <= 256 ? 1 : 4;
+  while (p.chunks > 1 && qg::ceil_div(M, 32) * qg::ceil_div(N, 128L * p.chunks) < 384) p.chunks /= 2;
   p.s = r <= 32 ? 1 : r <= 64 ? 2 : 4;
-  if (p.s == 4) p.mt_up = std::min(p.mt_up, 2);
   p.at_mid = round16((long)M * (long)sizeof(int32_t));
   p.bytes = p.at_mid + (long)p.splits * M * r * (long)sizeof(float);
   return p;
@@ -411,36 +419,32 @@ int qgemm_adapters(const void* x, const void* a_w, const void* b_w, const int32_
   g.splits = plan.splits;
   g.k_split = plan.k_split;
   g.lists = plan.lists;
-  g.vec = aligned16(y) && y_stride % 4 == 0;
+  g.chunks = plan.chunks;
   const long down = qg::ceil_div(M, 16L * plan.mt_down) * plan.lists * plan.splits * qg::ceil_div(r, 16L * plan.jt);
-  const long up = qg::ceil_div(M, 16L * plan.mt_up) * qg::ceil_div(N, 16L * plan.nt * qg::kAdWaves);
+  const long up = qg::ceil_div(M, 16L * plan.mt_up) * qg::ceil_div(N, 16L * plan.nt * plan.chunks * qg::kAdWaves);
   if (!qg::grid_fits(down, qg::kAdThreads) || !qg::grid_fits(up, qg::kAdThreads)) return fail(QGEMM_EUNSUPPORTED, "too many workgroups");
   (void)hipGetLastError();
   auto launch = [&](auto kernel, long groups) { hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(qg::kAdThreads), 0, stream, g); };
   if (plan.mt_down == 1) {
-    if (plan.jt == 1) launch(qg::adapter_down_kernel<1, 1>, down);
-    else if (plan.jt == 2) launch(qg::adapter_down_kernel<1, 2>, down);
-    else launch(qg::adapter_down_kernel<1, 4>, down);
+    if (plan.jt == 1) launch(qg::adapter_down_kernel<1, 1, qg::kAdWaves>, down);
+    else if (plan.jt == 2) launch(qg::adapter_down_kernel<1, 2, qg::kAdWaves>, down);
+    else launch(qg::adapter_down_kernel<1, 4, qg::kAdWaves>, down);
   } else {
-    if (plan.jt == 1) launch(qg::adapter_down_kernel<2, 1>, down);
-    else if (plan.jt == 2) launch(qg::adapter_down_kernel<2, 2>, down);
-    else launch(qg::adapter_down_kernel<2, 4>, down);
+    if (plan.jt == 1) launch(qg::adapter_down_kernel<2, 1, qg::kAdWaves>, down);
+    else if (plan.jt == 2) launch(qg::adapter_down_kernel<2, 2, qg::kAdWaves>, down);
+    else launch(qg::adapter_down_kernel<2, 4, qg::kAdWaves>, down);
   }
   rc = check_launch("qgemm_adapters");
   if (rc != QGEMM_OK) return rc;
-  auto by_rank = [&](auto mt, auto nt) {
-    constexpr int MT = decltype(mt)::value, NT = decltype(nt)::value;
-    if (plan.s == 1) launch(qg::adapter_up_kernel<MT, NT, 1>, up);
-    else if (plan.s == 2) launch(qg::adapter_up_kernel<MT, NT, 2>, up);
-    else if constexpr (MT <= 2) launch(qg::adapter_up_kernel<MT, NT, 4>, up);
-  };
-  using one = std::integral_constant<int, 1>;
-  using two = std::integral_constant<int, 2>;
-  using four = std::integral_constant<int, 4>;
-  if (plan.nt == 1) by_rank(one{}, one{});
-  else if (plan.mt_up == 1) by_rank(one{}, four{});
-  else if (plan.mt_up == 2) by_rank(two{}, four{});
-  else by_rank(four{}, four{});
+  if (plan.nt == 1) {
+    if (plan.s == 1) launch(qg::adapter_up_kernel<1, 1, 1, 8>, up);
+    else if (plan.s == 2) launch(qg::adapter_up_kernel<1, 1, 2, 8>, up);
+    else launch(qg::adapter_up_kernel<1, 1, 4, 4>, up);
+  } else {
+    if (plan.s == 1) launch(qg::adapter_up_kernel<2, 2, 1, 1>, up);
+    else if (plan.s == 2) launch(qg::adapter_up_kernel<2, 2, 2, 1>, up);
+    else launch(qg::adapter_up_kernel<2, 2, 4, 1>, up);
+  }
   rc = check_launch("qgemm_adapters (up)");
   return rc == QGEMM_OK ? ok() : rc;
 }
