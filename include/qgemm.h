@@ -429,7 +429,7 @@ int qgemm_attention_kv4_workspace(int T, int R, int H, int Hkv, int D, int W, in
  * Rows behind the last request are left as they are. Keys of a page outside [0, pages) or past the table make the rows
  * that see them NaN, shared ones those of the whole group. groups or a cu_q that do not ascend leave o unspecified.
  * Results are the same on every call. workspace as there, of qgemm_attention_kv4_shared_workspace's bytes.
- * R and G <= 4096; else the limits of qgemm_attention_kv4, with the larger of R and G in the last.
+ * R and G <= 2048; else the limits of qgemm_attention_kv4, with the larger of R and G in the last.
  */
 int qgemm_attention_kv4_shared(const void* q, const void* cache, const int32_t* block_table,
                                const int32_t* kv_len, const int32_t* cu_q, const int32_t* groups,

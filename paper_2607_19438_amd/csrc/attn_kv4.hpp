@@ -191,11 +191,11 @@ struct Kv4WideLds {
 
 template <int D, typename Rq, typename Finish>
 __device__ __forceinline__ void kv4_wide(const Kv4Args& a, const Rq& rq, int r, int tile, int h, int a0, int a1, const Finish& fin,
-                                         const Kv4WideLds& lds) {
+                                         const Kv4WideLds& lds, int tid) {
   constexpr int BK = 64, DW = D / 32, KSTEPS = D / 16, DT = D / 32;
   uint16_t *const ks0 = lds.ks0, *const ks1 = lds.ks1, *const vt0 = lds.vt0, *const vt1 = lds.vt1;
   unsigned long long* const nans[2] = {lds.nans[0], lds.nans[1]};
-  const int tid = threadIdx.x, lane = tid & 63;
+  const int lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 31, hh = lane >> 5;
   const int G = a.H / a.Hkv;
@@ -441,8 +441,8 @@ template <int D>
 struct Kv4Lane {
   int tid, lane, wave, col, grp, G, page_mask;
   uint32_t page_bytes, k_off, v_off, ks_off, vs_off;
-  __device__ __forceinline__ explicit Kv4Lane(const Kv4Args& a) {
-    tid = threadIdx.x, lane = tid & 63;
+  __device__ __forceinline__ Kv4Lane(const Kv4Args& a, int t) {
+    tid = t, lane = tid & 63;
     wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     col = lane & 15, grp = lane >> 4;
     G = a.H / a.Hkv;
@@ -835,7 +835,7 @@ __device__ __forceinline__ void kv4_body(const Kv4Args& a) {
   bool first_segment = true;
   Kv4Head header{-1};
 
-  const Kv4Lane<D> places(a);
+  const Kv4Lane<D> places(a, tid);
   while (g < ge) {
     // the unit's share, its start's granules left out: with nothing but those it is left to the next workgroup
     const int v1 = (int)min((unsigned)(kKv4Start + rq.grans), (unsigned)gi + (ge - g));
@@ -844,7 +844,7 @@ __device__ __forceinline__ void kv4_body(const Kv4Args& a) {
       const bool whole = a0 == 0 && a1 == rq.grans;
       const Kv4Finish fin{whole, a.part + (size_t)(2 * w + (first_segment ? 0 : 1)) * kKv4PartFloats<D, NT>};
       if constexpr (NT == kKv4Wide) {
-        kv4_wide<D>(a, rq, r, tile, h, a0, a1, fin, Kv4WideLds{ks0, ks1, vt0, vt1, {nans[0], nans[1]}});
+        kv4_wide<D>(a, rq, r, tile, h, a0, a1, fin, Kv4WideLds{ks0, ks1, vt0, vt1, {nans[0], nans[1]}}, tid);
       } else {
         kv4_tile<D, NT>(a, rq, r, tile, h, a0, a1, fin, places, vbuf, ml);
       }

@@ -23,7 +23,9 @@
 namespace qg {
 namespace {
 
-constexpr int kSharedMaxR = 4096;          // requests (and groups, each of which takes 12 bytes of LDS)
+constexpr int kSharedMaxR = 2048;          // requests, and groups
+// int32 of LDS in which a workgroup looks them up: 72 KiB at most, beside the tiles' 66
+__host__ __device__ constexpr int shared_lds(int R, int Gn) { return 4 * R + 4 * Gn + Gn + 1; }
 constexpr int kSharedBlock = 64;           // shared keys come in blocks of so many
 
 struct SharedRow {          // where a request's rows have their results
@@ -89,7 +91,7 @@ struct SharedFinish {
   }
 };
 
-template <int D, bool WIDE, int NT>
+template <int D, int NT>
 struct SharedTileLds {
   uint16_t vbuf[kKv4Waves][32 * D];
   float ml[kKv4Waves][16 * NT][2];
@@ -112,7 +114,7 @@ template <int D, int NP, int NT>
 __global__ __launch_bounds__(kKv4Threads, (kKv4PerCU<D, (NP > NT ? NP : NT)>)) void kv4_shared_kernel(SharedArgs sa) {
   constexpr bool kAnyWide = NP == kKv4Wide || NT == kKv4Wide;
   constexpr int kMostTile = (NP == kKv4Wide ? 1 : NP) > (NT == kKv4Wide ? 1 : NT) ? (NP == kKv4Wide ? 1 : NP) : (NT == kKv4Wide ? 1 : NT);
-  using TileLds = SharedTileLds<D, false, kMostTile>;
+  using TileLds = SharedTileLds<D, kMostTile>;
   using WideLds = SharedWideLds<D>;
   constexpr size_t kLds = kAnyWide && sizeof(WideLds) > sizeof(TileLds) ? sizeof(WideLds) : sizeof(TileLds);
   __shared__ __attribute__((aligned(16))) char lds[kLds];
@@ -126,85 +128,78 @@ __global__ __launch_bounds__(kKv4Threads, (kKv4PerCU<D, (NP > NT ? NP : NT)>)) v
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int G = a.H / a.Hkv, R = a.R, Gn = sa.Gn;
-  int32_t* gstart = group_lds;               // [Gn + 1] first requests of the groups
-  int32_t* gkeys = group_lds + Gn + 1;       // [Gn] their shared keys
-  unsigned* gbase = reinterpret_cast<unsigned*>(gkeys + Gn);       // [Gn] first granules of their units
+  int4* const req = reinterpret_cast<int4*>(group_lds);        // [R] first row, rows, keys, group (-1: none)
+  int4* const grp = req + R;                                   // [Gn] first row, rows, shared keys, first granule of its units
+  int32_t* const gstart = reinterpret_cast<int32_t*>(grp + Gn);          // [Gn + 1] first requests of the groups
 
-  // ---- the groups' shared keys, and where the units are in the two sequences of granules
+  // ---- requests and groups, in one round of loads
   bool ascends = true;
   const int most_keys = a.W << a.page_log2;
-  for (int i = tid; i <= Gn; i += kKv4Threads) {
-    const int at = sa.groups[i];
-    gstart[i] = clamp_i(at, 0, R);
-    if (i < Gn) {
-      gkeys[i] = clamp_i(sa.prefix[i], 0, most_keys);
-      ascends = ascends && at <= sa.groups[i + 1];
-    }
-  }
-  __syncthreads();
-  auto rows_of = [&](int r, int& c0, int& n) {
-    c0 = a.cu ? clamp_i(a.cu[r], 0, a.T) : r;
-    n = a.cu ? clamp_i(a.cu[r + 1], c0, a.T) - c0 : 1;
-  };
-  // the last group that begins at or before request r; it is the request's if it ends behind r
-  auto group_of = [&](int r) {
-    int lo = 0, hi = Gn - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (gstart[mid] <= r) lo = mid;
-      else hi = mid - 1;
-    }
-    return lo;
-  };
-  auto in_group = [&](int g, int r) { return Gn > 0 && gstart[g] <= r && r < gstart[g + 1]; };
-  const int per = (R + kKv4Threads - 1) / kKv4Threads;
-  const int r0 = min(R, tid * per), r1 = min(R, r0 + per);
-  int g0 = Gn > 0 && r0 < R ? group_of(r0) : 0;
-  for (int r = r0, g = g0; r < r1; ++r) {
-    while (g + 1 < Gn && gstart[g + 1] <= r) ++g;
-    int c0, n;
-    rows_of(r, c0, n);
-    if (a.cu) ascends = ascends && a.cu[r] <= a.cu[r + 1];
-    if (n > 0 && in_group(g, r)) atomicMin(&gkeys[g], max(max(a.kv_len[r], 0) - n, 0));
+  for (int i = tid; i < max(R, Gn) + 1; i += kKv4Threads) {
+    const int r = min(i, R), g = min(i, Gn);
+    const int c = a.cu ? a.cu[r] : r, c1 = a.cu ? a.cu[min(i + 1, R)] : min(i + 1, R);
+    const int kv = a.kv_len[min(i, R - 1)];
+    const int at = sa.groups[g], at1 = sa.groups[min(i + 1, Gn)], keys = Gn > 0 ? sa.prefix[min(i, Gn - 1)] : 0;
+    ascends = ascends && c <= c1 && at <= at1;
+    const int c0 = clamp_i(c, 0, a.T);
+    if (i < R) req[i] = make_int4(c0, max(clamp_i(c1, 0, a.T) - c0, 0), max(kv, 0), -1);
+    if (i <= Gn) gstart[i] = clamp_i(at, 0, R);
+    if (i < Gn) grp[i].z = clamp_i(keys, 0, most_keys);
   }
   const bool good = !__syncthreads_or(!ascends);
-  auto shared_keys = [&](int g) { return gkeys[g] & -kSharedBlock; };
-  auto tail_unit = [&](int r, int g) {
+  // ---- the requests' groups, the groups' rows and shared keys
+  const int per = (R + kKv4Threads - 1) / kKv4Threads;
+  const int r0 = min(R, tid * per), r1 = min(R, r0 + per);
+  if (Gn > 0 && r0 < r1) {
+    int g = 0;
+    for (int hi = Gn - 1; g < hi;) {             // the last group that begins at or before the request
+      const int mid = (g + hi + 1) >> 1;
+      if (gstart[mid] <= r0) g = mid;
+      else hi = mid - 1;
+    }
+    for (int r = r0; r < r1; ++r) {
+      while (g + 1 < Gn && gstart[g + 1] <= r) ++g;
+      if (gstart[g] > r || r >= gstart[g + 1]) continue;
+      req[r].w = g;
+      if (req[r].y > 0) atomicMin(&grp[g].z, max(req[r].z - req[r].y, 0));
+    }
+  }
+  const int gper = (Gn + kKv4Threads - 1) / kKv4Threads;
+  const int p0 = min(Gn, tid * gper), p1 = min(Gn, p0 + gper);
+  for (int g = p0; g < p1; ++g) {
+    const int first = gstart[g], last = gstart[g + 1];
+    const int c0 = last > first ? req[first].x : 0;
+    grp[g].x = c0;
+    grp[g].y = last > first ? req[last - 1].x + req[last - 1].y - c0 : 0;
+  }
+  __syncthreads();
+  auto tail_unit = [&](int r) {
+    const int4 q = req[r];
     SharedUnit u;
-    rows_of(r, u.c0, u.n);
-    u.kv = max(a.kv_len[r], 0);
+    u.c0 = q.x;
+    u.n = q.y;
+    u.kv = q.z;
     u.len = (int)min((long)u.kv, (long)most_keys);
-    u.first = in_group(g, r) ? shared_keys(g) : 0;
-    u.first = min(u.first, u.len & -kSharedBlock);         // (a request of no rows may have fewer)
+    u.first = min(q.w >= 0 ? grp[max(q.w, 0)].z : 0, u.len) & -kSharedBlock;         // (a request of no rows may have fewer)
     u.pre = false;
     u.size<NT>(a, G);
     return u;
   };
   auto pre_unit = [&](int g) {
+    const int4 q = grp[g];
     SharedUnit u;
-    int c1, n1;
-    const int first = gstart[g], last = gstart[g + 1];
-    u.c0 = u.n = 0;
-    if (last > first) {
-      rows_of(first, u.c0, u.n);
-      rows_of(last - 1, c1, n1);
-      u.n = c1 + n1 - u.c0;
-    }
-    u.len = shared_keys(g);
-    u.kv = u.len;
+    u.c0 = q.x;
+    u.n = q.y;
+    u.len = u.kv = q.z & -kSharedBlock;
     u.first = 0;
     u.pre = true;
     u.size<NP>(a, G);
     return u;
   };
-  const int gper = (Gn + kKv4Threads - 1) / kKv4Threads;
-  const int p0 = min(Gn, tid * gper), p1 = min(Gn, p0 + gper);
+  // ---- where the units are in the two sequences of granules
   unsigned mine[2] = {0, 0};
   for (int g = p0; g < p1; ++g) mine[0] += pre_unit(g).weight(a.Hkv);
-  for (int r = r0, g = g0; r < r1; ++r) {
-    while (g + 1 < Gn && gstart[g + 1] <= r) ++g;
-    mine[1] += tail_unit(r, g).weight(a.Hkv);
-  }
+  for (int r = r0; r < r1; ++r) mine[1] += tail_unit(r).weight(a.Hkv);
   unsigned base[2], total[2];
 #pragma unroll
   for (int kind = 0; kind < 2; ++kind) {
@@ -247,8 +242,8 @@ __global__ __launch_bounds__(kKv4Threads, (kKv4PerCU<D, (NP > NT ? NP : NT)>)) v
   }
   // the kinds alternate over the launch
   const unsigned bid = blockIdx.x;
-  const unsigned pb = (unsigned)((unsigned long long)bid * np / (unsigned)a.nwg);
-  const unsigned pe = (unsigned)((unsigned long long)(bid + 1) * np / (unsigned)a.nwg);
+  const unsigned pb = bid * (unsigned)np / (unsigned)a.nwg;           // (at most 1024 workgroups)
+  const unsigned pe = (bid + 1) * (unsigned)np / (unsigned)a.nwg;
   const int kind = pe > pb ? 0 : 1;
   const unsigned w = kind == 0 ? pb : bid - pb;
   const unsigned ww = kind == 0 ? w : (unsigned)np + w;        // its place among all, and its slots'
@@ -261,18 +256,17 @@ __global__ __launch_bounds__(kKv4Threads, (kKv4PerCU<D, (NP > NT ? NP : NT)>)) v
     if (tid == 0) *sa.cut = {good && total[1] ? 1 : 0, np, {each[0], each[1]}, {more[0], more[1]}};
     unsigned at = base[0];
     for (int g = p0; g < p1; ++g) {
-      gbase[g] = at;
+      grp[g].w = (int)at;
       at += pre_unit(g).weight(a.Hkv);
     }
     __syncthreads();
     at = base[1];
-    for (int r = r0, g = g0; r < r1; ++r) {
-      while (g + 1 < Gn && gstart[g + 1] <= r) ++g;
-      const SharedUnit u = tail_unit(r, g);
+    for (int r = r0; r < r1; ++r) {
+      const SharedUnit u = tail_unit(r);
       SharedRow row{u.c0, u.n, u.first, at, (unsigned)u.grans, 0, 0, 0};
-      if (in_group(g, r)) {
+      if (const int g = req[r].w; g >= 0) {
         const SharedUnit p = pre_unit(g);
-        row.pre_c0 = p.c0, row.pre_base = gbase[g], row.pre_grans = p.weight(a.Hkv) ? (unsigned)p.grans : 0u;
+        row.pre_c0 = p.c0, row.pre_base = (unsigned)grp[g].w, row.pre_grans = p.weight(a.Hkv) ? (unsigned)p.grans : 0u;
       }
       sa.rows[r] = row;
       at += u.weight(a.Hkv);
@@ -282,23 +276,13 @@ __global__ __launch_bounds__(kKv4Threads, (kKv4PerCU<D, (NP > NT ? NP : NT)>)) v
   if (base[kind] <= gs && gs < base[kind] + mine[kind]) {
     unsigned off = gs - base[kind];
     int v = kind == 0 ? p0 : r0;
-    if (kind == 0) {
-      for (unsigned wt; off >= (wt = pre_unit(v).weight(a.Hkv)); ++v) off -= wt;
-    } else {
-      int g = g0;
-      for (;; ++v) {
-        while (g + 1 < Gn && gstart[g + 1] <= v) ++g;
-        const unsigned wt = tail_unit(v, g).weight(a.Hkv);
-        if (off < wt) break;
-        off -= wt;
-      }
-    }
+    if (kind == 0 ? p1 - p0 > 1 : r1 - r0 > 1)        // (one unit to a thread is that one)
+      for (unsigned wt; off >= (wt = kind == 0 ? pre_unit(v).weight(a.Hkv) : tail_unit(v).weight(a.Hkv)); ++v) off -= wt;
     where = {v, off};
   }
   __syncthreads();
   // ---- the workgroup's units
   int v = __builtin_amdgcn_readfirstlane(where.v);
-  int g = Gn > 0 ? (kind == 0 ? v : group_of(v)) : 0;
   auto uniform = [&](SharedUnit u) {
     u.c0 = __builtin_amdgcn_readfirstlane(u.c0), u.n = __builtin_amdgcn_readfirstlane(u.n);
     u.kv = __builtin_amdgcn_readfirstlane(u.kv), u.len = __builtin_amdgcn_readfirstlane(u.len);
@@ -307,15 +291,12 @@ __global__ __launch_bounds__(kKv4Threads, (kKv4PerCU<D, (NP > NT ? NP : NT)>)) v
     u.pre = kind == 0;
     return u;
   };
-  auto unit_at = [&]() { return uniform(kind == 0 ? pre_unit(v) : tail_unit(v, g)); };
+  auto unit_at = [&]() { return uniform(kind == 0 ? pre_unit(v) : tail_unit(v)); };
   // the request whose table a unit reads: of a group the first that has rows
   auto table_of = [&]() {
     if (kind == 1) return v;
     int r = gstart[v];
-    for (int c0, n; r + 1 < gstart[v + 1]; ++r) {
-      rows_of(r, c0, n);
-      if (n > 0) break;
-    }
+    while (r + 1 < gstart[v + 1] && req[r].y == 0) ++r;
     return __builtin_amdgcn_readfirstlane(r);
   };
   SharedUnit u = unit_at();
@@ -331,21 +312,23 @@ __global__ __launch_bounds__(kKv4Threads, (kKv4PerCU<D, (NP > NT ? NP : NT)>)) v
   const size_t nrows = (size_t)a.T * a.H;
   unsigned at = gs;
   bool first_segment = true;
-  const Kv4Lane<D> places(a);
   while (at < ge) {
     const int v1 = (int)min((unsigned)(kKv4Start + u.grans), (unsigned)gi + (ge - at));
     const int a0 = max(0, gi - kKv4Start), a1 = v1 - kKv4Start;
     if (a1 > a0) {
       const SharedFinish<D> fin{a0 == 0 && a1 == u.grans, a.part + (size_t)(2 * ww + (first_segment ? 0 : 1)) * sa.part_floats,
                                 sa.whole + kind * nrows * D, sa.whole_ml + kind * nrows * 2};
+      int t = tid;                           // opaque, so that what follows from it is computed for each unit anew and not
+      asm volatile("" : "+v"(t));           // held in registers, for both kinds of tiles, from the kernel's start
       auto tiles = [&](auto nt) {
         constexpr int N = decltype(nt)::value;
         if constexpr (N == kKv4Wide) {
           WideLds& wl = *reinterpret_cast<WideLds*>(lds);
-          kv4_wide<D>(a, u, r, tile, h, a0, a1, fin, Kv4WideLds{wl.tile[0], wl.tile[1], wl.tile[2], wl.tile[3], {wl.nans[0], wl.nans[1]}});
+          kv4_wide<D>(a, u, r, tile, h, a0, a1, fin, Kv4WideLds{wl.tile[0], wl.tile[1], wl.tile[2], wl.tile[3], {wl.nans[0], wl.nans[1]}}, t);
           __syncthreads();
         } else {
-          SharedTileLds<D, false, N>& tl = *reinterpret_cast<SharedTileLds<D, false, N>*>(lds);
+          const Kv4Lane<D> places(a, t);
+          SharedTileLds<D, N>& tl = *reinterpret_cast<SharedTileLds<D, N>*>(lds);
           kv4_tile<D, N>(a, u, r, tile, h, a0, a1, fin, places, tl.vbuf, tl.ml);
         }
       };
@@ -361,7 +344,6 @@ __global__ __launch_bounds__(kKv4Threads, (kKv4PerCU<D, (NP > NT ? NP : NT)>)) v
         tile = 0;
         do {
           ++v;
-          if (kind == 1) while (g + 1 < Gn && gstart[g + 1] <= v) ++g;
           u = unit_at();
         } while (u.weight(a.Hkv) == 0);       // (granules are left, so a unit with some is)
         r = table_of();
@@ -379,11 +361,10 @@ __global__ __launch_bounds__(64 * kSharedJoinRows) void kv4_shared_join_kernel(S
   constexpr int CH = D / 16;
   const Kv4Args& a = sa.k;
   const int lane = threadIdx.x & 63, ch = lane & 15, quarter = lane >> 4;
-  const long row = (long)blockIdx.x * kSharedJoinRows + (threadIdx.x >> 6);       // (token, head)
-  if (row >= (long)a.T * a.H) return;
+  const unsigned row = blockIdx.x * kSharedJoinRows + (unsigned)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);      // (token, head), below 2^31
+  if (row >= (unsigned)a.T * (unsigned)a.H) return;
   const SharedCut cut = *sa.cut;
-  if (!cut.ok) return;
-  const int G = a.H / a.Hkv, t = (int)(row / a.H), hq = (int)(row - (long)t * a.H), h = hq / G;
+  const int G = a.H / a.Hkv, t = (int)(row / (unsigned)a.H), hq = (int)(row - (unsigned)t * (unsigned)a.H), h = (int)((unsigned)hq / (unsigned)G);
   int r = t;
   if (a.cu) {                  // requests that end at or before the row: two looks of 64 entries each
     const int step = (a.R + 63) / 64;
@@ -395,41 +376,57 @@ __global__ __launch_bounds__(64 * kSharedJoinRows) void kv4_shared_join_kernel(S
     if (r >= a.R) return;
   }
   const SharedRow of = sa.rows[r];
+  if (!cut.ok) return;
   if (t < of.c0 || t >= of.c0 + of.n) return;
   float top = -__builtin_inff(), sum = 0.0f, out[CH] = {};
-  auto add = [&](float m, float l, const float* x) {
-    const float to = fmaxf(top, m);
-    const float was = part_weight(top, to, a.sl2), wt = part_weight(m, to, a.sl2);
-    sum = (top == -__builtin_inff() ? sum : was * sum) + (m == -__builtin_inff() ? l : wt * l);    // (NaN of an empty part stays)
+  constexpr int DEEP = 4;                 // parts whose loads are on their way at once
+  struct Part {
+    float m, l;
+    f32x4 x[CH / 4];
+  };
+  auto load = [&](const float* ml, const float* x) {
+    Part p;
+    const float2 v = *reinterpret_cast<const float2*>(ml);
+    p.m = v.x, p.l = v.y;
 #pragma unroll
-    for (int c = 0; c < CH / 4; ++c) {
-      const f32x4 y = *reinterpret_cast<const f32x4*>(x + ch * CH + 4 * c);
+    for (int c = 0; c < CH / 4; ++c) p.x[c] = *reinterpret_cast<const f32x4*>(x + ch * CH + 4 * c);
+    return p;
+  };
+  auto add = [&](const Part& p) {
+    const float to = fmaxf(top, p.m);
+    const float was = part_weight(top, to, a.sl2), wt = part_weight(p.m, to, a.sl2);
+    sum = (top == -__builtin_inff() ? sum : was * sum) + (p.m == -__builtin_inff() ? p.l : wt * p.l);    // (NaN of an empty part stays)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) out[4 * c + e] = out[4 * c + e] * was + wt * y[e];
-    }
+    for (int c = 0; c < CH / 4; ++c)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) out[4 * c + e] = out[4 * c + e] * was + wt * p.x[c][e];
     top = to;
   };
   auto parts = [&](int kind, int n16, unsigned base, unsigned grans, int c0) {
     if (grans == 0) return;
-    const int rho = (t - c0) * G + (hq - h * G), tile = rho / n16, lr = rho - tile * n16;
+    const int rho = (t - c0) * G + (hq - h * G), tile = (int)((unsigned)rho / (unsigned)n16), lr = rho - tile * n16;
     const unsigned unit = base + ((unsigned)tile * (unsigned)a.Hkv + (unsigned)h) * (kKv4Start + grans);
     const unsigned w0 = cut_owner(unit + kKv4Start, cut.each[kind], cut.more[kind]);
     const unsigned w1 = cut_owner(unit + kKv4Start + grans - 1, cut.each[kind], cut.more[kind]);
     if (w0 == w1) {
       const size_t at = (size_t)kind * a.T * a.H + row;
-      if (quarter == kind) {
-        const float2 ml = *reinterpret_cast<const float2*>(sa.whole_ml + 2 * at);
-        add(ml.x, ml.y, sa.whole + at * D);
-      }
+      if (quarter == kind) add(load(sa.whole_ml + 2 * at, sa.whole + at * D));
       return;
     }
     // in its first workgroup the unit is the second segment where one before it has granules there
     const unsigned second = cut_begin(w0, cut.each[kind], cut.more[kind]) < unit ? 1 : 0;
     const unsigned np = kind ? (unsigned)cut.np : 0u;
-    for (unsigned w = w0 + quarter; w <= w1; w += 4) {
-      const float* sl = a.part + (size_t)(2 * (np + w) + (w == w0 ? second : 0u)) * sa.part_floats;
-      const float2 ml = *reinterpret_cast<const float2*>(sl + 2 * lr);
-      add(ml.x, ml.y, sl + 2 * n16 + lr * D);
+    for (unsigned i0 = w0 + quarter; i0 <= w1; i0 += 4 * DEEP) {
+      Part p[DEEP];
+#pragma unroll
+      for (int k = 0; k < DEEP; ++k) {
+        const unsigned w = min(i0 + 4 * k, w1);
+        const float* sl = a.part + (size_t)(2 * (np + w) + (w == w0 ? second : 0u)) * sa.part_floats;
+        p[k] = load(sl + 2 * lr, sl + 2 * n16 + lr * D);
+      }
+#pragma unroll
+      for (int k = 0; k < DEEP; ++k)
+        if (i0 + 4 * k <= w1) add(p[k]);
     }
   };
   parts(0, 16 * NP, of.pre_base, of.pre_grans, of.pre_c0);

@@ -36,9 +36,17 @@ SharedPlan shared_plan(int T, int R, int Gn, int H, int Hkv, int D, int W, int p
   const long G = H / Hkv;
   const long rows = qg::ceil_div((long)T * G, R), group_rows = qg::ceil_div((long)T * G, std::max(Gn, 1));
   SharedPlan p{};
+  // Units over shared keys take pairs of 16-row tiles, and wide ones only for many rows: each part of a wide tile is 64 KiB,
+  // and a few tiles over long keys are cut into many parts. (us, pairs and wide: 64 requests behind 7919 keys, 32/8 heads of 128
+  // 34.3, 34.0; the same with D = 64 25.7, 27.0; 24 x 8 beams, 32/4 heads of 64 25.5, 29.3; 128 requests, 32/4 heads of 128 36.4,
+  // 39.0; 192 with 32/8 63.9, 58.8; 64 of 5 tokens 69.4, 59.4.)
+  const bool wide = group_rows >= 256 && (long)T * G / (16 * qg::kKv4Wide) * Hkv >= 40;
   p.nt = rows <= 16 ? 1 : rows >= 512 ? qg::kKv4Wide : 2;
-  p.np = p.nt == qg::kKv4Wide || group_rows >= 96 ? qg::kKv4Wide : group_rows <= 16 && p.nt == 1 ? 1 : 2;
-  p.cost = p.np == qg::kKv4Wide && p.nt != qg::kKv4Wide ? 64 : p.np > p.nt ? 24 : 16;
+  p.np = p.nt == qg::kKv4Wide || wide ? qg::kKv4Wide : group_rows <= 16 && p.nt == 1 ? 1 : 2;
+  // What a granule over shared keys takes longer: measured for pairs against single tiles with 16, 20, 24, 28: 24 x 8 beams 26.7,
+  // 25.8, 25.5, 25.8; 64 requests 36.6, 34.9, 34.6, 34.3; for wide against single ones with 24, 32, 48: 192 requests 62.6, 64.4,
+  // 58.8; wide against pairs: 64 of 5 tokens 61.9, 59.4, 62.2.
+  p.cost = p.np == p.nt ? 16 : p.np == 2 ? 24 : p.nt == 1 ? 48 : 32;
   const int most = std::max(p.np, p.nt);
   const long per_cu = most == qg::kKv4Wide ? 2 : (D == 128 ? 3 : 4) - (most - 1);
   const long fill = kCUs * per_cu;
@@ -72,7 +80,7 @@ int check_shared(int T, int R, int Gn, int H, int Hkv, int D, int W, int page) {
 
 template <int D, int NP, int NT>
 int launch_shared(const qg::SharedArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL((qg::kv4_shared_kernel<D, NP, NT>), dim3((unsigned)a.k.nwg), dim3(qg::kKv4Threads), (3 * (size_t)a.Gn + 1) * sizeof(int32_t), s, a);
+  hipLaunchKernelGGL((qg::kv4_shared_kernel<D, NP, NT>), dim3((unsigned)a.k.nwg), dim3(qg::kKv4Threads), (size_t)qg::shared_lds(a.k.R, a.Gn) * sizeof(int32_t), s, a);
   int rc = check_launch("qgemm_attention_kv4_shared");
   if (rc != QGEMM_OK) return rc;
   const long groups = qg::ceil_div((long)a.k.T * a.k.H, qg::kSharedJoinRows);

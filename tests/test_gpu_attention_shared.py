@@ -261,9 +261,9 @@ def test_many_requests_and_groups():
     own = [int(n) for n in rng.integers(1, 40, 700)]
     new = [int(min(n, m)) for n, m in zip(own, rng.integers(0, 3, 700))]
     check(torch, make(groups, [int(n) for n in rng.integers(0, 300, 300)], own, new, 2, 1, 64, 16, seed=18))
-    own = [1] * 4096
-    c = make([0, 4096], [70], own, [1] * 4096, 2, 1, 64, 16, seed=19)
-    check(torch, c, cu=False, rows={0, 1, 2047, 4095})
+    for groups, prefix in (([0, 2048], [70]), (list(range(2049)), [70] * 2048)):        # as many as there may be
+        c = make(groups, prefix, [1] * 2048, [1] * 2048, 2, 1, 64, 16, seed=19)
+        check(torch, c, cu=False, rows={0, 1, 1023, 2047})
 
 
 def test_tables_of_no_pages_and_no_requests():

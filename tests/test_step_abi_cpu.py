@@ -28,7 +28,7 @@ def test_attention_kv4_shared_refusals(m):
                {"scale": float("nan")}, {"qs": 255}, {"cu": 0}, {"bytes": 0}, {"q": 0}, {"cache": 0}, {"tab": 0}, {"kv": 0}, {"groups": 0}, {"prefix": 0},
                {"o": 0}, {"ws": 0}):
         assert call(**kw) == -1, kw
-    for kw in ({"D": 96}, {"R": 4097}, {"G": 4097}, {"W": 1 << 27}, {"T": 1 << 24, "H": 4, "D": 128}, {"T": 1 << 18, "H": 64, "Hkv": 64, "W": 1 << 20}):
+    for kw in ({"D": 96}, {"R": 2049}, {"G": 2049}, {"W": 1 << 27}, {"T": 1 << 24, "H": 4, "D": 128}, {"T": 1 << 18, "H": 64, "Hkv": 64, "W": 1 << 20}):
         assert call(**kw) == -3, kw
     for kw in ({"q": 24}, {"cache": 24}, {"o": 24}, {"ws": 24}, {"tab": 18}, {"kv": 18}, {"cu": 18}, {"groups": 18}, {"prefix": 18}, {"qs": 260}):
         assert call(**kw) == -2, kw
