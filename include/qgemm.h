@@ -444,7 +444,7 @@ int qgemm_attention_kv4_shared_workspace(int T, int R, int G, int H, int Hkv, in
  *   scores[r][b] + x[v] - log sum_u exp x[u],  x the row r*B + b of logits,
  * the K of largest value, in descending order, equal ones the lower beam first, of a beam the lower token:
  *   out_scores[r][k] its value, out_parents[r][k] = b, out_tokens[r][k] = v
- * A beam with finished[r][b] != 0 has one candidate, the token `end` at its own score; its logits are not read. No
+ * A beam with finished[r][b] != 0 has one candidate, the token `end` at its own score; its logits do not matter. No
  * candidates are those worth -inf or NaN: all of a beam whose score is (a beam that is not there: before the first
  * selection all but one of a prompt's), tokens of logit -inf, and all of a row that holds NaN or +inf. Behind the last
  * candidate stand score -inf, parent -1 and token `end`. So finished is (out_tokens == end) for the next selection.
@@ -474,7 +474,7 @@ int qgemm_beam_select_workspace(int R, int B, int V, int K, int64_t* bytes);
  * negative entries.
  * block_table, new_table: int32 [R*B][W]; kv_len (negative counts as 0), parents, new_len, src, dst: int32 [R*B];
  * free_pages: int32 [F]; keep: int32 [R]; used, n_released: int32 [1]; released: int32 [Q]. Nothing that is written may share
- * memory with another array: a loop keeps two tables that take turns. B <= 64, R*B <= 65536, R*B*W < 2^31.
+ * memory with another array: a loop keeps two tables that take turns. B <= 64, R*B <= 65536, R*B*W < 2^31. R == 0 is a no-op.
  * workspace: caller-owned, 4-byte aligned, of qgemm_kv_reorder_workspace's bytes, without initialisation.
  */
 int qgemm_kv_reorder(const int32_t* block_table, const int32_t* kv_len, const int32_t* parents,

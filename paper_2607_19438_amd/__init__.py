@@ -101,7 +101,9 @@ def lib():
         if way is not None and _header_of(handle) != way.header:
             way = _no_compiled_way("it was built from another header than the library")
         if way is not None:
-            names = ("kv_plan", "rope", "kv4_store", "kv4_load", "attention_packed", "attention_kv4", "attention_kv4_workspace")
+            names = ("kv_plan", "rope", "kv4_store", "kv4_load", "attention_packed", "attention_kv4", "attention_kv4_workspace",
+                     "attention_kv4_shared", "attention_kv4_shared_workspace", "beam_select", "beam_select_workspace", "kv_reorder",
+                     "kv_reorder_workspace", "kv4_copy", "adapters", "adapters_workspace")
             way.bind(_raw_stream, *[ctypes.cast(getattr(handle, "qgemm_" + n), ctypes.c_void_p).value for n in names])
         _lib = handle
         _fast = way
@@ -746,6 +748,10 @@ def attention_kv4_shared(q: torch.Tensor, cache: torch.Tensor, block_table: torc
 
     ``groups`` [G+1]: first requests of the groups; ``prefix_len`` [G]: keys that a group's requests have in common. The other
     arguments are ``attention_kv4``'s, and so are the results, up to the order of summation."""
+    if _fast is not None:
+        r = _fast.attention_kv4_shared(q, cache, block_table, kv_len, groups, prefix_len, cu_q, scale, out)
+        if r is not NotImplemented:
+            return r
     (T, H, D), qs = _need_rows(q, "q", _BF16)
     _need(block_table, "block_table", _I32, 2)
     _need(kv_len, "kv_len", _I32, 1)
@@ -790,6 +796,10 @@ def beam_select(logits: torch.Tensor, scores: torch.Tensor, count: int | None = 
     ``logits`` [R*B][V] fp32 or bf16, rows at any stride; ``scores`` [R][B] fp32, -inf for a beam that is not there;
     ``finished`` [R][B] bool or uint8: beams that go on with ``end`` at their own score. Where candidates are missing the score
     is -inf, the parent -1 and the token ``end``, so that ``tokens == end`` is the next call's ``finished``."""
+    if _fast is not None:
+        r = _fast.beam_select(logits, scores, count, finished, end)
+        if r is not NotImplemented:
+            return r
     _need(scores, "scores", (torch.float32,), 2)
     R, B = scores.shape
     if not isinstance(logits, torch.Tensor):
@@ -844,6 +854,12 @@ def kv_reorder(block_table: torch.Tensor, kv_len: torch.Tensor, parents: torch.T
     ``keep`` [R]: first columns whose pages are never listed as released; ``released``: length of that list (by default that
     of the table, which is enough for all). ``out``: an earlier result of the same sizes to write into, with no tensor
     of it among the inputs."""
+    if _fast is not None and out is None:
+        r = _fast.kv_reorder(block_table, kv_len, parents, free_pages, page, keep, released)
+        if r is not NotImplemented:
+            new = KvReorder.__new__(KvReorder)
+            new.block_table, new.kv_len, new.src, new.dst, new.used, new.released, new.n_released = r
+            return new
     _need(block_table, "block_table", _I32, 2)
     _need(kv_len, "kv_len", _I32, 1)
     _need(parents, "parents", _I32, 2)
@@ -878,12 +894,18 @@ def kv_reorder(block_table: torch.Tensor, kv_len: torch.Tensor, parents: torch.T
              None if keep is None else keep.data_ptr(), out.block_table.data_ptr(), out.kv_len.data_ptr(), out.src.data_ptr(),
              out.dst.data_ptr(), out.used.data_ptr(), out.released.data_ptr(), out.n_released.data_ptr(), ws.data_ptr(), need, R, B, W,
              free_pages.shape[0], Q, page)
+    if rows == 0:             # the library leaves a reordering of nothing alone
+        out.used.zero_()
+        out.n_released.zero_()
+        out.released.fill_(-1)
     return out
 
 
 def kv4_copy(cache: torch.Tensor, src: torch.Tensor, dst: torch.Tensor, D: int | None = None):
     """Whole pages within a cache, page ``src[i]`` to page ``dst[i]`` (``qgemm_kv4_copy``); negative numbers are skipped.
     A page's bytes are copied as they are, so the head dimension ``D`` need not be given."""
+    if _fast is not None and _fast.kv4_copy(cache, src, dst, D) is None:
+        return
     _need(cache, "cache", (torch.uint8,), 3)
     _need(src, "src", _I32, 1)
     _need(dst, "dst", _I32, 1)
@@ -906,6 +928,10 @@ def adapters(y: torch.Tensor, x: torch.Tensor, a: torch.Tensor, b: torch.Tensor,
     ``y`` [M][N] fp32 and ``x`` [M][K] bf16, rows at any stride (``x``'s a multiple of 8); ``a`` [n][r][K], ``b`` [n][N][r] bf16;
     ``gain`` [n] fp32; ``cu_q`` [R+1]: first rows of the requests, or None where each has one. Rows of an id outside [0, n)
     are left as they are."""
+    if _fast is not None:
+        done = _fast.adapters(y, x, a, b, ids, gain, cu_q)
+        if done is not NotImplemented:
+            return done
     for t, name, dtypes in ((y, "y", (torch.float32,)), (x, "x", _BF16)):
         if not isinstance(t, torch.Tensor):
             raise TypeError(f"{name} must be a torch.Tensor")

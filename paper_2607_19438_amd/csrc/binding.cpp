@@ -3,7 +3,8 @@
 // else a function here answers NotImplemented, having done nothing, and the Python function goes its own way, which
 // says what is wrong. A decode step's calls take less time on the GPU than their checks take in Python: host time
 // of a call of 16 rows (us, Python alone and with this file) rope 8.5, 4.4; plan 10.2, 5.1; store and load 16.5, 8.9;
-// packed prompts 9.0, 4.7; attention over the cache 10.5, 5.4; a launch is 2.4 of it, an allocation 0.6.
+// packed prompts 9.0, 4.7; attention over the cache 10.5, 5.4; over shared prefixes 14.3, 8.6; selection of beams 15.1, 7.6;
+// table reordering 16.5, 10.0 and page copies 6.7, 3.3; adapters 12.0, 7.4; a launch is 2.4 of it, an allocation 0.6.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
@@ -26,6 +27,15 @@ struct {
   decltype(&qgemm_attention_packed) packed;
   decltype(&qgemm_attention_kv4) kv4;
   decltype(&qgemm_attention_kv4_workspace) kv4_workspace;
+  decltype(&qgemm_attention_kv4_shared) shared;
+  decltype(&qgemm_attention_kv4_shared_workspace) shared_workspace;
+  decltype(&qgemm_beam_select) beam;
+  decltype(&qgemm_beam_select_workspace) beam_workspace;
+  decltype(&qgemm_kv_reorder) reorder;
+  decltype(&qgemm_kv_reorder_workspace) reorder_workspace;
+  decltype(&qgemm_kv4_copy) copy;
+  decltype(&qgemm_adapters) adapters;
+  decltype(&qgemm_adapters_workspace) adapters_workspace;
   PyObject* raw_stream;
 } lib = {};
 
@@ -123,6 +133,31 @@ at::Tensor piece(const at::Tensor& t, int64_t at, int64_t n) {
   return p;
 }
 
+// rows of n elements of a dense int32 tensor from `at` on, as a tensor of their own, int32 or fp32
+at::Tensor piece(const at::Tensor& t, int64_t at, int64_t rows, int64_t n, at::ScalarType type = at::kInt) {
+  at::Tensor p = at::detail::make_tensor<c10::TensorImpl>(c10::TensorImpl::VIEW, c10::Storage(t.storage()), t.key_set(),
+                                                          at::scalarTypeToTypeMeta(type));
+  p.unsafeGetTensorImpl()->set_storage_offset(at);
+  p.unsafeGetTensorImpl()->set_sizes_contiguous({rows, n});
+  return p;
+}
+
+template <size_t N>
+PyObject* tuple(const at::Tensor (&out)[N]) {
+  PyObject* r = PyTuple_New(N);
+  for (size_t i = 0; r && i < N; ++i) PyTuple_SET_ITEM(r, i, THPVariable_Wrap(out[i]));
+  return r;
+}
+
+// [rows][n] with the elements of a row end to end; the elements between rows
+bool matrix(const at::Tensor* t, int64_t* stride) {
+  if (!t || !t->is_cuda() || t->dim() != 2) return false;
+  const int64_t m = t->size(0), n = t->size(1);
+  if (m > 0 && n > 1 && t->stride(1) != 1) return false;
+  *stride = m > 1 ? t->stride(0) : n;
+  return true;
+}
+
 // (kv_len, q_len, block_table, free_pages, page, tokens) -> (cu_q, kv_len, used, positions, slots)
 PyObject* kv_plan_(PyObject* const* a) {
   const at::Tensor *kv = tensor(a[0]), *ql = tensor(a[1]), *tab = tensor(a[2]), *fr = tensor(a[3]);
@@ -143,9 +178,7 @@ PyObject* kv_plan_(PyObject* const* a) {
     return not_here();
   const at::Tensor out[5] = {piece(buf, 0, R + 1), piece(buf, R + 1, R), piece(buf, 2 * R + 1, 1), piece(buf, 2 * R + 2, T),
                              piece(buf, 2 * R + 2 + T, T)};
-  PyObject* r = PyTuple_New(5);
-  for (int i = 0; r && i < 5; ++i) PyTuple_SET_ITEM(r, i, THPVariable_Wrap(out[i]));
-  return r;
+  return tuple(out);
 }
 
 // (x, positions, inv_freq, rot_heads, interleaved, gain, out)
@@ -276,6 +309,147 @@ PyObject* attention_kv4_(PyObject* const* a) {
   return o ? Py_NewRef(a[6]) : THPVariable_Wrap(made);
 }
 
+// (q, cache, block_table, kv_len, groups, prefix_len, cu_q, scale, out)
+PyObject* attention_kv4_shared_(PyObject* const* a) {
+  const at::Tensor *q = tensor(a[0]), *c = tensor(a[1]), *tab = tensor(a[2]), *kv = tensor(a[3]), *gr = tensor(a[4]), *pre = tensor(a[5]);
+  const at::Tensor *cu = a[6] == Py_None ? nullptr : tensor(a[6]), *o = a[8] == Py_None ? nullptr : tensor(a[8]);
+  int64_t qs;
+  int pages, Hkv, page;
+  float scale;
+  hipStream_t s;
+  if (!lib.shared || !lib.shared_workspace || !rows(q, &qs) || q->scalar_type() != at::kBFloat16 || !dense(tab, at::kInt, 2) ||
+      !dense(kv, at::kInt, 1) || !dense(gr, at::kInt, 1) || !dense(pre, at::kInt, 1) || (a[6] != Py_None && !cu) || (a[8] != Py_None && !o))
+    return not_here();
+  const int64_t T = q->size(0), H = q->size(1), D = q->size(2), R = tab->size(0), W = tab->size(1), G = pre->size(0);
+  if (!cache_sizes(c, D, &pages, &Hkv, &page) || kv->size(0) != R || gr->size(0) != G + 1 ||
+      (cu ? !dense(cu, at::kInt, 1) || cu->size(0) != R + 1 : T != R) || !small({T, H, R, W, G}) || !to_scale(a[7], D, &scale) ||
+      !stream_of({q, c, tab, kv, gr, pre, cu, o}, &s))
+    return not_here();
+  if (o && (!dense(o, at::kBFloat16, 3) || o->sizes() != q->sizes())) return not_here();
+  int64_t need = 0;
+  if (lib.shared_workspace((int)T, (int)R, (int)G, (int)H, Hkv, (int)D, (int)W, page, &need) != 0) return not_here();
+  at::Tensor made;
+  if (!o) made = at::empty({T, H, D}, q->options());
+  const at::Tensor ws = at::empty({need}, q->options().dtype(at::kByte));
+  void *y = memory(o ? o : &made), *qp = memory(q), *cp = memory(c), *wp = memory(&ws);
+  const int32_t *tp = memory<int32_t>(tab), *kp = memory<int32_t>(kv), *up = memory<int32_t>(cu), *gp = memory<int32_t>(gr),
+                *pp = memory<int32_t>(pre);
+  if (call([&] {
+        return lib.shared(qp, cp, tp, kp, up, gp, pp, y, wp, need, (int)T, (int)R, (int)G, (int)H, Hkv, (int)D, (int)W, pages, page, qs,
+                          scale, s);
+      }) != 0)
+    return not_here();
+  return o ? Py_NewRef(a[8]) : THPVariable_Wrap(made);
+}
+
+// (logits, scores, count, finished, end) -> (scores, parents, tokens)
+PyObject* beam_select_(PyObject* const* a) {
+  const at::Tensor *x = tensor(a[0]), *sc = tensor(a[1]), *fin = a[3] == Py_None ? nullptr : tensor(a[3]);
+  int64_t xs;
+  int K, end;
+  hipStream_t s;
+  if (!lib.beam || !lib.beam_workspace || !matrix(x, &xs) || (x->scalar_type() != at::kFloat && x->scalar_type() != at::kBFloat16) ||
+      !dense(sc, at::kFloat, 2) || (a[3] != Py_None && !fin) || !to_int(a[4], &end))
+    return not_here();
+  const int64_t R = sc->size(0), B = sc->size(1), V = x->size(1);
+  if (x->size(0) != R * B || !small({R, B, R * B, V}) || (fin && !dense(fin, at::kBool, 2) && !dense(fin, at::kByte, 2)) ||
+      (fin && fin->sizes() != sc->sizes()) || (a[2] == Py_None ? (K = (int)B, false) : !to_int(a[2], &K)) || !stream_of({x, sc, fin}, &s))
+    return not_here();
+  int64_t need = 0;
+  if (lib.beam_workspace((int)R, (int)B, (int)V, K, &need) != 0) return not_here();
+  const int64_t n = R * K, at = need / 4;
+  const at::Tensor buf = at::empty({at + 3 * n}, sc->options().dtype(at::kInt));
+  int32_t* p = memory<int32_t>(&buf);
+  void *xp = memory(x), *fp = memory(fin);
+  const float* sp = memory<float>(sc);
+  const int type = x->scalar_type() == at::kBFloat16 ? QGEMM_BF16 : QGEMM_F32;
+  if (call([&] {
+        return lib.beam(xp, type, sp, static_cast<const uint8_t*>(fp), reinterpret_cast<float*>(p + at), p + at + n, p + at + 2 * n, p, need,
+                        (int)R, (int)B, (int)V, K, xs, end, s);
+      }) != 0)
+    return not_here();
+  const at::Tensor out[3] = {piece(buf, at, R, K, at::kFloat), piece(buf, at + n, R, K), piece(buf, at + 2 * n, R, K)};
+  return tuple(out);
+}
+
+// (block_table, kv_len, parents, free_pages, page, keep, released)
+// -> (block_table, kv_len, src, dst, used, released, n_released)
+PyObject* kv_reorder_(PyObject* const* a) {
+  const at::Tensor *tab = tensor(a[0]), *kv = tensor(a[1]), *of = tensor(a[2]), *fr = tensor(a[3]), *keep = a[5] == Py_None ? nullptr : tensor(a[5]);
+  int page, Q;
+  hipStream_t s;
+  if (!lib.reorder || !lib.reorder_workspace || !dense(tab, at::kInt, 2) || !dense(kv, at::kInt, 1) || !dense(of, at::kInt, 2) ||
+      !dense(fr, at::kInt, 1) || !to_int(a[4], &page) || (a[5] != Py_None && !dense(keep, at::kInt, 1)))
+    return not_here();
+  const int64_t rows = tab->size(0), W = tab->size(1), R = of->size(0), B = of->size(1), F = fr->size(0);
+  if (rows == 0 || R * B != rows || kv->size(0) != rows || !small({rows, W, F, rows * W}) || (keep && keep->size(0) != R) ||
+      (a[6] == Py_None ? (Q = (int)(rows * W), false) : !to_int(a[6], &Q)) || Q < 0 || !stream_of({tab, kv, of, fr, keep}, &s))
+    return not_here();
+  int64_t need = 0;
+  if (lib.reorder_workspace((int)R, (int)B, (int)W, &need) != 0) return not_here();
+  const int64_t n = rows * W, len = n, src = len + rows, dst = src + rows, gone = dst + rows, used = gone + Q, all = used + 2;
+  const at::Tensor buf = at::empty({all}, tab->options()), ws = at::empty({need}, tab->options().dtype(at::kByte));
+  int32_t *p = memory<int32_t>(&buf), *tp = memory<int32_t>(tab), *kp = memory<int32_t>(kv), *op = memory<int32_t>(of),
+          *fp = memory<int32_t>(fr), *ep = memory<int32_t>(keep);
+  void* wp = memory(&ws);
+  if (call([&] {
+        return lib.reorder(tp, kp, op, fp, ep, p, p + len, p + src, p + dst, p + used, p + gone, p + used + 1, wp, need, (int)R, (int)B, (int)W,
+                           (int)F, Q, page, s);
+      }) != 0)
+    return not_here();
+  const at::Tensor out[7] = {piece(buf, 0, rows, W),   piece(buf, len, rows), piece(buf, src, rows),    piece(buf, dst, rows),
+                             piece(buf, used, 1), piece(buf, gone, Q),   piece(buf, used + 1, 1)};
+  return tuple(out);
+}
+
+// (cache, src, dst, D)
+PyObject* kv4_copy_(PyObject* const* a) {
+  const at::Tensor *c = tensor(a[0]), *src = tensor(a[1]), *dst = tensor(a[2]);
+  int D = 128, pages, Hkv, page;
+  hipStream_t s;
+  if (!lib.copy || !dense(src, at::kInt, 1) || !dense(dst, at::kInt, 1) || src->sizes() != dst->sizes() || !small({src->size(0)})) return not_here();
+  if (a[3] != Py_None) {
+    if (!to_int(a[3], &D) || !cache_sizes(c, D, &pages, &Hkv, &page)) return not_here();
+  } else if (!cache_sizes(c, D, &pages, &Hkv, &page) || page < 16) {       // (a record of either dimension has the same bytes)
+    D = 64;
+    if (!cache_sizes(c, D, &pages, &Hkv, &page)) return not_here();
+  }
+  if (!stream_of({c, src, dst}, &s)) return not_here();
+  void* cp = memory(c);
+  const int32_t *sp = memory<int32_t>(src), *dp = memory<int32_t>(dst);
+  const int n = (int)src->size(0);
+  if (call([&] { return lib.copy(cp, sp, dp, n, Hkv, D, pages, page, s); }) != 0) return not_here();
+  Py_RETURN_NONE;
+}
+
+// (y, x, a, b, ids, gain, cu_q) -> y
+PyObject* adapters_(PyObject* const* args) {
+  const at::Tensor *y = tensor(args[0]), *x = tensor(args[1]), *a = tensor(args[2]), *b = tensor(args[3]), *ids = tensor(args[4]);
+  const at::Tensor *gain = args[5] == Py_None ? nullptr : tensor(args[5]), *cu = args[6] == Py_None ? nullptr : tensor(args[6]);
+  int64_t xs, ys;
+  hipStream_t s;
+  if (!lib.adapters || !lib.adapters_workspace || !matrix(y, &ys) || !matrix(x, &xs) || y->scalar_type() != at::kFloat ||
+      x->scalar_type() != at::kBFloat16 || !dense(a, at::kBFloat16, 3) || !dense(b, at::kBFloat16, 3) || !dense(ids, at::kInt, 1) ||
+      (args[5] != Py_None && !dense(gain, at::kFloat, 1)) || (args[6] != Py_None && !dense(cu, at::kInt, 1)))
+    return not_here();
+  const int64_t M = x->size(0), K = x->size(1), n = a->size(0), r = a->size(1), N = y->size(1), R = ids->size(0);
+  if (y->size(0) != M || a->size(2) != K || b->size(0) != n || b->size(1) != N || b->size(2) != r || !small({M, N, K, r, n, R}) ||
+      (gain && gain->size(0) != n) || (cu ? cu->size(0) != R + 1 : M != R) || !stream_of({y, x, a, b, ids, gain, cu}, &s))
+    return not_here();
+  int64_t need = 0;
+  if (lib.adapters_workspace((int)M, (int)N, (int)K, (int)r, &need) != 0) return not_here();
+  const at::Tensor ws = at::empty({need}, x->options().dtype(at::kByte));
+  void *xp = memory(x), *ap = memory(a), *bp = memory(b), *wp = memory(&ws);
+  const int32_t *ip = memory<int32_t>(ids), *cp = memory<int32_t>(cu);
+  const float* gp = memory<float>(gain);
+  float* yp = memory<float>(y);
+  if (call([&] {
+        return lib.adapters(xp, ap, bp, ip, cp, gp, yp, wp, need, (int)M, (int)N, (int)K, (int)r, (int)n, (int)R, xs, ys, s);
+      }) != 0)
+    return not_here();
+  return Py_NewRef(args[0]);
+}
+
 // C++ exceptions (an allocation that fails, a tensor without memory) end here: Python's way meets and reports them.
 template <PyObject* (*F)(PyObject* const*), Py_ssize_t N>
 PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
@@ -287,11 +461,15 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
   }
 }
 
-// (raw_stream, kv_plan, rope, store, load, packed, kv4, kv4_workspace): a callable and addresses
+// (raw_stream, kv_plan, rope, store, load, packed, kv4, kv4_workspace[, shared, shared_workspace, beam, beam_workspace,
+// reorder, reorder_workspace, copy, adapters, adapters_workspace]): a callable and addresses; functions that are not
+// given answer NotImplemented
 PyObject* bind(PyObject*, PyObject* args) {
   PyObject* stream;
-  unsigned long long p[7];
-  if (!PyArg_ParseTuple(args, "OKKKKKKK", &stream, p, p + 1, p + 2, p + 3, p + 4, p + 5, p + 6)) return nullptr;
+  unsigned long long p[16] = {};
+  if (!PyArg_ParseTuple(args, "OKKKKKKK|KKKKKKKKK", &stream, p, p + 1, p + 2, p + 3, p + 4, p + 5, p + 6, p + 7, p + 8, p + 9, p + 10, p + 11,
+                        p + 12, p + 13, p + 14, p + 15))
+    return nullptr;
   auto at = [&](int i, auto*& f) { f = reinterpret_cast<std::remove_reference_t<decltype(f)>>((uintptr_t)p[i]); };
   at(0, lib.kv_plan);
   at(1, lib.rope);
@@ -300,6 +478,15 @@ PyObject* bind(PyObject*, PyObject* args) {
   at(4, lib.packed);
   at(5, lib.kv4);
   at(6, lib.kv4_workspace);
+  at(7, lib.shared);
+  at(8, lib.shared_workspace);
+  at(9, lib.beam);
+  at(10, lib.beam_workspace);
+  at(11, lib.reorder);
+  at(12, lib.reorder_workspace);
+  at(13, lib.copy);
+  at(14, lib.adapters);
+  at(15, lib.adapters_workspace);
   Py_INCREF(stream);
   Py_XSETREF(lib.raw_stream, stream);
   Py_RETURN_NONE;
@@ -318,6 +505,11 @@ PyMethodDef methods[] = {
     {"kv4_load", fast<kv4_load_, 3>(), METH_FASTCALL, nullptr},
     {"attention_packed", fast<attention_packed_, 6>(), METH_FASTCALL, nullptr},
     {"attention_kv4", fast<attention_kv4_, 7>(), METH_FASTCALL, nullptr},
+    {"attention_kv4_shared", fast<attention_kv4_shared_, 9>(), METH_FASTCALL, nullptr},
+    {"beam_select", fast<beam_select_, 5>(), METH_FASTCALL, nullptr},
+    {"kv_reorder", fast<kv_reorder_, 7>(), METH_FASTCALL, nullptr},
+    {"kv4_copy", fast<kv4_copy_, 4>(), METH_FASTCALL, nullptr},
+    {"adapters", fast<adapters_, 7>(), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
