@@ -5,6 +5,10 @@
 // through the list: the products of all rows of the tile with one adapter are one MFMA operand's columns, and each row
 // keeps its own adapter's. A prompt's tile has one or two adapters; a decode step's has one a row, whose weights have to
 // be read once anyway, and the matrix cores that compute 16 columns for one have nothing else to do.
+// Bounds: of many rows HBM, which y passes twice (8500 rows of 8192 columns, rank 64, K = 2048: 26 us for the first
+// kernel, 120 for the second, 4.7 TB/s; reading and writing y alone by the same tiles 101); of a decode step the two launches
+// and their chains of loads (16 rows of 2048 columns 8.5 us), then the adapters' weights (96 rows with 64 adapters of 8192
+// columns, 38 MB, 15.9 us).
 // A row is chosen, never multiplied by zero: an infinity or NaN of one adapter or request reaches no other.
 #pragma once
 
@@ -38,21 +42,32 @@ struct AdapterArgs {
   int chunks;              // of the columns of a workgroup
 };
 
-// The adapter of row m: the last request that begins at or before it, if it has a row there.
+// The adapter of row m, -1 for none: that of the last request that begins at or before the row. All lanes of a wave take
+// part: each loads an edge of 64 parts of the requests, so that up to 64 of them take one load, and a part's search the rest.
 __device__ __forceinline__ int adapter_of(const AdapterArgs& a, int m) {
-  if (m >= a.M) return -1;
-  int r = m;
-  if (a.cu) {
-    int lo = 0, hi = a.R;                  // the first entry of cu[1 ..] above m
-    while (lo < hi) {
-      const int mid = (lo + hi) >> 1;
-      if (a.cu[mid + 1] > m) hi = mid;
-      else lo = mid + 1;
+  int id = -1;
+  if (!a.cu) {
+    if (m < a.M) id = a.ids[m];
+  } else {
+    const int lane = threadIdx.x & 63, step = (a.R + 63) / 64;
+    const int edge = a.cu[min((lane + 1) * step, a.R)], start = a.cu[0];
+    const int ids = a.ids[min(lane, a.R - 1)];
+    int b = 0;                             // parts that end at or before m
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) b += __shfl(edge, b + d - 1) <= m ? d : 0;
+    b += __shfl(edge, b) <= m ? 1 : 0;
+    int r = b * step;
+    id = __shfl(ids, min(r, 63));
+    if (step > 1) {
+      for (int hi = min(r + step, a.R); r < hi;) {       // its first request that ends behind m
+        const int mid = (r + hi) >> 1;
+        if (a.cu[mid + 1] > m) hi = mid;
+        else r = mid + 1;
+      }
+      if (r < a.R) id = a.ids[r];
     }
-    r = lo;
-    if (r >= a.R || a.cu[r] > m) return -1;
+    if (m < start || m >= a.M || r >= a.R) id = -1;
   }
-  const int id = a.ids[r];
   return (unsigned)id < (unsigned)a.n ? id : -1;
 }
 
@@ -85,9 +100,12 @@ __global__ __launch_bounds__(64 * WAVES) void adapter_down_kernel(AdapterArgs a)
   w /= jb;
   const int split = w % a.splits;
   w /= a.splits;
-  const int lane_of_list = w % a.lists;
-  const int m0 = w / a.lists * ROWS;
-  const int own = lane < ROWS ? adapter_of(a, m0 + lane) : -1;
+  // (a tile's later lists, many of them empty, come last: next to each other they would leave most XCDs nothing else)
+  const int tiles = (a.M + ROWS - 1) / ROWS;
+  const int lane_of_list = w / tiles;
+  const int m0 = (w - lane_of_list * tiles) * ROWS;
+  const int looked = adapter_of(a, m0 + lane);
+  const int own = lane < ROWS ? looked : -1;
   if (tid < ROWS && m0 + tid < a.M && split == 0 && lane_of_list == 0 && j0 == 0) a.row_id[m0 + tid] = own;
   const int k_begin = split * a.k_split, k_end = min(a.K, k_begin + a.k_split);
   const uint16_t* xp[MT];
@@ -171,7 +189,7 @@ __device__ __forceinline__ void split_bf16(float x, uint32_t (&p)[3]) {
 
 // y[m][c] += sum_j b[id][c][j] mid[m][j]. A wave takes 16 MT rows and `chunks` times 16 NT columns, the next of which are on
 // their way while it computes; its rows' mid stays in registers. S: runs of 32 of the rank. U: adapters whose weights
-// are loaded at once.
+// are loaded at once; more than one only where `chunks` is 1.
 template <int MT, int NT, int S, int U>
 __global__ __launch_bounds__(kAdThreads) void adapter_up_kernel(AdapterArgs a) {
   constexpr int ROWS = 16 * MT, COLS = 16 * NT * kAdWaves;
@@ -181,7 +199,6 @@ __global__ __launch_bounds__(kAdThreads) void adapter_up_kernel(AdapterArgs a) {
   const int m0 = (int)blockIdx.x / nb * ROWS;
   int n0 = (int)blockIdx.x % nb * a.chunks * COLS + wave * 16 * NT;
   const int n_end = min(a.N, ((int)blockIdx.x % nb + 1) * a.chunks * COLS);
-  if (n0 >= n_end) return;
   const int own = lane < ROWS && m0 + lane < a.M ? a.row_id[m0 + lane] : -1;
   auto load = [&](int at, f32x4 (&y)[MT][NT]) {
 #pragma unroll
@@ -198,79 +215,117 @@ __global__ __launch_bounds__(kAdThreads) void adapter_up_kernel(AdapterArgs a) {
       }
     }
   };
+  // the weights of adapters id[] for the columns from `at` on
+  auto weights = [&](int at, const int (&id)[U], u32x4 (&bf)[U][NT][S]) {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int c = 0; c < NT; ++c) {
+        const uint16_t* bp = a.b + ((size_t)id[u] * a.N + min(at + 16 * c + col, a.N - 1)) * a.r;
+#pragma unroll
+        for (int k = 0; k < S; ++k) bf[u][c][k] = *reinterpret_cast<const u32x4*>(bp + min(32 * k + 8 * g, a.r - 8));
+      }
+  };
+  auto take = [](AdapterList& list, int (&id)[U]) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) id[u] = u == 0 || list.left ? list.next() : id[0];       // (one of them again changes nothing)
+  };
   f32x4 out[MT][NT];
   load(n0, out);
-  const AdapterList all(own);
-  if (!all.left) return;
+  AdapterList rest(own);
+  if (!rest.left) return;
+  int first[U];
+  take(rest, first);
+  u32x4 bf[U][NT][S];
+  weights(n0, first, bf);
   int mine[MT];
-  bf16x8 mid[MT][S][3];
 #pragma unroll
-  for (int t = 0; t < MT; ++t) {
-    const int m = m0 + 16 * t + col;
-    mine[t] = __shfl(own, 16 * t + col);
+  for (int t = 0; t < MT; ++t) mine[t] = __shfl(own, 16 * t + col);
+  // mid of 16 rows and a run of the rank as matrix operands
+  auto operands = [&](int t, int k, int of, u32x4 (&w)[3]) {
+    const int m = m0 + 16 * t + col, j = 32 * k + 8 * g;
+    float v[8] = {};
+    if (of >= 0 && j < a.r) {
+      for (int p = 0; p < a.splits; ++p) {
+        const float* mp = a.mid + ((size_t)p * a.M + m) * a.r + j;
+        const f32x4 v0 = *reinterpret_cast<const f32x4*>(mp), v1 = *reinterpret_cast<const f32x4*>(mp + 4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] += v0[e], v[4 + e] += v1[e];
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      uint32_t p0[3], p1[3];
+      split_bf16(v[2 * e], p0);
+      split_bf16(v[2 * e + 1], p1);
+#pragma unroll
+      for (int i = 0; i < 3; ++i) w[i][e] = p0[i] | p1[i] << 16;
+    }
+  };
+  bf16x8 mid[MT][S][3];
+  // (each wave for itself, they were a third of the time of 8500 rows of rank 64: 134 us, shared 120)
+  if constexpr (MT == 1) {
 #pragma unroll
     for (int k = 0; k < S; ++k) {
-      const int j = 32 * k + 8 * g;
-      float v[8] = {};
-      if (mine[t] >= 0 && j < a.r) {
-        for (int p = 0; p < a.splits; ++p) {
-          const float* mp = a.mid + ((size_t)p * a.M + m) * a.r + j;
-          const f32x4 v0 = *reinterpret_cast<const f32x4*>(mp), v1 = *reinterpret_cast<const f32x4*>(mp + 4);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) v[e] += v0[e], v[4 + e] += v1[e];
-        }
-      }
       u32x4 w[3];
+      operands(0, k, mine[0], w);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        uint32_t p0[3], p1[3];
-        split_bf16(v[2 * e], p0);
-        split_bf16(v[2 * e + 1], p1);
-#pragma unroll
-        for (int i = 0; i < 3; ++i) w[i][e] = p0[i] | p1[i] << 16;
-      }
-#pragma unroll
-      for (int i = 0; i < 3; ++i) mid[t][k][i] = __builtin_bit_cast(bf16x8, w[i]);
+      for (int i = 0; i < 3; ++i) mid[0][k][i] = __builtin_bit_cast(bf16x8, w[i]);
     }
+  } else {                 // each wave some of them for all
+    __shared__ u32x4 shared_mid[MT * S][3][64];
+    for (int p = wave; p < MT * S; p += kAdWaves) {
+      u32x4 w[3];
+      operands(p / S, p % S, __shfl(own, 16 * (p / S) + col), w);
+#pragma unroll
+      for (int i = 0; i < 3; ++i) shared_mid[p][i][lane] = w[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int p = 0; p < MT * S; ++p)
+#pragma unroll
+      for (int i = 0; i < 3; ++i) mid[p / S][p % S][i] = __builtin_bit_cast(bf16x8, shared_mid[p][i][lane]);
   }
-  for (;;) {
-    f32x4 next[MT][NT];
-    const bool more = n0 + COLS < n_end;
-    if (more) load(n0 + COLS, next);
-    AdapterList list = all;
-    while (list.left) {
-      int id[U];
-      u32x4 bf[U][NT][S];
+  if (n0 >= n_end) return;
+  auto multiply = [&](const int (&id)[U], const u32x4 (&bf)[U][NT][S]) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) id[u] = u == 0 || list.left ? list.next() : id[0];       // (one of them again changes nothing)
+    for (int u = 0; u < U; ++u) {
 #pragma unroll
-      for (int u = 0; u < U; ++u)
+      for (int c = 0; c < NT; ++c) {
+        u32x4 w[S];
 #pragma unroll
-        for (int c = 0; c < NT; ++c) {
-          const uint16_t* bp = a.b + ((size_t)id[u] * a.N + min(n0 + 16 * c + col, a.N - 1)) * a.r;
+        for (int k = 0; k < S; ++k) w[k] = 32 * k + 8 * g < a.r ? bf[u][c][k] : u32x4{};
 #pragma unroll
-          for (int k = 0; k < S; ++k) bf[u][c][k] = *reinterpret_cast<const u32x4*>(bp + min(32 * k + 8 * g, a.r - 8));
-        }
+        for (int t = 0; t < MT; ++t) {
+          f32x4 acc = f32x4{};
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
+          for (int i = 2; i >= 0; --i)       // the smallest first
 #pragma unroll
-        for (int c = 0; c < NT; ++c) {
+            for (int k = 0; k < S; ++k)
+              acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w[k]), mid[t][k][i], acc, 0, 0, 0);
+          const bool keep = mine[t] == id[u] && (u == 0 || id[u] != id[0]);
 #pragma unroll
-          for (int k = 0; k < S; ++k) bf[u][c][k] = 32 * k + 8 * g < a.r ? bf[u][c][k] : u32x4{};
-#pragma unroll
-          for (int t = 0; t < MT; ++t) {
-            f32x4 acc = f32x4{};
-#pragma unroll
-            for (int i = 2; i >= 0; --i)       // the smallest first
-#pragma unroll
-              for (int k = 0; k < S; ++k)
-                acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, bf[u][c][k]), mid[t][k][i], acc, 0, 0, 0);
-            const bool keep = mine[t] == id[u] && (u == 0 || id[u] != id[0]);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) out[t][c][e] = keep ? out[t][c][e] + acc[e] : out[t][c][e];
-          }
+          for (int e = 0; e < 4; ++e) out[t][c][e] = keep ? out[t][c][e] + acc[e] : out[t][c][e];
         }
       }
+    }
+  };
+  for (;;) {
+    // Loads end in the order in which they begin: what the next columns need goes out here, all of it, so that none of these
+    // columns' waits for it.
+    f32x4 next[MT][NT];
+    u32x4 bn[U][NT][S];
+    const bool more = U == 1 && n0 + COLS < n_end;
+    if (more) {
+      weights(n0 + COLS, first, bn);
+      load(n0 + COLS, next);
+    }
+    multiply(first, bf);
+    for (AdapterList list = rest; list.left;) {
+      int id[U];
+      take(list, id);
+      weights(n0, id, bf);
+      multiply(id, bf);
     }
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
@@ -293,6 +348,10 @@ __global__ __launch_bounds__(kAdThreads) void adapter_up_kernel(AdapterArgs a) {
     for (int t = 0; t < MT; ++t)
 #pragma unroll
       for (int c = 0; c < NT; ++c) out[t][c] = next[t][c];
+#pragma unroll
+    for (int c = 0; c < NT; ++c)
+#pragma unroll
+      for (int k = 0; k < S; ++k) bf[0][c][k] = bn[0][c][k];
   }
 }
 

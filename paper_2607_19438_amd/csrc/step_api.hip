@@ -158,25 +158,32 @@ struct AdapterPlan {
 
 AdapterPlan adapter_plan(int M, int N, int K, int r) {
   AdapterPlan p{};
-  // mid: K is split over workgroups while they are few (us for splits of 1, 2, 4: 16 rows, rank 16 6.7, 5.0, 4.1; 96 rows, rank
-  // 32 10.0, 7.5, 7.0; 1252 rows, rank 8 12.4, 8.7, 6.3; 8500, rank 64 27.4, 23.3, 20.0; K = 2048 each). The second kernel
-  // adds the parts up, each of its workgroups those of its rows: 0.3 us for each of 96 rows of 8192 columns, but 10 to 20 of
-  // 8500 rows at rank 64.
-  p.mt_down = M > 4096 ? 2 : 1;
+  // mid: K is split over workgroups while they are few; the second kernel adds the parts up, each of its workgroups those of
+  // its rows. (us of the first kernel and the second, for splits of 1, 2, 4; K = 2048, 8192 columns: 96 rows, rank 32 9.8, 7.3,
+  // 6.9, and 13.0, 13.3, 14.2; 2048 rows, rank 16 7.0, 6.4, 6.8 and 30.4, 30.8, 31.5; 2500 rows, rank 64 15.1, 10.1, 10.0 and
+  // 41.9, 44.7, 48.9; 8500 rows, rank 64 26.2, 22.3, 22.1 and 119.6, 123.8, 139.0.) Tiles of 32 rows read A half as often
+  // (8500 rows, rank 64 26.2 and 38.6 us; 1252 rows, two splits 9.8 and 12.6), those of 16 have fewer adapters.
+  p.mt_down = M > 1024 ? 2 : 1;
   p.jt = r <= 16 ? 1 : r <= 32 ? 2 : 4;
-  p.lists = M <= 256 ? 16 : 1;           // a tile's adapters side by side where each row may have its own
+  // A tile's adapters side by side: each row may have its own (96 rows, 64 adapters: 1, 4, 16 at once 35.8, 11.9, 6.9 us); of
+  // prompts a tile has two or three where they meet, and the kernel waits for it (1252 rows of 14 prompts, rank 64: 1, 2, 4 at
+  // once 18.6, 13.5, 12.6 us).
+  p.lists = M <= 256 ? 16 : 4;
   const long tiles = qg::ceil_div(r, 16L * p.jt);
-  const long want = M <= 256 ? 256 / (M * tiles) : std::min(768 / (qg::ceil_div(M, 16L * p.mt_down) * tiles), 64L / r);
+  const long want = M <= 256 ? 256 / (M * tiles) : M <= 4096 ? 2 : 1;
   p.splits = (int)std::max<long>(1, std::min<long>({4, want, K / 256}));
   p.k_split = (int)(qg::ceil_div(qg::ceil_div(K, p.splits), qg::kAdRun) * qg::kAdRun);
   p.splits = (int)qg::ceil_div(K, p.k_split);
   // y: of few rows 16 columns to a wave and eight adapters at once (96 rows with 64 adapters, 8192 columns: 10.2 us, with 64
-  // columns 14.7 and 11.7 for one and two at once; 64 rows with 32, 4096 columns 5.6, with two at once 6.4); of many tiles
-  // of 32 by 32, four of them to a wave in turn (8500 rows of 8192, rank 64: 1, 2, 4, 8 in turn 177, 139, 136, 152 us, 32 by
-  // 64 169, 136, 151, 167; 2048 rows, rank 16 33.7, 31.2, 32.0, 38.8).
-  p.mt_up = p.nt = M <= 256 ? 1 : 2;
-  p.chunks = M <= 256 ? 1 : 4;
-  while (p.chunks > 1 && qg::ceil_div(M, 32) * qg::ceil_div(N, 128L * p.chunks) < 384) p.chunks /= 2;
+  // columns 14.7 and 11.7 for one and two at once; 64 rows with 32, 4096 columns 5.6, with two at once 6.4). Else tiles of 32 by
+  // 32, two of them to a wave in turn where that leaves four workgroups to a CU (8500 rows of 8192, rank 64: 1, 2, 4 in turn 130,
+  // 120, 124 us, tiles of 16 rows 204, 159, 155; 1252 rows, rank 64 26.2, 24.8, 26.8). At a rank up to 32 the operands are soon
+  // made, and few tiles are of 16 rows (1252 rows of 5003, rank 8 14.0, 12.2 us, of 32 rows 15.3, 13.3; 540 rows of 4096, rank
+  // 16 6.3 and 7.0; but 2048 rows of 8192 31.2 and 30.4).
+  const bool small = r <= 32 && qg::ceil_div(M, 32) * qg::ceil_div(N, 256) < 4 * kCUs;
+  p.nt = M <= 256 ? 1 : 2;
+  p.mt_up = M <= 256 || small ? 1 : 2;
+  p.chunks = M > 256 && qg::ceil_div(M, 16L * p.mt_up) * qg::ceil_div(N, 256) >= 4 * kCUs ? 2 : 1;
   p.s = r <= 32 ? 1 : r <= 64 ? 2 : 4;
   p.at_mid = round16((long)M * (long)sizeof(int32_t));
   p.bytes = p.at_mid + (long)p.splits * M * r * (long)sizeof(float);
@@ -449,7 +456,8 @@ int qgemm_adapters(const void* x, const void* a_w, const void* b_w, const int32_
     else if (plan.s == 2) launch(qg::adapter_up_kernel<1, 1, 2, 8>, up);
     else launch(qg::adapter_up_kernel<1, 1, 4, 4>, up);
   } else {
-    if (plan.s == 1) launch(qg::adapter_up_kernel<2, 2, 1, 1>, up);
+    if (plan.mt_up == 1) launch(qg::adapter_up_kernel<1, 2, 1, 1>, up);
+    else if (plan.s == 1) launch(qg::adapter_up_kernel<2, 2, 1, 1>, up);
     else if (plan.s == 2) launch(qg::adapter_up_kernel<2, 2, 2, 1>, up);
     else launch(qg::adapter_up_kernel<2, 2, 4, 1>, up);
   }

@@ -63,6 +63,18 @@ def test_sizes(lens, N, K, r, n, pad):
         check(torch, c, False, gain=False)
 
 
+@pytest.mark.parametrize("R,most,N,K,r,pad", [(63, 9, 40, 64, 8, 3), (64, 9, 40, 64, 40, 0), (65, 9, 40, 64, 16, 1), (130, 3, 33, 40, 8, 0), (1000, 2, 20, 16, 24, 5),
+                                             (4100, 1, 20, 16, 8, 0), (300, 60, 1030, 64, 48, 7), (300, 60, 1030, 64, 8, 0), (90, 60, 1030, 264, 16, 2)])
+def test_many_requests(R, most, N, K, r, pad):
+    """Requests of no row up to `most`, in every part of a look-up among up to thousands, and tiles of several adapters whose
+    workgroups go through more than one piece of the columns."""
+    torch = torch_or_skip()
+    lens = np.random.default_rng(R).integers(0, most + 1, R)
+    lens[[0, R // 2, R - 1]] = [0, most, 0]
+    c = make(list(lens), N, K, r, 5, seed=R, pad=pad)
+    check(torch, c, True)
+
+
 def test_interleaved_tenants():
     """Rows that change their adapter at every step, in a batch large enough for tiles of several rows."""
     torch = torch_or_skip()
