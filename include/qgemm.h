@@ -449,7 +449,7 @@ int qgemm_attention_kv4_shared_workspace(int T, int R, int G, int H, int Hkv, in
  * selection all but one of a prompt's), tokens of logit -inf, and all of a row that holds NaN or +inf. Behind the last
  * candidate stand score -inf, parent -1 and token `end`. So finished is (out_tokens == end) for the next selection.
  * logits: fp32 (as qgemm_dense writes them) or bf16 [R*B][V] at `stride` elements between rows, aligned to their
- * elements; scores: fp32 [R][B]; finished: uint8 [R][B] or null; outputs [R][K]. Maximum and sum of a row in
+ * elements; scores: fp32 [R][B]; finished: uint8 [R][B] or null; outputs [R][K], which share no memory with an input or each other. Maximum and sum of a row in
  * fp32 and fp64, values in fp64, rounded once. Results are the same on every call. B <= 64, K <= 128 (of more than one
  * beam K = B continues as many, K = 2B leaves a choice), R*B <= 2^20, V <= 2^30. workspace: caller-owned, 16-byte aligned,
  * of the bytes that qgemm_beam_select_workspace gives, without initialisation; calls that can overlap need one each.

@@ -123,6 +123,20 @@ def test_chunks(groups, prefix, own, new, H, Hkv, D, page):
 
 
 @pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("groups,prefix,new,H,Hkv,page", [
+    ([0, 170], [900], [1] * 170, 32, 8, 64), ([0, 170], [130], [1] * 170, 32, 8, 16),                # 128 rows to a tile of the shared keys,
+    ([1, 90, 179], [700, 300], [1] * 180, 64, 8, 32), ([0, 44], [1500], [4 + i % 3 for i in range(44)], 32, 8, 128),   # 16 or 32 of the others
+    ([0, 20, 41], [260, 640], [3 + i % 6 for i in range(43)], 64, 8, 16),
+])
+def test_many_rows_to_a_group(groups, prefix, new, H, Hkv, page, D):
+    torch = torch_or_skip()
+    own = [n + (41 * i) % 150 for i, n in enumerate(new)]
+    c = make(groups, prefix, own, new, H, Hkv, D, page, seed=len(new), pad=1)
+    rows = set(range(0, int(c["cu"][-1]), 7)) | {int(c["cu"][-1]) - 1}
+    check(torch, c, rows=rows)
+
+
+@pytest.mark.parametrize("D", [64, 128])
 def test_long_prefix_split_over_the_chip(D):
     torch = torch_or_skip()
     own = [1 + (37 * i) % 500 for i in range(33)]
