@@ -4,7 +4,7 @@
 // says what is wrong. A decode step's calls take less time on the GPU than their checks take in Python: host time
 // of a call of 16 rows (us, Python alone and with this file) rope 8.5, 4.4; plan 10.2, 5.1; store and load 16.5, 8.9;
 // packed prompts 9.0, 4.7; attention over the cache 10.5, 5.4; over shared prefixes 14.3, 8.6; selection of beams 15.1, 7.6;
-// table reordering 16.5, 10.0 and page copies 6.7, 3.3; adapters 12.0, 7.4; a launch is 2.4 of it, an allocation 0.6.
+// table reordering 16.1, 9.0 and page copies 6.7, 3.3; adapters 12.0, 7.4; a launch is 2.4 of it, an allocation 0.6.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
@@ -388,12 +388,11 @@ PyObject* kv_reorder_(PyObject* const* a) {
   int64_t need = 0;
   if (lib.reorder_workspace((int)R, (int)B, (int)W, &need) != 0) return not_here();
   const int64_t n = rows * W, len = n, src = len + rows, dst = src + rows, gone = dst + rows, used = gone + Q, all = used + 2;
-  const at::Tensor buf = at::empty({all}, tab->options()), ws = at::empty({need}, tab->options().dtype(at::kByte));
+  const at::Tensor buf = at::empty({all + need / 4}, tab->options());          // with the workspace, as an allocation is 0.6 us
   int32_t *p = memory<int32_t>(&buf), *tp = memory<int32_t>(tab), *kp = memory<int32_t>(kv), *op = memory<int32_t>(of),
           *fp = memory<int32_t>(fr), *ep = memory<int32_t>(keep);
-  void* wp = memory(&ws);
   if (call([&] {
-        return lib.reorder(tp, kp, op, fp, ep, p, p + len, p + src, p + dst, p + used, p + gone, p + used + 1, wp, need, (int)R, (int)B, (int)W,
+        return lib.reorder(tp, kp, op, fp, ep, p, p + len, p + src, p + dst, p + used, p + gone, p + used + 1, p + all, need, (int)R, (int)B, (int)W,
                            (int)F, Q, page, s);
       }) != 0)
     return not_here();
