@@ -500,7 +500,7 @@ int qgemm_kv4_copy(void* cache, const int32_t* src, const int32_t* dst, int n, i
  * x: bf16 [M][K] at x_stride elements between rows (a multiple of 8); a: bf16 [n][r][K]; b: bf16 [n][N][r]; ids: int32 [R];
  * gain: fp32 [n] or null (1); y: fp32 [M][N] at y_stride elements, so that the columns of one projection within a wider
  * row can be given. y is read and written (the one output here that is added to), and shares no memory with an input.
- * K and r multiples of 8 (an adapter of lower rank has zeros behind it), r <= 128, M, N and K <= 2^28. fp32
+ * K and r multiples of 8 (an adapter of lower rank has zeros behind it), r <= 128, M <= 2^25, N, K and R <= 2^28. fp32
  * accumulation; the inner sums enter the second product as three bf16 numbers each, which hold them whole. What one
  * adapter or request holds (infinities and NaN included) reaches no other's rows. Results are the same on every call.
  * Rows of an adapter that stand next to each other share the reading of its weights.

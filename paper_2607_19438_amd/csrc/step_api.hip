@@ -196,7 +196,8 @@ int check_adapters(int M, int N, int K, int r, int n, int R) {
   if (K < 8 || K % 8 != 0) return fail(QGEMM_EINVAL, "K must be a positive multiple of 8 (got %d)", K);
   if (r < 8 || r % 8 != 0) return fail(QGEMM_EINVAL, "the rank must be a positive multiple of 8 (got %d)", r);
   if (r > qg::kAdMaxRank) return fail(QGEMM_EUNSUPPORTED, "rank %d exceeds the supported %d", r, qg::kAdMaxRank);
-  if (N > (1 << 28) || K > (1 << 28) || M > (1 << 28)) return fail(QGEMM_EUNSUPPORTED, "M, N and K must be at most 2^28");
+  if (N > (1 << 28) || K > (1 << 28) || R > (1 << 28)) return fail(QGEMM_EUNSUPPORTED, "N, K and R must be at most 2^28");
+  if (M > (1 << 25)) return fail(QGEMM_EUNSUPPORTED, "M must be at most 2^25");        // the first kernel's grid, with its lists and rank tiles
   return QGEMM_OK;
 }
 

@@ -102,7 +102,7 @@ def test_adapters_refusals(m):
     for kw in ({"M": -1}, {"R": -1}, {"N": 0}, {"n": 0}, {"K": 0}, {"K": 60}, {"r": 0}, {"r": 12}, {"xs": 56}, {"ys": 19}, {"cu": 0}, {"x": 0}, {"a": 0},
                {"b": 0}, {"ids": 0}, {"y": 0}, {"ws": 0}, {"bytes": 0}):
         assert call(**kw) == -1, kw
-    for kw in ({"r": 136}, {"N": 1 << 29, "ys": 1 << 30}, {"K": 1 << 29, "xs": 1 << 29}, {"M": 1 << 29}):
+    for kw in ({"r": 136}, {"N": 1 << 29, "ys": 1 << 30}, {"K": 1 << 29, "xs": 1 << 29}, {"M": 1 << 29}, {"M": (1 << 25) + 1}, {"R": 1 << 29}):
         assert call(**kw) == -3, kw
     for kw in ({"x": 24}, {"a": 24}, {"b": 24}, {"ws": 24}, {"ids": 18}, {"cu": 18}, {"gain": 18}, {"y": 18}, {"xs": 68}):
         assert call(**kw) == -2, kw
