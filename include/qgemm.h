@@ -444,8 +444,10 @@ int qgemm_attention_kv4_shared_workspace(int T, int R, int G, int H, int Hkv, in
 /*
  * The K best continuations of every request's B beams: of the candidates (beam b, token v), worth
  *   scores[r][b] + x[v] - log sum_u exp x[u],  x the row r*B + b of logits,
- * the K of largest value, in descending order, equal ones the lower beam first, of a beam the lower token:
+ * the K of largest value, in descending order:
  *   out_scores[r][k] its value, out_parents[r][k] = b, out_tokens[r][k] = v
+ * Of a beam the larger logit comes first, of equal ones the lower token, also where a large score hides the difference from the
+ * value; beams are compared by their candidates' values in fp64, equal ones the lower beam first.
  * A beam with finished[r][b] != 0 has one candidate, the token `end` at its own score; its logits do not matter. No
  * candidates are those worth -inf or NaN: all of a beam whose score is (a beam that is not there: before the first
  * selection all but one of a prompt's), tokens of logit -inf, and all of a row that holds NaN or +inf. Behind the last

@@ -78,13 +78,15 @@ def beam_values(logits, scores, finished, end):
 
 
 def beam_select(logits, scores, K, finished=None, end=0):
-    """logits [R*B][V], scores [R][B] -> (scores float64, parents, tokens), each [R][K]."""
+    """logits [R*B][V], scores [R][B] -> (scores float64, parents, tokens), each [R][K]. Equal values: the lower beam first, of a
+    beam the larger logit, then the lower token."""
     R, B = scores.shape
     V = logits.shape[1]
     best, par, tok = np.full((R, K), -np.inf), np.full((R, K), -1), np.full((R, K), end)
     for r in range(R):
         val = beam_values(logits[r * B:(r + 1) * B], scores[r], None if finished is None else finished[r], end).ravel()
-        for k, i in enumerate(np.lexsort((np.arange(len(val)), -val))[:K]):
+        order = np.arange(B * V), -np.asarray(logits[r * B:(r + 1) * B], dtype=np.float64).ravel(), np.arange(B * V) // V
+        for k, i in enumerate(np.lexsort((*order, -val))[:K]):
             if val[i] > -np.inf:
                 best[r, k], par[r, k], tok[r, k] = val[i], i // V, i % V
     return best, par, tok

@@ -319,12 +319,15 @@ __global__ __launch_bounds__(kBeamThreads, 4) void beam_rows_kernel(BeamArgs a) 
   for (int i = total + tid; i < K; i += kBeamThreads) out[i] = 0;
 }
 
-// One workgroup to a request. Candidate e = (beam, piece, place in the piece's list); equal values go to the lower e.
+// One workgroup to a request. Candidate e = (beam, piece, place in the piece's list). Equal values go to the lower beam, and of
+// a beam to the larger logit, then the lower token, as e has it: a large score makes the values of different logits equal, and
+// then their order must not follow the pieces. So a beam's candidates come in the order of their keys whatever their values
+// round to, and the K of largest key, which its pieces' lists hold, are all that can be chosen.
 // MOST: candidates at most.
 template <int MOST>
 __global__ __launch_bounds__(kBeamThreads) void beam_join_kernel(BeamArgs a) {
   __shared__ uint64_t kept_value[MOST];   // (all of them where all are worth the same)
-  __shared__ uint16_t kept_at[MOST];
+  __shared__ uint64_t kept_next[MOST];    // what their order goes by next, lower ones first: beam, logit turned round, e
   constexpr int kHeld = 4;                // of a thread's candidates, in registers
   __shared__ double off[kBeamMaxB];       // score - lse
   __shared__ float score[kBeamMaxB];
@@ -385,12 +388,12 @@ __global__ __launch_bounds__(kBeamThreads) void beam_join_kernel(BeamArgs a) {
 #pragma unroll
     for (int i = 0; i < kHeld; ++i) {
       const int e = tid + i * kBeamThreads;
-      if (e < n) f(e, value(e, held[i]));
+      if (e < n) f(e, value(e, held[i]), held[i]);
     }
-    for (int e = tid + kHeld * kBeamThreads; e < n; e += kBeamThreads) f(e, value(e, cand[e]));
+    for (int e = tid + kHeld * kBeamThreads; e < n; e += kBeamThreads) f(e, value(e, cand[e]), cand[e]);
   };
   uint32_t top = 0;
-  for_each([&](int, uint64_t v) { top = max(top, (uint32_t)(v >> 32)); });
+  for_each([&](int, uint64_t v, uint64_t) { top = max(top, (uint32_t)(v >> 32)); });
   // a bound that K candidates reach, from the threads' largest: with a candidate or two to a thread about K are left
   uint64_t from = 0;
   if (n > K) {
@@ -399,11 +402,11 @@ __global__ __launch_bounds__(kBeamThreads) void beam_join_kernel(BeamArgs a) {
     const uint32_t mine[4] = {each[lane], each[64 + lane], each[128 + lane], each[192 + lane]};
     from = (uint64_t)wave_bound<8>(mine, K) << 32;
   }
-  for_each([&](int e, uint64_t v) {
+  for_each([&](int e, uint64_t v, uint64_t k) {
     if (v && v >= from) {
       const int i = atomicAdd(&kept_n, 1);          // a set: its order does not matter
       kept_value[i] = v;
-      kept_at[i] = (uint16_t)e;
+      kept_next[i] = (uint64_t)beam_of(e) << 48 | (uint64_t)~(uint32_t)(k >> 32) << 16 | (uint32_t)e;
     }
   });
   __syncthreads();
@@ -413,11 +416,12 @@ __global__ __launch_bounds__(kBeamThreads) void beam_join_kernel(BeamArgs a) {
   int32_t* ot = a.out_tokens + (size_t)r * K;
   for (int i = tid; i < m; i += kBeamThreads) {
     const uint64_t v = kept_value[i];
-    const int e = kept_at[i], b = beam_of(e);
+    const uint64_t next = kept_next[i];
+    const int e = (int)(next & 0xffff), b = beam_of(e);
     const uint64_t k = cand[e];
     int p = 0;
 #pragma unroll 4
-    for (int j = 0; j < m; ++j) p += kept_value[j] > v || (kept_value[j] == v && kept_at[j] < e);
+    for (int j = 0; j < m; ++j) p += kept_value[j] > v || (kept_value[j] == v && kept_next[j] < next);
     if (p >= K) continue;
     os[p] = (float)__builtin_bit_cast(double, v ^ ((v >> 63) ? 1ull << 63 : ~0ull));
     ob[p] = b;
