@@ -123,7 +123,7 @@ __global__ __launch_bounds__(kKv4Threads, (kKv4PerCU<D, (NP > NT ? NP : NT)>)) v
   using WideLds = SharedWideLds<D>;
   constexpr size_t kLds = kAnyWide && sizeof(WideLds) > sizeof(TileLds) ? sizeof(WideLds) : sizeof(TileLds);
   __shared__ __attribute__((aligned(16))) char lds[kLds];
-  extern __shared__ int32_t group_lds[];
+  extern __shared__ int4 group_lds[];        // (its type is its alignment: requests and groups are read 16 bytes at once)
   __shared__ unsigned wsum[2][kKv4Waves];
   __shared__ struct {
     int v;
@@ -133,7 +133,7 @@ __global__ __launch_bounds__(kKv4Threads, (kKv4PerCU<D, (NP > NT ? NP : NT)>)) v
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int G = a.H / a.Hkv, R = a.R, Gn = sa.Gn;
-  int4* const req = reinterpret_cast<int4*>(group_lds);        // [R] first row, rows, keys, group (-1: none)
+  int4* const req = group_lds;                                 // [R] first row, rows, keys, group (-1: none)
   int4* const grp = req + R;                                   // [Gn] first row, rows, shared keys, first granule of its units
   int32_t* const gstart = reinterpret_cast<int32_t*>(grp + Gn);          // [Gn + 1] first requests of the groups
 
