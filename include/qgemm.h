@@ -505,8 +505,10 @@ int qgemm_kv4_copy(void* cache, const int32_t* src, const int32_t* dst, int n, i
  * gain: fp32 [n] or null (1); y: fp32 [M][N] at y_stride elements, so that the columns of one projection within a wider
  * row can be given. y is read and written (the one output here that is added to), and shares no memory with an input.
  * K and r multiples of 8 (an adapter of lower rank has zeros behind it), r <= 128, M <= 2^25, N, K and R <= 2^28. fp32
- * accumulation; the inner sums enter the second product as three bf16 numbers each, which hold them whole. What one
- * adapter or request holds (infinities and NaN included) reaches no other's rows. Results are the same on every call.
+ * accumulation; the inner sums, times gain, enter the second product as three bf16 numbers each, which hold them whole (of
+ * those below 2^-110 in size what is below 2^-133 is lost). An infinite weight or sum gives the formula's infinity or NaN
+ * (an infinite b with an inner sum that is not 0 but below 2^-90 in size may give NaN too). What one adapter or request
+ * holds (infinities and NaN included) reaches no other's rows. Results are the same on every call.
  * Rows of an adapter that stand next to each other share the reading of its weights.
  * workspace: caller-owned, 16-byte aligned, of qgemm_adapters_workspace's bytes, without initialisation; calls that can
  * overlap need one each.

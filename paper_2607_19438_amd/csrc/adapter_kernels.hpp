@@ -176,14 +176,22 @@ __global__ __launch_bounds__(64 * WAVES) void adapter_down_kernel(AdapterArgs a)
   }
 }
 
-// x = p[0] + p[1] + p[2] with eight bits of its significand in each, cut and not rounded, so that all 24 are there and
-// no finite number becomes infinite: as three bf16 numbers mid enters the product whole, and fp32 y sees no bf16 step.
+// x = p[0] + p[1] + p[2] with eight bits of its significand in each, so that all 24 are there: as three bf16 numbers mid
+// enters the product whole, and fp32 y sees no bf16 step. Cut and not rounded, so that no finite number becomes infinite. The
+// first two are the largest bf16 numbers below what is left in size, not up to it (1 is 1 - 2^-8 and so on), so that none
+// of the three is 0 beside one that is not, and an infinite weight gives an infinity of the product's sign: 0 times it
+// would be NaN. What is below, at most a step of the first part (2^-7), is exact in the other two: the second leaves at
+// most a step of its own, 2^-15, a multiple of 2^-23. Below 2^-90 the last part would come near bf16's smallest numbers,
+// and x is cut as it is. An infinity or NaN is all three parts.
 __device__ __forceinline__ void split_bf16(float x, uint32_t (&p)[3]) {
+  const uint32_t size = __builtin_bit_cast(uint32_t, x) & 0x7f800000u;
+  const bool finite = size != 0x7f800000u;
+  const uint32_t below = finite && size >= (127u - 90u) << 23 ? 1u : 0u;
 #pragma unroll
   for (int i = 0; i < 3; ++i) {
-    const uint32_t u = __builtin_bit_cast(uint32_t, x) & 0xffff0000u;
+    const uint32_t u = (__builtin_bit_cast(uint32_t, x) - (i < 2 ? below : 0u)) & 0xffff0000u;
     p[i] = u >> 16;
-    x = (u & 0x7f800000u) == 0x7f800000u ? 0.0f : x - __builtin_bit_cast(float, u);       // (infinity less itself is no 0)
+    x = finite ? x - __builtin_bit_cast(float, u) : x;
   }
 }
 
