@@ -434,10 +434,10 @@ __global__ __launch_bounds__(kBeamThreads) void beam_join_kernel(BeamArgs a) {
 // tables and pages after a selection
 // ---------------------------------------------------------------------------
 //
-// A workgroup takes 256 columns of a request's tables. Every one counts for itself the pages that the requests before
-// take from the free list (a thread to a row: a few loads), so that nothing waits for another. Pages that no row holds any
-// more are left in the caller's workspace, and a second kernel, which knows how many the workgroups before have
-// found, moves them to their places in the list.
+// A workgroup takes blocks of 256 columns of a request's tables, one unless there are very many. Every one counts for itself the
+// pages that the requests before take from the free list (a thread to a row: a few loads), so that nothing waits for
+// another. Pages that no row holds any more are left in the caller's workspace, and a second kernel, which knows how many
+// the blocks before have left, moves them to their places in the list.
 // Bound by chains of loads: lengths and parents, old entries, then the counts of the first kernel (4 x 4 beams of up to 3100 tokens
 // 6.2 and 2.1 us; 64 x 8 of up to 6200 tokens, pages of 32, 9.4 and 3.0 us, 0.8 MB in all).
 
@@ -457,9 +457,11 @@ struct ReorderArgs {
   int32_t* used;
   int32_t* released;          // [Q]
   int32_t* n_released;
-  int32_t* counts;            // [R * blocks] pages that a workgroup's columns release
+  int32_t* counts;            // [R * blocks] pages that a block's columns release
   int32_t* gone;              // [R * blocks][256 B] the pages
   int R, B, W, F, Q, page_log2, blocks;
+  int each, parts;            // blocks of a workgroup; workgroups of a request
+  int release_each, release;  // blocks of a workgroup of the second kernel; its workgroups
 };
 
 struct ReorderBeams {
@@ -549,14 +551,19 @@ __device__ __forceinline__ int reorder_beams(const ReorderArgs& a, int r, Reorde
   return before;
 }
 
+// SEVERAL: whether workgroups take several blocks (the loop that then goes over them costs 0.5 us, with one block too).
+template <bool SEVERAL>
 __global__ __launch_bounds__(kReorderThreads) void kv_reorder_kernel(ReorderArgs a) {
   extern __shared__ int32_t old_lds[];         // [B][256] the columns' old entries, each thread its own; -1 behind a row's pages
   __shared__ ReorderBeams s;
   __shared__ int gone_n[kReorderThreads / 64];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, B = a.B;
-  const int r = blockIdx.x / a.blocks, block = blockIdx.x - r * a.blocks;
+  const int parts = SEVERAL ? a.parts : a.blocks;
+  const int r = blockIdx.x / parts, part = blockIdx.x - r * parts;
+  int block = SEVERAL ? part * a.each : part;
+  const int block_end = SEVERAL ? min(a.blocks, block + a.each) : block + 1;
   const int32_t* old = a.table + (size_t)r * B * a.W;
-  const int j = block * kReorderThreads + tid;
+  int j = block * kReorderThreads + tid;
   // the first eight rows' entries are on their way while the request's beams are looked up
   int32_t x[8];
   auto load = [&](int b0) {
@@ -571,72 +578,81 @@ __global__ __launch_bounds__(kReorderThreads) void kv_reorder_kernel(ReorderArgs
     const bool can = fresh >= 0 && last < a.W && (long)before + fresh < a.F;
     const int page = can ? a.free_pages[(size_t)before + fresh] : -1;
     s.row[tid] = make_int4(max(p, 0), fresh >= 0 ? last : -1, page, p >= 0);
-    if (block == 0) {
+    if (part == 0) {
       const size_t row = (size_t)r * B + tid;
       a.new_len[row] = p < 0 ? 0 : s.len[p];
       a.src[row] = can ? old[(size_t)p * a.W + last] : -1;
       a.dst[row] = page;
     }
   }
-  if (r == a.R - 1 && block == 0 && tid == 0) a.used[0] = before + s.taken;
+  if (r == a.R - 1 && part == 0 && tid == 0) a.used[0] = before + s.taken;
   __syncthreads();
   auto entry = [&](int b) -> int32_t& { return old_lds[b * kReorderThreads + tid]; };
-  for (int b0 = 0; b0 < B; b0 += 8) {
-    if (b0) load(b0);
+  for (;;) {
+    for (int b0 = 0; b0 < B; b0 += 8) {
+      if (b0) load(b0);
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (b0 + i < B) entry(b0 + i) = j < s.have[b0 + i] ? x[i] : -1;
-  }
-  unsigned long long gone = 0;
-  if (j < a.W) {
-    int32_t* out = a.new_table + (size_t)r * B * a.W + j;
-#pragma unroll 4
-    for (int k = 0; k < B; ++k, out += a.W) {
-      const int4 row = s.row[k];
-      *out = !row.w ? -1 : j == row.y ? row.z : entry(row.x);
+      for (int i = 0; i < 8; ++i)
+        if (b0 + i < B) entry(b0 + i) = j < s.have[b0 + i] ? x[i] : -1;
     }
-    // Of the column's old entries, those that no new row holds any more. A page stands in the same column of all rows that
-    // share it, and a row's children hold all of its pages, so only rows without children can lose one.
-    if (j >= first)
-      for (unsigned long long m = s.childless; m; m &= m - 1) {
-        const int b = __builtin_ctzll(m), id = entry(b);
-        const unsigned long long others = s.live | (s.childless & ((1ull << b) - 1));      // (the lower ones list a page that they share)
-        bool stays = id < 0;
-#pragma unroll 8
-        for (int p = 0; p < B; ++p) stays |= entry(p) == id && (others >> p & 1);
-        if (!stays) gone |= 1ull << b;
+    unsigned long long gone = 0;
+    if (j < a.W) {
+      int32_t* out = a.new_table + (size_t)r * B * a.W + j;
+#pragma unroll 4
+      for (int k = 0; k < B; ++k, out += a.W) {
+        const int4 row = s.row[k];
+        *out = !row.w ? -1 : j == row.y ? row.z : entry(row.x);
       }
-  }
-  // the pages, by column and row
-  const int n = __builtin_popcountll(gone);
-  int inc = n;
+      // Of the column's old entries, those that no new row holds any more. A page stands in the same column of all rows that
+      // share it, and a row's children hold all of its pages, so only rows without children can lose one.
+      if (j >= first)
+        for (unsigned long long m = s.childless; m; m &= m - 1) {
+          const int b = __builtin_ctzll(m), id = entry(b);
+          const unsigned long long others = s.live | (s.childless & ((1ull << b) - 1));      // (the lower ones list a page that they share)
+          bool stays = id < 0;
+#pragma unroll 8
+          for (int p = 0; p < B; ++p) stays |= entry(p) == id && (others >> p & 1);
+          if (!stays) gone |= 1ull << b;
+        }
+    }
+    // the pages, by column and row
+    const int n = __builtin_popcountll(gone);
+    int inc = n;
 #pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int up = __shfl_up(inc, d);
-    if (lane >= d) inc += up;
-  }
-  if (lane == 63) gone_n[wave] = inc;
-  __syncthreads();
-  int at = inc - n, all = 0;
+    for (int d = 1; d < 64; d <<= 1) {
+      const int up = __shfl_up(inc, d);
+      if (lane >= d) inc += up;
+    }
+    if (lane == 63) gone_n[wave] = inc;
+    __syncthreads();
+    int at = inc - n, all = 0;
 #pragma unroll
-  for (int i = 0; i < kReorderThreads / 64; ++i) {
-    at += i < wave ? gone_n[i] : 0;
-    all += gone_n[i];
+    for (int i = 0; i < kReorderThreads / 64; ++i) {
+      at += i < wave ? gone_n[i] : 0;
+      all += gone_n[i];
+    }
+    const size_t at_block = SEVERAL ? (size_t)r * a.blocks + block : blockIdx.x;
+    if (tid == 0) a.counts[at_block] = all;
+    for (int32_t* out = a.gone + at_block * kReorderThreads * B; gone; gone &= gone - 1) out[at++] = entry(__builtin_ctzll(gone));
+    if (!SEVERAL || ++block >= block_end) return;
+    j = block * kReorderThreads + tid;
+    load(0);
+    __syncthreads();            // gone_n has been read
   }
-  if (tid == 0) a.counts[blockIdx.x] = all;
-  for (int32_t* out = a.gone + (size_t)blockIdx.x * kReorderThreads * B; gone; gone &= gone - 1) out[at++] = entry(__builtin_ctzll(gone));
 }
 
 // The released pages to their places, -1 behind the last.
+template <bool SEVERAL>
 __global__ __launch_bounds__(kReorderThreads) void kv_release_kernel(ReorderArgs a) {
   __shared__ int sums[kReorderThreads / 64][2];
-  const int tid = threadIdx.x, lane = tid & 63, nblk = a.R * a.blocks, me = (int)blockIdx.x;
-  const int mine = a.counts[me];
+  const int tid = threadIdx.x, lane = tid & 63, nblk = a.R * a.blocks;
+  const int begin = (int)blockIdx.x * (SEVERAL ? a.release_each : 1), end = min(nblk, begin + a.release_each);
+  int mine = a.counts[begin];
   int before = 0, all = 0;
   for (int i = tid; i < nblk; i += kReorderThreads) {
     const int c = a.counts[i];
     all += c;
-    if (i < me) before += c;
+    if (i < begin) before += c;
   }
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) before += __shfl_xor(before, d), all += __shfl_xor(all, d);
@@ -645,10 +661,16 @@ __global__ __launch_bounds__(kReorderThreads) void kv_release_kernel(ReorderArgs
   before = all = 0;
 #pragma unroll
   for (int i = 0; i < kReorderThreads / 64; ++i) before += sums[i][0], all += sums[i][1];
-  if (me == 0 && tid == 0) a.n_released[0] = all;
-  for (long i = (long)all + (long)me * kReorderThreads + tid; i < a.Q; i += (long)nblk * kReorderThreads) a.released[i] = -1;
-  const int32_t* from = a.gone + (size_t)me * kReorderThreads * a.B;
-  for (int i = tid; i < mine && before + i < a.Q; i += kReorderThreads) a.released[before + i] = from[i];
+  if (begin == 0 && tid == 0) a.n_released[0] = all;
+  const long step = (long)(SEVERAL ? a.release : nblk) * kReorderThreads;
+  for (long i = (long)all + (long)blockIdx.x * kReorderThreads + tid; i < a.Q; i += step) a.released[i] = -1;
+  for (int block = begin;;) {
+    const int32_t* from = a.gone + (size_t)block * kReorderThreads * a.B;
+    for (int i = tid; i < mine && before + i < a.Q; i += kReorderThreads) a.released[before + i] = from[i];
+    if (!SEVERAL || ++block >= end) return;
+    before += mine;
+    mine = a.counts[block];
+  }
 }
 
 struct CopyArgs {

@@ -360,14 +360,21 @@ int qgemm_kv_reorder(const int32_t* block_table, const int32_t* kv_len, const in
                             {"free_pages", free_pages, F}, {"keep", keep, keep ? R : 0}};
   rc = check_apart(written, 8, read, 5);
   if (rc != QGEMM_OK) return rc;
+  const qg::ReorderSplit split = qg::reorder_split(R, blocks);
   qg::ReorderArgs a{block_table, kv_len, parents, free_pages, keep, new_table, new_len, src, dst, used, released, n_released,
-                    static_cast<int32_t*>(workspace), static_cast<int32_t*>(workspace) + counts, R, B, W, F, Q, page_log2(page), (int)blocks};
-  if (!qg::grid_fits(counts, qg::kReorderThreads)) return fail(QGEMM_EUNSUPPORTED, "too many workgroups");
+                    static_cast<int32_t*>(workspace), static_cast<int32_t*>(workspace) + counts, R, B, W, F, Q, page_log2(page), (int)blocks,
+                    (int)split.each, (int)split.parts, (int)split.release_each, (int)split.release};
+  if (!qg::grid_fits(R * split.parts, qg::kReorderThreads)) return fail(QGEMM_EUNSUPPORTED, "too many workgroups");
   (void)hipGetLastError();
-  hipLaunchKernelGGL(qg::kv_reorder_kernel, dim3((unsigned)counts), dim3(qg::kReorderThreads), (size_t)B * qg::kReorderThreads * sizeof(int32_t), stream, a);
+  const dim3 block(qg::kReorderThreads);
+  const size_t lds = (size_t)B * qg::kReorderThreads * sizeof(int32_t);
+  const dim3 grid((unsigned)(R * split.parts)), release((unsigned)split.release);
+  if (split.each == 1) hipLaunchKernelGGL(qg::kv_reorder_kernel<false>, grid, block, lds, stream, a);
+  else hipLaunchKernelGGL(qg::kv_reorder_kernel<true>, grid, block, lds, stream, a);
   rc = check_launch("qgemm_kv_reorder");
   if (rc != QGEMM_OK) return rc;
-  hipLaunchKernelGGL(qg::kv_release_kernel, dim3((unsigned)counts), dim3(qg::kReorderThreads), 0, stream, a);
+  if (split.release_each == 1) hipLaunchKernelGGL(qg::kv_release_kernel<false>, release, block, 0, stream, a);
+  else hipLaunchKernelGGL(qg::kv_release_kernel<true>, release, block, 0, stream, a);
   rc = check_launch("qgemm_kv_reorder (released pages)");
   return rc == QGEMM_OK ? ok() : rc;
 }

@@ -249,4 +249,26 @@ inline bool attn_packed_split(bool d64, long T, long R, long heads) {
   return wide <= (R <= 2 ? 512 : R <= 3 ? 384 : 256);
 }
 
+// Table reordering (beam_kernels.hpp), over R requests of `blocks` blocks of 256 columns. A workgroup takes `each` blocks of one
+// request in turn, `parts` of them share it: each counts what the requests before its own take. In the second kernel, where
+// every workgroup adds up all blocks' counts, `release_each` blocks go to one of `release` workgroups. Up to 2048 of either
+// have a block each (the first: or one to a request): with more the reads would grow with the square of the blocks, 1 GiB
+// for 8192 columns of 512 requests (of four beams 184 us, as it is 97) and 282 TB for 32767 columns of 65536 requests of
+// one, which a call may have.
+constexpr long kReorderGroups = 2048;
+
+struct ReorderSplit {
+  long each, parts, release_each, release;
+};
+
+inline ReorderSplit reorder_split(long R, long blocks) {
+  ReorderSplit p;
+  const long most = kReorderGroups / R > 1 ? kReorderGroups / R : 1;
+  p.each = ceil_div(blocks, most);
+  p.parts = ceil_div(blocks, p.each);
+  p.release_each = ceil_div(R * blocks, kReorderGroups);
+  p.release = ceil_div(R * blocks, p.release_each);
+  return p;
+}
+
 }  // namespace qg

@@ -11,7 +11,7 @@ from paper_2607_19438_amd import build
 
 USE = {
     "group_lds": ("attn_shared.hpp", "qg::kv4_shared_kernel<128, 2, 1>", 16),
-    "old_lds": ("beam_kernels.hpp", "qg::kv_reorder_kernel", 4),
+    "old_lds": ("beam_kernels.hpp", "qg::kv_reorder_kernel<false>", 4),
 }
 
 
