@@ -822,10 +822,9 @@ def beam_select(logits: torch.Tensor, scores: torch.Tensor, count: int | None = 
     _sizes(R * B, V, K, abs(int(end)))
     dev = _device(logits, scores)
     need = _workspace("beam_select", R, B, V, K)
-    # one allocation, as a small selection is all latency
-    buf = torch.empty(need // 4 + 3 * R * K, dtype=torch.int32, device=logits.device)
-    ws, parents, tokens, best = buf.split_with_sizes((need // 4, R * K, R * K, R * K))
+    best, parents, tokens = torch.empty(3 * R * K, dtype=torch.int32, device=logits.device).split_with_sizes((R * K,) * 3)
     best = best.view(torch.float32)
+    ws = torch.empty(need, dtype=torch.uint8, device=logits.device)
     _enqueue(lib().qgemm_beam_select, dev, logits.data_ptr(), 1 if logits.dtype is torch.bfloat16 else 0, scores.data_ptr(),
              None if finished is None else finished.data_ptr(), best.data_ptr(), parents.data_ptr(), tokens.data_ptr(), ws.data_ptr(), need,
              R, B, V, K, logits.stride(0) if R * B > 1 else V, int(end))

@@ -357,18 +357,19 @@ PyObject* beam_select_(PyObject* const* a) {
     return not_here();
   int64_t need = 0;
   if (lib.beam_workspace((int)R, (int)B, (int)V, K, &need) != 0) return not_here();
-  const int64_t n = R * K, at = need / 4;
-  const at::Tensor buf = at::empty({at + 3 * n}, sc->options().dtype(at::kInt));
+  // (results that a caller keeps, for one the parents of all steps, hold no workspace)
+  const int64_t n = R * K;
+  const at::Tensor buf = at::empty({3 * n}, sc->options().dtype(at::kInt)), ws = at::empty({need}, sc->options().dtype(at::kByte));
   int32_t* p = memory<int32_t>(&buf);
-  void *xp = memory(x), *fp = memory(fin);
+  void *xp = memory(x), *fp = memory(fin), *wp = memory(&ws);
   const float* sp = memory<float>(sc);
   const int type = x->scalar_type() == at::kBFloat16 ? QGEMM_BF16 : QGEMM_F32;
   if (call([&] {
-        return lib.beam(xp, type, sp, static_cast<const uint8_t*>(fp), reinterpret_cast<float*>(p + at), p + at + n, p + at + 2 * n, p, need,
-                        (int)R, (int)B, (int)V, K, xs, end, s);
+        return lib.beam(xp, type, sp, static_cast<const uint8_t*>(fp), reinterpret_cast<float*>(p), p + n, p + 2 * n, wp, need, (int)R,
+                        (int)B, (int)V, K, xs, end, s);
       }) != 0)
     return not_here();
-  const at::Tensor out[3] = {piece(buf, at, R, K, at::kFloat), piece(buf, at + n, R, K), piece(buf, at + 2 * n, R, K)};
+  const at::Tensor out[3] = {piece(buf, 0, R, K, at::kFloat), piece(buf, n, R, K), piece(buf, 2 * n, R, K)};
   return tuple(out);
 }
 
@@ -387,12 +388,13 @@ PyObject* kv_reorder_(PyObject* const* a) {
     return not_here();
   int64_t need = 0;
   if (lib.reorder_workspace((int)R, (int)B, (int)W, &need) != 0) return not_here();
-  const int64_t n = rows * W, len = n, src = len + rows, dst = src + rows, gone = dst + rows, used = gone + Q, all = used + 2;
-  const at::Tensor buf = at::empty({all + need / 4}, tab->options());          // with the workspace, as an allocation is 0.6 us
+  const int64_t n = rows * W, len = n, src = len + rows, dst = src + rows, gone = dst + rows, used = gone + Q;
+  const at::Tensor buf = at::empty({used + 2}, tab->options()), ws = at::empty({need}, tab->options().dtype(at::kByte));
   int32_t *p = memory<int32_t>(&buf), *tp = memory<int32_t>(tab), *kp = memory<int32_t>(kv), *op = memory<int32_t>(of),
           *fp = memory<int32_t>(fr), *ep = memory<int32_t>(keep);
+  void* wp = memory(&ws);
   if (call([&] {
-        return lib.reorder(tp, kp, op, fp, ep, p, p + len, p + src, p + dst, p + used, p + gone, p + used + 1, p + all, need, (int)R, (int)B, (int)W,
+        return lib.reorder(tp, kp, op, fp, ep, p, p + len, p + src, p + dst, p + used, p + gone, p + used + 1, wp, need, (int)R, (int)B, (int)W,
                            (int)F, Q, page, s);
       }) != 0)
     return not_here();
