@@ -926,7 +926,8 @@ def adapters(y: torch.Tensor, x: torch.Tensor, a: torch.Tensor, b: torch.Tensor,
 
     ``y`` [M][N] fp32 and ``x`` [M][K] bf16, rows at any stride (``x``'s a multiple of 8); ``a`` [n][r][K], ``b`` [n][N][r] bf16;
     ``gain`` [n] fp32; ``cu_q`` [R+1]: first rows of the requests, or None where each has one. Rows of an id outside [0, n)
-    are left as they are."""
+    are left as they are. Nothing here has a backward pass: a ``y`` that requires a gradient is refused where gradients are
+    recorded, and a graph that has saved ``y`` refuses to go back through it afterwards, as after torch's own in-place operations."""
     if _fast is not None:
         done = _fast.adapters(y, x, a, b, ids, gain, cu_q)
         if done is not NotImplemented:
@@ -940,6 +941,8 @@ def adapters(y: torch.Tensor, x: torch.Tensor, a: torch.Tensor, b: torch.Tensor,
             raise TypeError(f"{name} has dtype {t.dtype}, expected one of {dtypes}")
         if t.dim() != 2 or (t.numel() and t.shape[1] > 1 and t.stride(1) != 1):
             raise ValueError(f"{name} must have 2 dimensions, the last of them contiguous")
+    if y.requires_grad and torch.is_grad_enabled():
+        raise ValueError("y requires a gradient, which would lack the adapters' part: call it under torch.no_grad()")
     _need(a, "a", _BF16, 3)
     _need(b, "b", _BF16, 3)
     _need(ids, "ids", _I32, 1)
@@ -967,6 +970,8 @@ def adapters(y: torch.Tensor, x: torch.Tensor, a: torch.Tensor, b: torch.Tensor,
     _enqueue(lib().qgemm_adapters, dev, x.data_ptr(), a.data_ptr(), b.data_ptr(), ids.data_ptr(), None if cu_q is None else cu_q.data_ptr(),
              None if gain is None else gain.data_ptr(), y.data_ptr(), ws.data_ptr(), need, M, N, K, r, n, R, x.stride(0) if M > 1 else K,
              y.stride(0) if M > 1 else N)
+    if not y.is_inference():
+        torch.autograd.graph.increment_version(y)        # a graph that has saved y must not go back through it
     return y
 
 

@@ -9,6 +9,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/core/GradMode.h>
 #include <c10/core/impl/VirtualGuardImpl.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -435,7 +436,8 @@ PyObject* adapters_(PyObject* const* args) {
     return not_here();
   const int64_t M = x->size(0), K = x->size(1), n = a->size(0), r = a->size(1), N = y->size(1), R = ids->size(0);
   if (y->size(0) != M || a->size(2) != K || b->size(0) != n || b->size(1) != N || b->size(2) != r || !small({M, N, K, r, n, R}) ||
-      (gain && gain->size(0) != n) || (cu ? cu->size(0) != R + 1 : M != R) || !stream_of({y, x, a, b, ids, gain, cu}, &s))
+      (gain && gain->size(0) != n) || (cu ? cu->size(0) != R + 1 : M != R) || (y->requires_grad() && c10::GradMode::is_enabled()) ||
+      !stream_of({y, x, a, b, ids, gain, cu}, &s))
     return not_here();
   int64_t need = 0;
   if (lib.adapters_workspace((int)M, (int)N, (int)K, (int)r, &need) != 0) return not_here();
@@ -448,6 +450,7 @@ PyObject* adapters_(PyObject* const* args) {
         return lib.adapters(xp, ap, bp, ip, cp, gp, yp, wp, need, (int)M, (int)N, (int)K, (int)r, (int)n, (int)R, xs, ys, s);
       }) != 0)
     return not_here();
+  if (!y->is_inference()) y->unsafeGetTensorImpl()->bump_version();       // a graph that has saved y must not go back through it
   return Py_NewRef(args[0]);
 }
 
