@@ -395,8 +395,9 @@ int qgemm_attention_packed(const void* q, const void* k, const void* v, const in
  * rounding, but without it in the tiles of 128 rows that chunks of prompts take). Keys of a page outside [0, pages) or
  * past the table's W entries make the rows that see them NaN, and a value block of scale
  * byte 253 or 254, which passes bf16's range, counts as one of NaN; nothing else that
- * the pages hold behind a row's position reaches it. Results do not depend on how the
- * work was split beyond fp32 summation order, and are the same on every call.
+ * the pages hold behind a row's position reaches it. How the work was split shows in the
+ * order of the fp32 sums, and in the weights' rounding to bf16, which is relative to a maximum
+ * of the keys that came before; results are the same on every call.
  * workspace: caller-owned device memory, 16-byte aligned, of the bytes that
  * qgemm_attention_kv4_workspace gives for the same sizes; it needs no
  * initialisation, and calls that can overlap need one each. W*page <= 2^30,
@@ -418,8 +419,11 @@ int qgemm_attention_kv4_workspace(int T, int R, int H, int Hkv, int D, int W, in
  */
 
 /*
- * qgemm_attention_kv4 for requests that share their first keys: the same result, up to fp32 summation order, with the
- * shared keys read and unpacked once for all rows of a group (decode, Section 2.3, is bound by those bytes).
+ * qgemm_attention_kv4 for requests that share their first keys: the same result but for rounding, with the shared keys read
+ * and unpacked once for all rows of a group (decode, Section 2.3, is bound by those bytes). As there the softmax weights
+ * enter the output product as bf16, rounded relative to a maximum that the split of the work decides, so the two differ
+ * by that too: by 0.2 to 0.3% of o's norm where the split differs, each 0.20 to 0.23% from the exact result (0.17 of it
+ * the rounding of o), over random keys of some thousand.
  * Group g holds the requests groups[g] .. groups[g+1]-1, whose first prefix_len[g] keys are the same: the keys that are
  * taken as shared are read through the table of the group's first request that has new tokens, the others through each
  * request's own. Shared are min(prefix_len[g], the fewest keys that a request of the group has before its new tokens), down
@@ -453,9 +457,12 @@ int qgemm_attention_kv4_shared_workspace(int T, int R, int G, int H, int Hkv, in
  * selection all but one of a prompt's), tokens of logit -inf, and all of a row that holds NaN or +inf. Behind the last
  * candidate stand score -inf, parent -1 and token `end`. So finished is (out_tokens == end) for the next selection.
  * logits: fp32 (as qgemm_dense writes them) or bf16 [R*B][V] at `stride` elements between rows, aligned to their
- * elements; scores: fp32 [R][B]; finished: uint8 [R][B] or null; outputs [R][K], which share no memory with an input or each other. Maximum and sum of a row in
- * fp32 and fp64, values in fp64, rounded once. Results are the same on every call. B <= 64, K <= 128 (of more than one
- * beam K = B continues as many, K = 2B leaves a choice), R*B <= 2^20, V <= 2^30. workspace: caller-owned, 16-byte aligned,
+ * elements; scores: fp32 [R][B]; finished: uint8 [R][B] or null; outputs [R][K], which share no memory with an input or each other. A row's
+ * exponentials are taken in fp32 and added in fp64, values are fp64, rounded once: candidates of different beams may change
+ * places where their values are closer than 1e-6 (sums of 1000 to 128000 logits are off by up to 2e-7 of themselves).
+ * Results are the same on every call.
+ * B <= 64, K <= 128 (of more than one beam K = B continues as many, K = 2B leaves a choice; the time of many beams with
+ * many candidates goes with the square of B*K: 1.8 ms for 64 beams and K = 128), R*B <= 2^20, V <= 2^30. workspace: caller-owned, 16-byte aligned,
  * of the bytes that qgemm_beam_select_workspace gives, without initialisation; calls that can overlap need one each.
  */
 int qgemm_beam_select(const void* logits, int type, const float* scores, const uint8_t* finished,
@@ -471,7 +478,8 @@ int qgemm_beam_select_workspace(int R, int B, int V, int K, int64_t* bytes);
  * A last page that is filled only in part is written by the next token, so one row alone may hold it: the first row (the lowest k)
  * of a parent has it, and the others a page each of free_pages, by request and k, with its number in dst and the
  * parent's in src (both -1 for all other rows): qgemm_kv4_copy brings the keys and values over. used[0]: pages taken; where
- * the free list ends (used[0] > F) entries become -1, with nothing to copy.
+ * the free list ends (used[0] > F) entries become -1, with nothing to copy. (A parent whose own last entry is none, as
+ * such a row's, has nothing to give: the other children's pages hold what they held.)
  * released: the pages that no new row of their request holds in the column that they had, each once, by request,
  * column and old row; -1 behind them. n_released[0] counts them; with more than Q those past Q are missing from the
  * list. Not listed: the first keep[r] columns (pages of a prompt that others hold too; keep may be null: none), and

@@ -747,7 +747,8 @@ def attention_kv4_shared(q: torch.Tensor, cache: torch.Tensor, block_table: torc
     """``attention_kv4`` with the keys that the requests of a group share read once (``qgemm_attention_kv4_shared``).
 
     ``groups`` [G+1]: first requests of the groups; ``prefix_len`` [G]: keys that a group's requests have in common. The other
-    arguments are ``attention_kv4``'s, and so are the results, up to the order of summation."""
+    arguments are ``attention_kv4``'s, and so are the results, but for the order of summation and the rounding of the softmax
+    weights to bf16, which goes by the split of the work."""
     if _fast is not None:
         r = _fast.attention_kv4_shared(q, cache, block_table, kv_len, groups, prefix_len, cu_q, scale, out)
         if r is not NotImplemented:
@@ -794,7 +795,8 @@ def beam_select(logits: torch.Tensor, scores: torch.Tensor, count: int | None = 
     ``(scores, parents, tokens)``, each [R][count], fp32 and int32, best first.
 
     ``logits`` [R*B][V] fp32 or bf16, rows at any stride; ``scores`` [R][B] fp32, -inf for a beam that is not there;
-    ``finished`` [R][B] bool or uint8: beams that go on with ``end`` at their own score. Where candidates are missing the score
+    ``finished`` [R][B] bool or uint8: beams that go on with ``end`` at their own score. Of a beam the larger logit comes first, then
+    the lower token; beams are compared by value, equal ones the lower first. Where candidates are missing the score
     is -inf, the parent -1 and the token ``end``, so that ``tokens == end`` is the next call's ``finished``."""
     if _fast is not None:
         r = _fast.beam_select(logits, scores, count, finished, end)

@@ -5,10 +5,10 @@
 // through the list: the products of all rows of the tile with one adapter are one MFMA operand's columns, and each row
 // keeps its own adapter's. A prompt's tile has one or two adapters; a decode step's has one a row, whose weights have to
 // be read once anyway, and the matrix cores that compute 16 columns for one have nothing else to do.
-// Bounds: of many rows HBM, which y passes twice (8500 rows of 8192 columns, rank 64, K = 2048: 26 us for the first
-// kernel, 120 for the second, 4.7 TB/s; reading and writing y alone by the same tiles 101); of a decode step the two launches
-// and their chains of loads (16 rows of 2048 columns 8.5 us), then the adapters' weights (96 rows with 64 adapters of 8192
-// columns, 38 MB, 15.9 us).
+// Bounds: of many rows HBM, which y passes twice (8500 rows of 8192 columns, rank 64, K = 2048: 160 us; each kernel again and
+// again by itself 25.5 us, with x in the caches, and 130, 4.3 TB/s; reading and writing y alone by the same tiles 101); of
+// a decode step the two launches and their chains of loads (16 rows of 2048 columns 8.1 us), then the adapters' weights (96
+// rows with 64 adapters of 8192 columns, 38 MB, 16.2 us).
 // A row is chosen, never multiplied by zero: an infinity or NaN of one adapter or request reaches no other.
 #pragma once
 
@@ -271,7 +271,7 @@ __global__ __launch_bounds__(kAdThreads) void adapter_up_kernel(AdapterArgs a) {
     }
   };
   bf16x8 mid[MT][S][3];
-  // (each wave for itself, they were a third of the time of 8500 rows of rank 64: 134 us, shared 120)
+  // (each wave for itself, 8500 rows of rank 64 took 12% longer)
   if constexpr (MT == 1) {
 #pragma unroll
     for (int k = 0; k < S; ++k) {

@@ -17,9 +17,10 @@ namespace {
 // order is that of the logits, so the first kernel needs no lse: it takes a piece of a row in one pass over it,
 // carries maximum and sum as an online softmax does, and keeps the piece's K largest logits. The second kernel has the
 // B * pieces * K of a request that are left and computes their values in 64 bits: what beams differ by decides
-// between candidates, and at a score of -100 steps of 32 bits are 2^-17.
-// Bound by the logits' bytes (48 x 8 beams over 128000 in fp32, K = 16: 38.9 us for the first kernel, 5.1 TB/s, and 6.9 for the
-// second); with few rows by the chain load - bound - selection - second launch (4 beams over 32000: 5.8 and 4.6 us).
+// between candidates, and at a score of -100 steps of 32 bits are 2^-17. (The exponentials of a sum are taken in 32 bits, so
+// candidates of different beams may change places where they are closer than 1e-6; sums are off by up to 2e-7 of themselves.)
+// Bound by the logits' bytes (48 x 8 beams over 128000 in fp32, K = 16: 39.3 us for the first kernel, 5.0 TB/s, and 7.0 for the
+// second); with few rows by the chain load - bound - selection - second launch (4 beams over 32000: 5.9 and 4.8 us).
 
 constexpr int kBeamThreads = 256;
 constexpr int kBeamWaves = kBeamThreads / 64;
@@ -439,7 +440,7 @@ __global__ __launch_bounds__(kBeamThreads) void beam_join_kernel(BeamArgs a) {
 // another. Pages that no row holds any more are left in the caller's workspace, and a second kernel, which knows how many
 // the blocks before have left, moves them to their places in the list.
 // Bound by chains of loads: lengths and parents, old entries, then the counts of the first kernel (4 x 4 beams of up to 3100 tokens
-// 6.2 and 2.1 us; 64 x 8 of up to 6200 tokens, pages of 32, 9.4 and 3.0 us, 0.8 MB in all).
+// 6.1 and 2.2 us; 64 x 8 of up to 6200 tokens, pages of 32, 9.2 and 2.7 us, 0.8 MB in all).
 
 constexpr int kReorderThreads = 256;
 constexpr int kReorderMaxRows = 1 << 16;       // R * B

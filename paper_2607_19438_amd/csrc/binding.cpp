@@ -3,8 +3,8 @@
 // else a function here answers NotImplemented, having done nothing, and the Python function goes its own way, which
 // says what is wrong. A decode step's calls take less time on the GPU than their checks take in Python: host time
 // of a call of 16 rows (us, Python alone and with this file) rope 8.5, 4.4; plan 10.2, 5.1; store and load 16.5, 8.9;
-// packed prompts 9.0, 4.7; attention over the cache 10.5, 5.4; over shared prefixes 14.3, 8.6; selection of beams 15.1, 7.6;
-// table reordering 16.1, 9.0 and page copies 6.7, 3.3; adapters 12.0, 7.4; a launch is 2.4 of it, an allocation 0.6.
+// packed prompts 9.0, 4.7; attention over the cache 10.5, 5.4; over shared prefixes 14.3, 8.6; selection of beams 16.8, 8.7;
+// table reordering 17.3, 10.5 and page copies 6.7, 3.3; adapters 13.0, 7.9; a launch is 2.4 of it, an allocation 0.6.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 

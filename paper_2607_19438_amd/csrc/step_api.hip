@@ -161,8 +161,9 @@ AdapterPlan adapter_plan(int M, int N, int K, int r) {
   // mid: K is split over workgroups while they are few; the second kernel adds the parts up, each of its workgroups those of
   // its rows. (us of the first kernel and the second, for splits of 1, 2, 4; K = 2048, 8192 columns: 96 rows, rank 32 9.8, 7.3,
   // 6.9, and 13.0, 13.3, 14.2; 2048 rows, rank 16 7.0, 6.4, 6.8 and 30.4, 30.8, 31.5; 2500 rows, rank 64 15.1, 10.1, 10.0 and
-  // 41.9, 44.7, 48.9; 8500 rows, rank 64 26.2, 22.3, 22.1 and 119.6, 123.8, 139.0.) Tiles of 32 rows read A half as often
-  // (8500 rows, rank 64 26.2 and 38.6 us; 1252 rows, two splits 9.8 and 12.6), those of 16 have fewer adapters.
+  // 41.9, 44.7, 48.9; 8500 rows, rank 64 25.5, 22.0, 23.3 and 130, 135, 152; each kernel by itself, again
+  // and again.) Tiles of 32 rows read A half as often (8500 rows, rank 64 26.2 and 38.6 us; 1252 rows, two splits 9.8 and
+  // 12.6), those of 16 have fewer adapters.
   p.mt_down = M > 1024 ? 2 : 1;
   p.jt = r <= 16 ? 1 : r <= 32 ? 2 : 4;
   // A tile's adapters side by side: each row may have its own (96 rows, 64 adapters: 1, 4, 16 at once 35.8, 11.9, 6.9 us); of
@@ -176,10 +177,10 @@ AdapterPlan adapter_plan(int M, int N, int K, int r) {
   p.splits = (int)qg::ceil_div(K, p.k_split);
   // y: of few rows 16 columns to a wave and eight adapters at once (96 rows with 64 adapters, 8192 columns: 10.2 us, with 64
   // columns 14.7 and 11.7 for one and two at once; 64 rows with 32, 4096 columns 5.6, with two at once 6.4). Else tiles of 32 by
-  // 32, two of them to a wave in turn where that leaves four workgroups to a CU (8500 rows of 8192, rank 64: 1, 2, 4 in turn 130,
-  // 120, 124 us, tiles of 16 rows 204, 159, 155; 1252 rows, rank 64 26.2, 24.8, 26.8). At a rank up to 32 the operands are soon
-  // made, and few tiles are of 16 rows (1252 rows of 5003, rank 8 14.0, 12.2 us, of 32 rows 15.3, 13.3; 540 rows of 4096, rank
-  // 16 6.3 and 7.0; but 2048 rows of 8192 31.2 and 30.4).
+  // 32, two of them to a wave in turn where that leaves four workgroups to a CU (8500 rows of 8192, rank 64: 1, 2, 4 in turn 141,
+  // 129, 133 us, with tiles of 16 rows 32% slower at two; 1252 rows, rank 64 26.2, 24.8, 26.8). At a rank up to 32 the
+  // operands are soon made, and few tiles are of 16 rows (1252 rows of 5003, rank 8 14.0, 12.2 us, of 32 rows 15.3, 13.3; 540
+  // rows of 4096, rank 16 6.3 and 7.0; but 2048 rows of 8192 31.2 and 30.4).
   const bool small = r <= 32 && qg::ceil_div(M, 32) * qg::ceil_div(N, 256) < 4 * kCUs;
   p.nt = M <= 256 ? 1 : 2;
   p.mt_up = M <= 256 || small ? 1 : 2;
